@@ -68,6 +68,10 @@ extern "C" {
 #define KV_F32 0
 #define KV_BF16 1
 
+/* ---- 8-bit code types (kv_paged_cache) -------------------------------------------------------- */
+#define KV_E4M3 0 /* OCP 8-bit floating point: 4 exponent bits, 3 mantissa bits, no infinities       */
+#define KV_INT8 1 /* -127 .. 127                                                                     */
+
 /* ---- depth-profile families (section 3.3) ----------------------------------------------------- */
 #define KV_PROFILE_GLOBAL 0   /* a(l) = a0                                   (1 parameter)      */
 #define KV_PROFILE_SEGMENTS 1 /* a(l) = a[floor(n_seg * l / n_layers)]       (n_seg parameters) */
@@ -387,6 +391,100 @@ size_t kv_decode_workspace_bytes(const kv_cache_batch* cb);
 int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, void* v_cache,
                         const void* k_new, const void* v_new, float scale, float* out, void* ws,
                         size_t ws_bytes, void* stream);
+
+/* A batch of caches held in 8 bits, in blocks that the problems share (section 4.3's generation over
+ * the kept rows, for caches of unequal and growing length).  A block holds block_rows rows (16, 32, 64 or
+ * 128) of every kv head: pools k, v [n_blocks][h_kv][block_rows][d] of 8-bit codes (KV_E4M3 or
+ * KV_INT8) and scales k_scale, v_scale [n_blocks][h_kv] fp32; an element is code * scale.  Row r of
+ * problem p is row r % block_rows of block table[p][r / block_rows] (table [n_prob][table_stride],
+ * len [n_prob]: the rows in use).  Every pointer is a device pointer, and table and len are read on
+ * the device alone: they may change between the replays of a captured graph.  max_len bounds
+ * the lengths (rows from max_len on are not seen) and sizes launches and workspaces.
+ *   - Scales as the library writes them are the least power of two s with max|x| <= 448 s (KV_E4M3) or
+ *     127 s (KV_INT8) over the block's finite elements (at least 2^-126), 0 for zeros; a code is x / s
+ *     rounded to nearest even.  An infinity takes the largest code of its sign; a NaN stays one
+ *     in KV_E4M3 and becomes 0 in KV_INT8.
+ *   - A table entry outside [0, n_blocks) is a missing block: its rows are not written, and not seen.
+ *   - Rows of a block that no problem has written may hold anything.
+ * dtype: of queries, new rows and outputs.  n_blocks * block_rows and table_stride * block_rows below
+ * 2^31, h_q / h_kv <= 16, h_kv <= 4096, d in {64, 128}, max_len <= 2^24, else KV_ERR_SHAPE; pools
+ * 16-byte aligned.  kv_paged_tables uses n_prob, block_rows, n_blocks, table_stride, table and len
+ * alone. */
+typedef struct kv_paged_cache {
+  int32_t dtype;
+  int32_t qtype;
+  int32_t n_prob;
+  int32_t h_q;
+  int32_t h_kv;
+  int32_t d;
+  int32_t block_rows;
+  int32_t n_blocks;
+  int32_t table_stride;
+  int32_t max_len;
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t* table;
+  int32_t* len;
+} kv_paged_cache;
+
+/* Block tables and slots for add[p] new rows of every problem behind its len_in[p] rows, on the
+ * device (no value is read by the host).  With R = block_rows, have_p = ceil(len_in[p] / R) and
+ * need_p = ceil((len_in[p] + add[p]) / R):
+ *   tok_off[p] = sum_{q < p} add[q], p = 0 .. n_prob (the new rows of the batch in order);
+ *   blk_off[p] = taken_in + sum_{q < p} (need_q - have_q), p = 0 .. n_prob;
+ *   table[p][have_p + i] = free_blocks[blk_off[p] + i], i < need_p - have_p (other entries stay);
+ *   slots[tok_off[p] + i] = table[p][r / R] * R + r % R, r = len_in[p] + i: where row i of the problem's
+ *     new rows goes; -1 from tok_off[n_prob] on (n_slots may count a padded batch);
+ *   len[p] = len_in[p] + add[p];  taken_out = blk_off[n_prob].
+ * len_in: NULL is 0, and it may be len itself.  add: NULL is 1.  free_blocks [n_free]: NULL is
+ * 0, 1, 2, ..  taken_in, taken_out: one value each, the entries of free_blocks used so far (NULL: 0,
+ * and not written); they may be the same.  Where the free list ends, or a row lies past the table, entries and slots
+ * are -1 and taken_out still counts the blocks asked for (rows past the table ask for none).  Rows
+ * past n_slots get their blocks and no slot.  Lengths are taken as at least 0 and at most 2^24; the
+ * new rows of a call must be fewer than 2^31.  len, table, tok_off, blk_off and slots must not overlap. */
+int kv_paged_tables(const kv_paged_cache* pc, const int32_t* len_in, const int32_t* add,
+                    const int32_t* free_blocks, int32_t n_free, const int32_t* taken_in,
+                    int32_t* taken_out, int32_t* tok_off, int32_t* blk_off, int32_t* slots,
+                    int32_t n_slots, void* stream);
+
+/* New rows into the blocks: token t's row of head g, k_new / v_new + t * tok_stride + g * d elements
+ * (tok_stride 0: h_kv * d; at least that, and whole 16-byte chunks), into slot slots[t] (as
+ * kv_paged_tables gives them; one outside [0, n_blocks * block_rows) is skipped).  Tokens of one block have to be
+ * consecutive in the batch, in consecutive slots, the first behind the block's rows in use; each block
+ * once in a call.  A block's first row sets its scale; where later rows need a larger scale, the codes
+ * of the rows it holds are rounded to that.  Rows behind the last new one stay as they were. */
+int kv_paged_append(const kv_paged_cache* pc, const void* k_new, const void* v_new, int64_t tok_stride,
+                    const int32_t* slots, int32_t n_tok, void* stream);
+
+/* kv_compact_cache_ex into the blocks (sections 1 and 3.1): rows 0 .. B_p - 1 of problem p and head g are
+ * the rows of the selected positions in ascending order, then the last keep_tail positions, each block
+ * coded with its scale.  pr, k, v, sel_idx, budget, keep_tail and the budgets as there (budget <= 8192);
+ * pc with pr's n_prob, dtype, h_kv and d, and B_p + keep_tail rows in its table (KV_ERR_SHAPE).  A selected
+ * position outside [0, L_p) becomes a row of zeros.  len is not read. */
+int kv_paged_compact(const kv_problem* pr, const void* k, const void* v, const int32_t* sel_idx,
+                     int32_t budget, int32_t keep_tail, const int32_t* budget_host,
+                     const int32_t* budget_dev, const kv_paged_cache* pc, void* stream);
+
+/* Bytes of device workspace kv_paged_attention needs (0 if none; 256-byte alignment).  Returns 0 for
+ * invalid arguments as well. */
+size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_tok, int32_t max_q);
+
+/* Attention of the last tokens of every problem over its cache (one generated token, a few drafted ones, or
+ * a further prompt turn; their own rows are in the cache already).  Problem p has the tokens
+ * tok_off[p] .. tok_off[p+1] - 1 (n_p of them, at most max_q; tok_off [n_prob + 1] on the device, NULL:
+ * one token each, then n_tok = n_prob and max_q = 1).  Token j of problem p sees the rows
+ * r <= len[p] - n_p + j:
+ *   out[t,h,:] = sum_r softmax_r(scale <q[t,h], k[r]>) v[r],  kv head h / (h_q / h_kv);
+ * 0 where it sees none.  q: token t at t * q_stride elements (0: h_q * d; at least that, whole 16-byte
+ * chunks), [h_q][d]; out [n_tok][h_q][d] of the queries' type.  Logits, softmax and sums in fp32; the weights enter
+ * the product with V with at least 16 significant bits (bf16 queries; 24 for fp32).  The outputs of
+ * tokens outside every problem (a padded batch) stay as they were, and so do a problem's whose tok_off reaches outside
+ * [0, n_tok] or spans more than max_q.  Calls that overlap on one workspace race. */
+int kv_paged_attention(const kv_paged_cache* pc, const void* q, int64_t q_stride, const int32_t* tok_off,
+                       int32_t n_tok, int32_t max_q, float scale, void* out, void* ws, size_t ws_bytes,
+                       void* stream);
 
 /* Per-layer budgets that fall with depth at the total of a uniform `budget` (section 3.1: the runs
  * use such an allocation; the paper prints no schedule), host-only.  With

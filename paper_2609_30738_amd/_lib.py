@@ -31,6 +31,9 @@ SIGMA_ROWS = {"group_mean": KV_SIGMA_GROUP_MEAN, "all_rows": KV_SIGMA_ALL_ROWS}
 KV_F32 = 0
 KV_BF16 = 1
 
+KV_E4M3 = 0
+KV_INT8 = 1
+
 KV_PROFILE_GLOBAL = 0
 KV_PROFILE_SEGMENTS = 1
 KV_PROFILE_CURVE = 2
@@ -48,7 +51,9 @@ SYMBOLS = ("kv_strerror", "kv_version", "kv_workspace_bytes", "kv_candidate_stri
            "kv_mmr_select_compact", "kv_mmr_select_scored", "kv_window_candidates",
            "kv_candidates_workspace_bytes", "kv_mmr_select_candidates", "kv_evict_pass",
            "kv_compact_cache", "kv_compact_cache_ex", "kv_decode_workspace_bytes",
-           "kv_decode_attention", "kv_pyramid_budgets", "kv_depth_profile")
+           "kv_decode_attention", "kv_paged_tables", "kv_paged_append", "kv_paged_compact",
+           "kv_paged_attention", "kv_paged_attention_workspace_bytes", "kv_pyramid_budgets",
+           "kv_depth_profile")
 
 
 class KvError(RuntimeError):
@@ -68,6 +73,12 @@ class KvCacheBatch(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("n_prob", ctypes.c_int32), ("h_q", ctypes.c_int32),
                 ("h_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("row_stride", ctypes.c_int32),
                 ("len_host", ctypes.c_void_p), ("len_dev", ctypes.c_void_p)]
+
+
+class KvPagedCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "qtype", "n_prob", "h_q", "h_kv", "d", "block_rows",
+                                              "n_blocks", "table_stride", "max_len")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "len")]
 
 
 class KvSelectOpts(ctypes.Structure):
@@ -132,6 +143,13 @@ def lib() -> ctypes.CDLL:
         h.kv_decode_workspace_bytes.argtypes = [cb]
         h.kv_decode_workspace_bytes.restype = sz
         h.kv_decode_attention.argtypes = [cb, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, sz, vp]
+        pc, i64 = ctypes.POINTER(KvPagedCache), ctypes.c_int64
+        h.kv_paged_tables.argtypes = [pc, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp]
+        h.kv_paged_append.argtypes = [pc, vp, vp, i64, vp, i32, vp]
+        h.kv_paged_compact.argtypes = [pr, vp, vp, vp, i32, i32, vp, vp, pc, vp]
+        h.kv_paged_attention_workspace_bytes.argtypes = [pc, i32, i32]
+        h.kv_paged_attention_workspace_bytes.restype = sz
+        h.kv_paged_attention.argtypes = [pc, vp, i64, vp, i32, i32, ctypes.c_float, vp, vp, sz, vp]
         h.kv_pyramid_budgets.argtypes = [i32, i32, ctypes.c_double, ctypes.POINTER(ctypes.c_int32)]
         h.kv_depth_profile.argtypes = [i32, ctypes.POINTER(ctypes.c_double), i32, i32,
                                        ctypes.POINTER(ctypes.c_float)]
@@ -140,6 +158,7 @@ def lib() -> ctypes.CDLL:
                      "kv_window_base_scores", "kv_mmr_select", "kv_mmr_select_ex",
                      "kv_mmr_select_scored", "kv_window_candidates", "kv_mmr_select_candidates",
                      "kv_evict_pass", "kv_compact_cache", "kv_compact_cache_ex", "kv_decode_attention",
+                     "kv_paged_tables", "kv_paged_append", "kv_paged_compact", "kv_paged_attention",
                      "kv_pyramid_budgets", "kv_depth_profile"):
             getattr(h, name).restype = ctypes.c_int
         _LIB = h
@@ -477,6 +496,147 @@ def decode_attention(cb: CacheBatch, q, k_cache, v_cache, k_new, v_new, scale: f
                                      _ptr(v_new), float(scale), _ptr(out), _ptr(ws),
                                      0 if ws is None else ws.numel() * ws.element_size(),
                                      _stream(stream)), "kv_decode_attention")
+
+
+class PagedCache:
+    """A batch of 8-bit caches in shared blocks (kv_paged_cache), around the caller's device tensors:
+    k, v [n_blocks, h_kv, block_rows, d] (torch.float8_e4m3fn or int8), k_scale, v_scale
+    [n_blocks, h_kv] fp32, table [n_prob, table_stride] int32 and lens [n_prob] int32.  dtype ("bf16" or
+    "f32") is that of queries, new rows and outputs; max_len bounds the lengths (default: what the
+    table holds)."""
+
+    def __init__(self, dtype: str, h_q: int, k, v, k_scale, v_scale, table, lens,
+                 max_len: Optional[int] = None):
+        import torch
+        n_blocks, h_kv, block_rows, d = k.shape
+        if k.dtype not in (torch.float8_e4m3fn, torch.int8) or v.dtype != k.dtype or v.shape != k.shape:
+            raise ValueError("k and v must be float8_e4m3fn or int8 tensors of one shape")
+        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or \
+                k_scale.numel() != n_blocks * h_kv or v_scale.numel() != n_blocks * h_kv:
+            raise ValueError("k_scale and v_scale must be float32 [n_blocks, h_kv]")
+        self._tables(table, lens, n_blocks, block_rows)
+        self.dtype_name = dtype
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        s = self.struct
+        s.dtype = KV_BF16 if dtype == "bf16" else KV_F32
+        s.qtype = KV_E4M3 if k.dtype == torch.float8_e4m3fn else KV_INT8
+        s.h_q, s.h_kv, s.d = int(h_q), h_kv, d
+        s.max_len = min(table.shape[1] * block_rows, 1 << 24) if max_len is None else int(max_len)
+        s.k, s.v = _ptr(k).value, _ptr(v).value
+        s.k_scale, s.v_scale = _ptr(k_scale).value, _ptr(v_scale).value
+
+    def _tables(self, table, lens, n_blocks, block_rows):
+        _int32(table, "table")
+        _int32(lens, "lens")
+        if table.dim() != 2 or lens.numel() != table.shape[0]:
+            raise ValueError("table must be [n_prob, table_stride] and lens [n_prob]")
+        self.table, self.lens = table, lens
+        self.struct = KvPagedCache(n_prob=table.shape[0], block_rows=int(block_rows), n_blocks=int(n_blocks),
+                                   table_stride=table.shape[1], table=_ptr(table).value, len=_ptr(lens).value)
+
+    @classmethod
+    def for_tables(cls, block_rows: int, n_blocks: int, table, lens) -> "PagedCache":
+        """A cache without pools: what paged_tables needs."""
+        self = cls.__new__(cls)
+        self._tables(table, lens, n_blocks, block_rows)
+        return self
+
+    @classmethod
+    def allocate(cls, dtype: str, qtype: str, h_q: int, h_kv: int, d: int, block_rows: int, n_blocks: int,
+                 n_prob: int, table_stride: int, max_len: Optional[int] = None, device=None) -> "PagedCache":
+        """Empty pools (their contents are undefined), a table of missing blocks and lengths of 0."""
+        import torch
+        dev = torch.device("cuda") if device is None else torch.device(device)
+        qt = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}[qtype]
+        pool = lambda: torch.empty(n_blocks, h_kv, block_rows, d, dtype=torch.uint8, device=dev).view(qt)
+        scales = lambda: torch.empty(n_blocks, h_kv, dtype=torch.float32, device=dev)
+        return cls(dtype, h_q, pool(), pool(), scales(), scales(),
+                   torch.full((n_prob, table_stride), -1, dtype=torch.int32, device=dev),
+                   torch.zeros(n_prob, dtype=torch.int32, device=dev), max_len)
+
+    @property
+    def n_prob(self) -> int:
+        return self.struct.n_prob
+
+    def ref(self):
+        return ctypes.byref(self.struct)
+
+
+def _int32(t, name: str):
+    import torch
+    if t is not None and t.dtype != torch.int32:
+        raise ValueError(f"{name} must be an int32 tensor")
+
+
+def _token_rows(pc: PagedCache, t, heads: int, name: str):
+    """Address and token stride of [n, heads, d] rows; tokens may lie apart (a slice of a projection)."""
+    import torch
+    want = torch.bfloat16 if pc.struct.dtype == KV_BF16 else torch.float32
+    if not t.is_cuda or t.dtype != want or t.dim() != 3 or t.shape[1:] != (heads, pc.struct.d):
+        raise ValueError(f"{name} must be a device tensor [tokens, {heads}, {pc.struct.d}] of {want}")
+    if (t.stride(2) != 1 or t.stride(1) != pc.struct.d) and t.numel() > 0:
+        raise ValueError(f"the heads of a token must be contiguous in {name}")
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * pc.struct.d)
+
+
+def paged_tables(pc: PagedCache, len_in, add, free_blocks, taken_in, taken_out, tok_off, blk_off, slots,
+                 n_free: Optional[int] = None, stream=None) -> None:
+    """kv_paged_tables: writes pc.table, pc.lens, tok_off, blk_off [n_prob + 1], slots and taken_out.
+    len_in None: empty caches; add None: one row each; free_blocks None: n_free blocks 0, 1, 2, ..
+    (default: the pool's)."""
+    for t, name, n in ((len_in, "len_in", pc.n_prob), (add, "add", pc.n_prob), (tok_off, "tok_off", pc.n_prob + 1),
+                       (blk_off, "blk_off", pc.n_prob + 1), (taken_in, "taken_in", 1),
+                       (taken_out, "taken_out", 1), (free_blocks, "free_blocks", 0), (slots, "slots", 0)):
+        _int32(t, name)
+        if t is not None and t.numel() < n:
+            raise ValueError(f"{name} must have {n} elements")
+    if free_blocks is not None:
+        n_free = free_blocks.numel() if n_free is None else min(int(n_free), free_blocks.numel())
+    elif n_free is None:
+        n_free = pc.struct.n_blocks
+    _check(lib().kv_paged_tables(pc.ref(), _ptr(len_in), _ptr(add), _ptr(free_blocks), int(n_free),
+                                 _ptr(taken_in), _ptr(taken_out), _ptr(tok_off), _ptr(blk_off), _ptr(slots),
+                                 0 if slots is None else slots.numel(), _stream(stream)), "kv_paged_tables")
+
+
+def paged_append(pc: PagedCache, k_new, v_new, slots, stream=None) -> None:
+    """kv_paged_append: k_new, v_new [tokens, h_kv, d], tokens of one stride (slices of a projection's
+    output, for instance); slots [tokens] int32."""
+    kp, ks = _token_rows(pc, k_new, pc.struct.h_kv, "k_new")
+    vp, vs = _token_rows(pc, v_new, pc.struct.h_kv, "v_new")
+    _int32(slots, "slots")
+    if k_new.shape != v_new.shape or ks != vs or slots.numel() < k_new.shape[0]:
+        raise ValueError("k_new and v_new must have one shape and token stride, slots an entry per token")
+    _check(lib().kv_paged_append(pc.ref(), kp, vp, ks, _ptr(slots), k_new.shape[0], _stream(stream)),
+           "kv_paged_append")
+
+
+def paged_compact(batch: Batch, k, v, sel_idx, budget: int, keep_tail: int, pc: PagedCache,
+                  budgets: Optional[Budgets] = None, stream=None) -> None:
+    """kv_paged_compact: the selected rows of k and v and the tail into pc's blocks."""
+    bh, bd = budgets.pointers() if budgets is not None else (None, None)
+    _check(lib().kv_paged_compact(batch.ref(), _ptr(k), _ptr(v), _ptr(sel_idx), int(budget), int(keep_tail),
+                                  bh, bd, pc.ref(), _stream(stream)), "kv_paged_compact")
+
+
+def paged_attention_workspace_bytes(pc: PagedCache, n_tok: Optional[int] = None, max_q: int = 1) -> int:
+    n_tok = pc.n_prob if n_tok is None else n_tok
+    return int(lib().kv_paged_attention_workspace_bytes(pc.ref(), int(n_tok), int(max_q)))
+
+
+def paged_attention(pc: PagedCache, q, scale: float, out, tok_off=None, max_q: int = 1, ws=None,
+                    stream=None) -> None:
+    """kv_paged_attention: q [tokens, h_q, d] (tokens of one stride), out the same shape, contiguous;
+    tok_off [n_prob + 1] int32 for several tokens to a problem, at most max_q each."""
+    qp, qs = _token_rows(pc, q, pc.struct.h_q, "q")
+    _int32(tok_off, "tok_off")
+    if out.dtype != q.dtype or out.shape != q.shape:
+        raise ValueError("out must have the shape and type of q")
+    if tok_off is not None and tok_off.numel() < pc.n_prob + 1:
+        raise ValueError("tok_off must have n_prob + 1 elements")
+    _check(lib().kv_paged_attention(pc.ref(), qp, qs, _ptr(tok_off), q.shape[0], int(max_q), float(scale),
+                                    _ptr(out), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                    _stream(stream)), "kv_paged_attention")
 
 
 def pyramid_budgets(budget: int, n_layers: int, beta: float) -> np.ndarray:

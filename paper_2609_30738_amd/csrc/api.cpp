@@ -11,6 +11,7 @@
 
 #include "kernels.h"
 #include "kvevict.h"
+#include "paged.h"
 
 namespace {
 
@@ -783,6 +784,155 @@ int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, 
   a.part = static_cast<float*>(ws);
   return launch_status(kv::launch_decode(cb->dtype == KV_BF16 ? kv::kDtBf16 : kv::kDtF32, cb->d,
                                          cb->n_prob, a, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+// Checks shared by the paged entry points; fills the kernels' description.  tables: only what the block
+// tables need (the pools and the head layout may be unset).
+int check_paged(const kv_paged_cache* c, kv::Paged* pc, bool tables = false) {
+  if (!c) return KV_ERR_NULL;
+  if (c->n_prob < 1 || c->n_prob > kMaxGrid) return KV_ERR_ARG;
+  if (!c->table || !c->len) return KV_ERR_NULL;
+  if (c->block_rows != 16 && c->block_rows != 32 && c->block_rows != 64 && c->block_rows != 128)
+    return KV_ERR_SHAPE;
+  // slots are 32-bit numbers, and so are a problem's rows
+  if (c->n_blocks < 1 || (int64_t)c->n_blocks * c->block_rows > INT32_MAX) return KV_ERR_SHAPE;
+  if (c->table_stride < 1 || (int64_t)c->table_stride * c->block_rows > INT32_MAX) return KV_ERR_SHAPE;
+  if (!tables) {
+    if (c->dtype != KV_F32 && c->dtype != KV_BF16) return KV_ERR_DTYPE;
+    if (c->qtype != KV_E4M3 && c->qtype != KV_INT8) return KV_ERR_DTYPE;
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return KV_ERR_NULL;
+    if (!aligned16(c->k) || !aligned16(c->v)) return KV_ERR_ARG;
+    if (c->h_kv < 1 || c->h_kv > 4096 || c->h_q < c->h_kv || c->h_q % c->h_kv != 0 || c->h_q / c->h_kv > 16)
+      return KV_ERR_SHAPE;
+    if (c->d != 64 && c->d != 128) return KV_ERR_SHAPE;
+    if (c->max_len < 0 || c->max_len > kMaxLen) return KV_ERR_SHAPE;
+  }
+  pc->dtype = c->dtype == KV_BF16 ? kv::kDtBf16 : kv::kDtF32;
+  pc->qtype = c->qtype == KV_E4M3 ? kv::kQtE4m3 : kv::kQtInt8;
+  pc->n_prob = c->n_prob;
+  pc->h_q = c->h_q;
+  pc->h_kv = c->h_kv;
+  pc->d = c->d;
+  pc->shift = c->block_rows == 16 ? 4 : (c->block_rows == 32 ? 5 : (c->block_rows == 64 ? 6 : 7));
+  pc->n_blocks = c->n_blocks;
+  pc->table_stride = c->table_stride;
+  pc->max_len = c->max_len;
+  pc->k = static_cast<uint8_t*>(c->k);
+  pc->v = static_cast<uint8_t*>(c->v);
+  pc->k_scale = c->k_scale;
+  pc->v_scale = c->v_scale;
+  pc->table = c->table;
+  pc->len = c->len;
+  return KV_OK;
+}
+
+// Elements between two tokens' rows of `heads` heads: 0 is packed; whole 16-byte chunks.
+int check_stride(const kv::Paged& pc, int heads, int64_t* stride) {
+  const int64_t packed = (int64_t)heads * pc.d;
+  if (*stride == 0) *stride = packed;
+  if (*stride < packed || *stride % (pc.dtype == kv::kDtBf16 ? 8 : 4) != 0) return KV_ERR_ARG;
+  return KV_OK;
+}
+
+// Grid limits of an attention call: columns of a problem, and of the grid's axes.
+int check_tokens(const kv::Paged& pc, int32_t n_tok, int32_t max_q) {
+  if (n_tok < 1 || max_q < 1 || max_q > n_tok) return KV_ERR_ARG;
+  const int64_t groups = ((int64_t)max_q * pc.group() + 15) / 16;
+  if (max_q > kMaxLen || groups * pc.h_kv > kMaxGrid) return KV_ERR_SHAPE;
+  return KV_OK;
+}
+
+}  // namespace
+
+int kv_paged_tables(const kv_paged_cache* c, const int32_t* len_in, const int32_t* add,
+                    const int32_t* free_blocks, int32_t n_free, const int32_t* taken_in,
+                    int32_t* taken_out, int32_t* tok_off, int32_t* blk_off, int32_t* slots,
+                    int32_t n_slots, void* stream) {
+  kv::Paged pc{};
+  const int st = check_paged(c, &pc, true);
+  if (st != KV_OK) return st;
+  if (!tok_off || !blk_off || (!slots && n_slots > 0)) return KV_ERR_NULL;
+  if (n_free < 0 || n_slots < 0) return KV_ERR_ARG;
+  const kv::TablesArgs a{len_in, add, free_blocks, n_free, taken_in, taken_out, tok_off, blk_off, slots, n_slots};
+  return launch_status(kv::launch_paged_tables(pc, a, static_cast<hipStream_t>(stream)));
+}
+
+int kv_paged_append(const kv_paged_cache* c, const void* k_new, const void* v_new, int64_t tok_stride,
+                    const int32_t* slots, int32_t n_tok, void* stream) {
+  kv::Paged pc{};
+  int st = check_paged(c, &pc);
+  if (st != KV_OK) return st;
+  if (!k_new || !v_new || !slots) return KV_ERR_NULL;
+  if (!aligned16(k_new) || !aligned16(v_new) || n_tok < 1) return KV_ERR_ARG;
+  st = check_stride(pc, pc.h_kv, &tok_stride);
+  if (st != KV_OK) return st;
+  return launch_status(kv::launch_paged_append(pc, k_new, v_new, tok_stride, slots, n_tok,
+                                               static_cast<hipStream_t>(stream)));
+}
+
+int kv_paged_compact(const kv_problem* pr, const void* k, const void* v, const int32_t* sel_idx,
+                     int32_t budget, int32_t keep_tail, const int32_t* budget_host,
+                     const int32_t* budget_dev, const kv_paged_cache* c, void* stream) {
+  kv::Shape s;
+  int st = check_problem(pr, &s);
+  if (st != KV_OK) return st;
+  kv::Paged pc{};
+  st = check_paged(c, &pc);
+  if (st != KV_OK) return st;
+  if (!k || !v || !sel_idx) return KV_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v)) return KV_ERR_ARG;
+  if (c->dtype != pr->dtype) return KV_ERR_DTYPE;
+  if (pc.n_prob != s.n_prob || pc.h_kv != s.h_kv || pc.d != s.d) return KV_ERR_SHAPE;
+  st = check_budget(pr, budget, keep_tail, budget_host != nullptr || budget_dev != nullptr);
+  if (st != KV_OK) return st;
+  st = check_budgets(pr, budget, keep_tail, budget_host, budget_dev);
+  if (st != KV_OK) return st;
+  if (budget > kMaxCompactBudget) return KV_ERR_BUDGET;
+  // every problem's kept rows fit its row of the table
+  for (int p = 0; p < pr->n_prob; ++p) {
+    const int64_t rows = (int64_t)(budget_host ? budget_host[p] : budget) + keep_tail;
+    if (rows > (int64_t)pc.table_stride << pc.shift) return KV_ERR_SHAPE;
+  }
+  return launch_status(kv::launch_paged_compact(pc, s.lens, s.tok_off, k, v, sel_idx, budget, budget_dev,
+                                                keep_tail, static_cast<hipStream_t>(stream)));
+}
+
+size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* c, int32_t n_tok, int32_t max_q) {
+  kv::Paged pc{};
+  if (check_paged(c, &pc) != KV_OK || check_tokens(pc, n_tok, max_q) != KV_OK) return 0;
+  return align_up(kv::paged_ws_bytes(pc, n_tok, kv::paged_plan(pc, max_q)));
+}
+
+int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride, const int32_t* tok_off,
+                       int32_t n_tok, int32_t max_q, float scale, void* out, void* ws, size_t ws_bytes,
+                       void* stream) {
+  kv::PagedAttnArgs a{};
+  int st = check_paged(c, &a.pc);
+  if (st != KV_OK) return st;
+  if (!q || !out) return KV_ERR_NULL;
+  if (!aligned16(q) || !aligned16(out) || !std::isfinite(scale)) return KV_ERR_ARG;
+  st = check_tokens(a.pc, n_tok, max_q);
+  if (st != KV_OK) return st;
+  if (!tok_off && (n_tok != a.pc.n_prob || max_q != 1)) return KV_ERR_ARG;
+  st = check_stride(a.pc, a.pc.h_q, &q_stride);
+  if (st != KV_OK) return st;
+  const kv::PagedPlan plan = kv::paged_plan(a.pc, max_q);
+  const size_t need = align_up(kv::paged_ws_bytes(a.pc, n_tok, plan));
+  if (need > 0 && (ws_bytes < need || !ws || (reinterpret_cast<uintptr_t>(ws) & (kWsAlign - 1))))
+    return KV_ERR_WORKSPACE;
+  a.q = q;
+  a.q_stride = q_stride;
+  a.tok_off = tok_off;
+  a.n_tok = n_tok;
+  a.max_q = max_q;
+  a.c = scale * kLog2eF;
+  a.out = out;
+  a.split_rows = plan.split_rows;
+  a.n_split = plan.n_split;
+  a.part = static_cast<float*>(ws);
+  return launch_status(kv::launch_paged_attention(a, static_cast<hipStream_t>(stream)));
 }
 
 int kv_pyramid_budgets(int32_t budget, int32_t n_layers, double beta, int32_t* budgets_host) {

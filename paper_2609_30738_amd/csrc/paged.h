@@ -1,0 +1,71 @@
+// The 8-bit paged cache on the host's side: its description as the kernels take it, and the
+// launchers.  Arguments are validated by the C ABI layer before any of these is called.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace kv {
+
+constexpr int kQtE4m3 = 0;
+constexpr int kQtInt8 = 1;
+
+// Pools [n_blocks][h_kv][1 << shift][d] of codes and [n_blocks][h_kv] of scales; row r of problem p is
+// row r % R of block table[p][r / R], R = 1 << shift.
+struct Paged {
+  int dtype, qtype;
+  int n_prob, h_q, h_kv, d;
+  int shift;
+  int n_blocks, table_stride, max_len;
+  uint8_t* k;
+  uint8_t* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t* table;
+  int32_t* len;
+  int group() const { return h_q / h_kv; }
+};
+
+// Block tables and slots (paged_tables.hip).
+struct TablesArgs {
+  const int32_t* len_in;  // [n_prob], null: 0
+  const int32_t* add;     // [n_prob], null: 1
+  const int32_t* free_blocks;  // [n_free], null: block i is i
+  int n_free;
+  const int32_t* taken_in;  // [1], null: 0
+  int32_t* taken_out;       // [1], nullable
+  int32_t* tok_off;         // [n_prob + 1]
+  int32_t* blk_off;         // [n_prob + 1]
+  int32_t* slots;           // [n_slots]
+  int n_slots;
+};
+hipError_t launch_paged_tables(const Paged& pc, const TablesArgs& a, hipStream_t stream);
+
+// Rows into the blocks (paged_store.hip).  tok_stride: elements between the rows of two tokens.
+hipError_t launch_paged_append(const Paged& pc, const void* k_new, const void* v_new, int64_t tok_stride,
+                               const int32_t* slots, int n_tok, hipStream_t stream);
+hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, const int64_t* tok_off, const void* k,
+                                const void* v, const int32_t* sel_idx, int budget, const int32_t* budgets,
+                                int keep_tail, hipStream_t stream);
+
+// Attention over the blocks (paged_attention.hip).
+struct PagedAttnArgs {
+  Paged pc;
+  const void* q;          // token t, head h: q_stride t + h d elements
+  int64_t q_stride;
+  const int32_t* tok_off;  // [n_prob + 1], null: one token per problem
+  int n_tok, max_q;
+  float c;  // softmax scale * log2(e)
+  void* out;  // [n_tok][h_q][d], the queries' type
+  int split_rows, n_split;
+  float* part;  // [n_tok][h_q][n_split][d + 2] when n_split > 1
+};
+struct PagedPlan {
+  int split_rows, n_split;
+};
+PagedPlan paged_plan(const Paged& pc, int max_q);
+size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);
+
+}  // namespace kv

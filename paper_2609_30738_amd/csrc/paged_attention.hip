@@ -1,0 +1,520 @@
+// Attention of the last tokens of every problem over its 8-bit paged cache (kv_paged_attention).
+//
+// paged_attn_kernel: one workgroup of four waves per (split of the rows, kv head and group of columns,
+//   problem).  A column is a (token, query head) pair of the kv head; a wave takes 16 NT of them
+//   against 32 rows a step:
+//     S^T = K Q^T by v_mfma_f32_16x16x32_bf16, 16 rows a tile: the codes are exact in bf16, and the
+//   block's scale multiplies the logits, not the keys.  Lane l of the accumulator holds column l % 16 and
+//   four rows, so the column's running maximum and sum stay in the lane, and the eight weights of a
+//   step's two tiles are exactly the eight of the lane's operand of
+//     O^T = V^T P^T.
+//   Row 4 j + l / 16 of a tile stands for row l / 16 * 4 + j of the accumulator, so that a load of V reads
+//   four whole consecutive rows; the lane's operand of V is transposed in registers.
+//   fp32 queries and weights are taken as three bf16 terms each (24 bits), the weights of bf16 queries as
+//   two: the matrix products lose nothing of the operands beyond that, and accumulate in fp32.
+//   The reference of a column's weights is raised, and the sums rescaled, only when a logit exceeds it by
+//   more than kSlack octaves; weights are 2^(t - m - kSlack), so that none exceeds 1.
+//   The four waves are merged through LDS; with several splits the partial sums go to the workspace and
+//   paged_combine_kernel joins them.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "paged.h"
+#include "paged_codes.h"
+
+namespace kv {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kStep = 32;               // rows of a wave's step
+constexpr int kMaxSplitRows = 2048;     // the blocks and scales of a split are held in LDS
+constexpr int kMaxSplitBlocks = kMaxSplitRows / 16;
+constexpr float kSlack = 8.f;           // octaves a logit may exceed its reference
+constexpr float kSlackScale = 0x1p-8f;  // of the weights
+
+typedef __bf16 __attribute__((ext_vector_type(8))) bf16x8v;
+typedef float __attribute__((ext_vector_type(4))) f32x4v;
+
+__device__ __forceinline__ f32x4v mfma16(const u32x4_t& a, const u32x4_t& b, const f32x4v& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, a), __builtin_bit_cast(bf16x8v, b), c,
+                                                 0, 0, 0);
+}
+
+// Two floats as a bf16 pair, rounded to nearest even.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  bf16x2_t r;
+  r[0] = (__bf16)a;
+  r[1] = (__bf16)b;
+  return __builtin_bit_cast(uint32_t, r);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+
+// Eight floats as N bf16 terms that add up to them (8 bits of each per term).
+template <int N> __device__ __forceinline__ void split_terms(const float (&x)[8], u32x4_t (&t)[N]) {
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      t[n][i] = pack_bf16(r[2 * i], r[2 * i + 1]);
+      if (n + 1 < N) {
+        r[2 * i] -= bf16_lo(t[n][i]);
+        r[2 * i + 1] -= bf16_hi(t[n][i]);
+      }
+    }
+}
+
+// Largest value and sum over the four lanes of a column (l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float column_max(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Weight of a partial sum of reference m under the joint reference M: 0 where no finite logit came in.
+__device__ __forceinline__ float part_weight(float m, float M) {
+  return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+}
+
+// A / S, 0 for a token that sees no row (a NaN stays one).
+template <int DT> __device__ __forceinline__ void store_out(void* out, int64_t at, float A, float S) {
+  const float o = S == 0.f ? 0.f : A / S;
+  if constexpr (DT == kDtBf16) static_cast<__bf16*>(out)[at] = (__bf16)o;
+  else static_cast<float*>(out)[at] = o;
+}
+
+// What a problem's call sees: its tokens, and the cache rows that the batch's table can reach.
+struct Span {
+  int tok0, n_tok, len, cap;
+  // rows visible to token j
+  __device__ __forceinline__ int visible(int j) const { return max(0, min(len - n_tok + j + 1, cap)); }
+};
+__device__ __forceinline__ Span span_of(const PagedAttnArgs& a, int p) {
+  Span s;
+  s.tok0 = a.tok_off ? a.tok_off[p] : p;
+  const int end = a.tok_off ? a.tok_off[p + 1] : p + 1;
+  s.n_tok = end - s.tok0;
+  if (s.tok0 < 0 || end > a.n_tok || s.n_tok > a.max_q) s.n_tok = 0;  // offsets outside the call's rows
+  s.len = a.pc.len[p];
+  s.cap = (int)min((int64_t)a.pc.table_stride << a.pc.shift, (int64_t)a.pc.max_len);
+  return s;
+}
+
+}  // namespace
+
+template <int DT, int QT, int D, int NT>
+__global__ __launch_bounds__(kThreads) void paged_attn_kernel(PagedAttnArgs a, int n_groups) {
+  constexpr int NS = D / 32;                       // matrix steps over the head dimension
+  constexpr int NI = D / 16;                       // 16-wide tiles of the output
+  constexpr int KH = D / 64;                       // 16-byte loads of a key
+  constexpr int VW = D / 64;                       // words of a value row that a lane loads
+  constexpr int QN = DT == kDtBf16 ? 1 : 3;        // bf16 terms of a query
+  constexpr int PN = DT == kDtBf16 ? 2 : 3;        // and of a weight
+  constexpr int COLS = 16 * NT;
+  __shared__ int32_t sh_block[kMaxSplitBlocks];
+  __shared__ float sh_ks[kMaxSplitBlocks], sh_vs[kMaxSplitBlocks];
+  __shared__ float sh_m[kWaves][16], sh_s[kWaves][16];
+  extern __shared__ __align__(16) float sh_acc[];  // [kWaves][up to 16 columns][D]
+
+  const int split = blockIdx.x, g = blockIdx.y / n_groups, cg = blockIdx.y % n_groups, p = blockIdx.z;
+  const int G = a.pc.h_q / a.pc.h_kv;
+  const Span sp = span_of(a, p);
+  const int col0 = cg * COLS;
+  const int n_cols = min(sp.n_tok * G - col0, COLS);
+  if (n_cols <= 0) return;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, kg = lane >> 4;
+  const int shift = a.pc.shift, R = 1 << shift;
+  const int r0 = split * a.split_rows;
+  const int vis_max = sp.visible((col0 + n_cols - 1) / G);
+  const int vis_min = sp.visible(col0 / G);
+  const int r1 = min(vis_max, r0 + a.split_rows);
+  if (r0 >= r1 && a.n_split > 1) return;  // the join reads the splits below a column's last row
+
+  // blocks and scales of the split's rows
+  for (int i = tid; i << shift < r1 - r0; i += kThreads) {
+    const int id = a.pc.table[(int64_t)p * a.pc.table_stride + (r0 >> shift) + i];
+    const bool ok = id >= 0 && id < a.pc.n_blocks;
+    sh_block[i] = ok ? id : -1;
+    const int64_t at = (int64_t)(ok ? id : 0) * a.pc.h_kv + g;
+    sh_ks[i] = ok ? a.pc.k_scale[at] * a.c : 0.f;
+    sh_vs[i] = ok ? a.pc.v_scale[at] : 0.f;
+  }
+
+  // the queries' operand: column n, elements 64 (s / 2) + 16 kg + 8 (s % 2) .. + 7 (D = 64: 16 kg + 8 s)
+  u32x4_t qf[NT][NS][QN];
+  int vis[NT];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    const int col = col0 + 16 * ct + n;
+    const bool live = 16 * ct + n < n_cols;
+    const int j = live ? col / G : 0, h = live ? col % G : 0;
+    vis[ct] = live ? sp.visible(j) : 0;
+    const int64_t at = (int64_t)(sp.tok0 + j) * a.q_stride + (int64_t)(g * G + h) * D;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int e = 64 * (s >> 1) + 16 * kg + 8 * (s & 1);
+      if constexpr (DT == kDtBf16) {
+        qf[ct][s][0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at + e);
+      } else {
+        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + e);
+        const float4 x = src[0], y = src[1];
+        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        split_terms<QN>(f, qf[ct][s]);
+      }
+    }
+  }
+  __syncthreads();
+
+  // the codes of 32 rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n
+  struct Rows {
+    u32x4_t k[2][KH];
+    uint32_t v[2][4][VW];
+  };
+  const int krow = 4 * (n & 3) + (n >> 2);
+  auto load = [&](Rows& x, int rb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = min(rb + 16 * t, (r1 - 1) & ~15) - r0;
+      const int64_t id = max(__builtin_amdgcn_readfirstlane(sh_block[r >> shift]), 0);
+      const int64_t at = ((id * a.pc.h_kv + g) << shift) * D + ((r & (R - 1)) * D);
+      const uint8_t* ks = a.pc.k + at + krow * D + 16 * kg;
+      const uint8_t* vs = a.pc.v + at + kg * D + n * (4 * VW);
+#pragma unroll
+      for (int i = 0; i < KH; ++i) x.k[t][i] = *reinterpret_cast<const u32x4_t*>(ks + 64 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (VW == 2) {
+          const u32x2_t u = *reinterpret_cast<const u32x2_t*>(vs + 4 * j * D);
+          x.v[t][j][0] = u[0];
+          x.v[t][j][1] = u[1];
+        } else {
+          x.v[t][j][0] = *reinterpret_cast<const uint32_t*>(vs + 4 * j * D);
+        }
+      }
+    }
+  };
+
+  float m[NT], mu[NT], sum[NT];  // mu: m, or 0 before the first finite logit
+  f32x4v acc[NT][NI];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    m[ct] = -INFINITY;
+    mu[ct] = 0.f;
+    sum[ct] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) acc[ct][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
+  }
+
+  auto step = [&](Rows& x, int rb) __attribute__((always_inline)) {
+    int blk[2];
+    float ksc[2], vsc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int i = (min(rb + 16 * t, (r1 - 1) & ~15) - r0) >> shift;
+      blk[t] = __builtin_amdgcn_readfirstlane(sh_block[i]);
+      ksc[t] = sh_ks[i];
+      vsc[t] = sh_vs[i];
+    }
+    // a step whose rows are not visible to every column, or whose blocks are missing
+    const bool masked = rb + kStep > vis_min || blk[0] < 0 || blk[1] < 0;
+    uint64_t nan_rows = 0;
+    if (masked) {
+      // a row without a column that sees it holds anything: zero its values, so that 0 times them is 0
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool in = blk[t] >= 0 && rb + 16 * t + 4 * j + kg < r1;
+#pragma unroll
+          for (int w = 0; w < VW; ++w) {
+            x.v[t][j][w] = in ? x.v[t][j][w] : 0u;
+            if constexpr (QT == kQtE4m3) {
+              const uint32_t u = (x.v[t][j][w] & 0x7F7F7F7Fu) + 0x01010101u;  // 0x80 in a byte of 0x7F
+              nan_rows |= __ballot((u & 0x80808080u) != 0);
+            }
+          }
+        }
+    }
+
+    u32x4_t kf[2][NS];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const u32x2_t lo = decode4_bf16<QT>(x.k[t][s >> 1][2 * (s & 1)]);
+        const u32x2_t hi = decode4_bf16<QT>(x.k[t][s >> 1][2 * (s & 1) + 1]);
+        kf[t][s] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+      }
+    u32x4_t pf[NT][PN];
+    bool over = false;
+    float lg[NT][8];
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) {
+      float tm = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x4v s4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = QN - 1; q >= 0; --q)
+#pragma unroll
+          for (int s = 0; s < NS; ++s) s4 = mfma16(kf[t][s], qf[ct][s][q], s4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float l = s4[j] * ksc[t];
+          if (masked && (blk[t] < 0 || rb + 16 * t + 4 * j + kg >= vis[ct])) l = -INFINITY;
+          lg[ct][4 * t + j] = l;
+          tm = fmaxf(tm, l);
+        }
+      }
+      over = over || tm > m[ct] + kSlack;
+    }
+    if (__ballot(over)) {
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        float tm = lg[ct][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) tm = fmaxf(tm, lg[ct][e]);
+        const float mn = fmaxf(m[ct], column_max(tm));
+        const float f = m[ct] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+        m[ct] = mn;
+        mu[ct] = mn == -INFINITY ? 0.f : mn;
+        sum[ct] *= f;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[ct][i][j] *= f;
+      }
+    }
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) {
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = __builtin_amdgcn_exp2f(lg[ct][e] - mu[ct]) * kSlackScale;
+        sum[ct] += w[e];
+        w[e] *= vsc[e >> 2];
+      }
+      split_terms<PN>(w, pf[ct]);
+    }
+
+    // V^T: eight rows' words of four elements, transposed to four elements' operands
+#pragma unroll
+    for (int w = 0; w < VW; ++w) {
+      u32x2_t b[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] = decode4_bf16<QT>(x.v[e >> 2][e & 3][w]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u32x4_t vf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          vf[e] = __builtin_amdgcn_perm(b[2 * e + 1][i >> 1], b[2 * e][i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
+        if (QT == kQtE4m3 && nan_rows) {
+          // a NaN counts for the columns that see its row alone: it leaves the products, and the columns
+          // that see one are marked by a product of indicators
+          u32x4_t nf;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            nf[e] = ((vf[e] & 0x7FFFu) > 0x7F80u ? 0x3F80u : 0u) | ((vf[e] & 0x7FFF0000u) > 0x7F800000u ? 0x3F800000u : 0u);
+            vf[e] &= ((nf[e] & 0xFFFFu) ? 0u : 0xFFFFu) | ((nf[e] >> 16) ? 0u : 0xFFFF0000u);
+          }
+#pragma unroll
+          for (int ct = 0; ct < NT; ++ct) {
+            float seen[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) seen[e] = rb + 16 * (e >> 2) + 4 * (e & 3) + kg < vis[ct] ? 1.f : 0.f;
+            u32x4_t one[1];
+            split_terms<1>(seen, one);
+            const f32x4v hit = mfma16(nf, one[0], f32x4v{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (hit[j] > 0.f) acc[ct][4 * w + i][j] = NAN;
+          }
+        }
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+          for (int q = PN - 1; q >= 0; --q) acc[ct][4 * w + i] = mfma16(vf, pf[ct][q], acc[ct][4 * w + i]);
+      }
+    }
+  };
+
+  // the waves' steps in turn, the next one's codes in flight
+  {
+    constexpr int kRound = kWaves * kStep;
+    Rows xa, xb;
+    int rb = r0 + wave * kStep;
+    if (rb < r1) load(xa, rb);
+    for (; rb < r1; rb += 2 * kRound) {
+      if (rb + kRound < r1) load(xb, rb + kRound);
+      step(xa, rb);
+      if (rb + kRound < r1) {
+        if (rb + 2 * kRound < r1) load(xa, rb + 2 * kRound);
+        step(xb, rb + kRound);
+      }
+    }
+  }
+
+  // merge of the waves, 16 columns at a time: element 4 VW (4 kg + j) + 4 w + i of column n
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    const int cols = min(n_cols - 16 * ct, 16);
+    if (cols <= 0) break;
+    const float s = column_sum(sum[ct]);
+    if (kg == 0) {
+      sh_m[wave][n] = m[ct];
+      sh_s[wave][n] = s;
+    }
+    if (n < cols) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int w = 0; w < VW; ++w)
+          *reinterpret_cast<float4*>(&sh_acc[(wave * cols + n) * D + (4 * kg + j) * 4 * VW + 4 * w]) =
+              make_float4(acc[ct][4 * w][j], acc[ct][4 * w + 1][j], acc[ct][4 * w + 2][j], acc[ct][4 * w + 3][j]);
+    }
+    __syncthreads();
+    for (int idx = tid; idx < cols * D; idx += kThreads) {
+      const int cc = idx / D, e = idx % D;
+      float M = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) M = fmaxf(M, sh_m[i][cc]);
+      float S = 0.f, A = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const float f = part_weight(sh_m[i][cc], M);
+        S = fmaf(sh_s[i][cc], f, S);
+        A = fmaf(sh_acc[(i * cols + cc) * D + e], f, A);
+      }
+      const int col = col0 + 16 * ct + cc;
+      const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
+      if (a.n_split == 1) {
+        store_out<DT>(a.out, row * D + e, A, S);
+      } else {
+        float* pt = a.part + (row * a.n_split + split) * (D + 2);
+        if (e == 0) {
+          pt[0] = M;
+          pt[1] = S;
+        }
+        pt[2 + e] = A;
+      }
+    }
+    if (ct + 1 < NT) __syncthreads();
+  }
+}
+
+// One workgroup per (column, kv head, problem): the splits below the column's last visible row.
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void paged_combine_kernel(PagedAttnArgs a) {
+  constexpr int PARTS = kThreads / D;
+  __shared__ float sh_a[PARTS][D], sh_m[PARTS], sh_s[PARTS];
+  const int col = blockIdx.x, g = blockIdx.y, p = blockIdx.z, G = a.pc.h_q / a.pc.h_kv;
+  const Span sp = span_of(a, p);
+  if (col >= sp.n_tok * G) return;
+  const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
+  const int n_split = (sp.visible(col / G) + a.split_rows - 1) / a.split_rows;
+  const int e = threadIdx.x % D, pt = threadIdx.x / D;
+  const float* part = a.part + row * a.n_split * (D + 2);
+  float m = -INFINITY, S = 0.f, A = 0.f;
+  for (int i = pt; i < n_split; i += PARTS) {
+    const float* x = part + (int64_t)i * (D + 2);
+    const float mn = fmaxf(m, x[0]), f = part_weight(m, mn), w = part_weight(x[0], mn);
+    S = fmaf(x[1], w, S * f);
+    A = fmaf(x[2 + e], w, A * f);
+    m = mn;
+  }
+  sh_a[pt][e] = A;
+  if (e == 0) {
+    sh_m[pt] = m;
+    sh_s[pt] = S;
+  }
+  __syncthreads();
+  if (pt != 0) return;
+  float M = -INFINITY;
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q) M = fmaxf(M, sh_m[q]);
+  S = 0.f;
+  A = 0.f;
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q) {
+    const float f = part_weight(sh_m[q], M);
+    S = fmaf(sh_s[q], f, S);
+    A = fmaf(sh_a[q][e], f, A);
+  }
+  store_out<DT>(a.out, row * D + e, A, S);
+}
+
+namespace {
+
+// 16-wide column tiles of a wave: one for up to 16 columns, else two.
+int column_tiles(int max_q, int group) { return max_q * group <= 16 ? 1 : 2; }
+int column_groups(int max_q, int group) {
+  const int w = 16 * column_tiles(max_q, group);
+  return (max_q * group + w - 1) / w;
+}
+
+}  // namespace
+
+PagedPlan paged_plan(const Paged& pc, int max_q) {
+  constexpr int64_t kRound = 768, kMinSplit = 256;
+  const int64_t units = (int64_t)pc.n_prob * pc.h_kv * column_groups(max_q, pc.group());
+  const int64_t rows = std::max<int64_t>(1, std::min<int64_t>(pc.max_len, (int64_t)pc.table_stride << pc.shift));
+  int64_t n = 1;
+  if (rows > 512) n = std::max<int64_t>(1, std::min(3 * kRound / units, (rows + kMinSplit - 1) / kMinSplit));
+  int64_t split = ((rows + n - 1) / n + 127) / 128 * 128;
+  split = std::min<int64_t>(split, kMaxSplitRows);
+  PagedPlan plan;
+  plan.split_rows = (int)split;
+  plan.n_split = (int)((rows + split - 1) / split);
+  return plan;
+}
+
+size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan) {
+  if (plan.n_split == 1) return 0;
+  return (size_t)n_tok * pc.h_q * plan.n_split * (pc.d + 2) * sizeof(float);
+}
+
+namespace {
+
+template <int DT, int QT, int D> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
+  const int G = a.pc.group(), nt = column_tiles(a.max_q, G), groups = column_groups(a.max_q, G);
+  const dim3 grid((unsigned)a.n_split, (unsigned)(a.pc.h_kv * groups), (unsigned)a.pc.n_prob);
+  const size_t lds = (size_t)kWaves * std::min(a.max_q * G, 16) * D * sizeof(float);
+  if (nt == 1) paged_attn_kernel<DT, QT, D, 1><<<grid, kThreads, lds, stream>>>(a, groups);
+  else paged_attn_kernel<DT, QT, D, 2><<<grid, kThreads, lds, stream>>>(a, groups);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.n_split == 1) return e;
+  const dim3 cols((unsigned)(a.max_q * G), (unsigned)a.pc.h_kv, (unsigned)a.pc.n_prob);
+  paged_combine_kernel<DT, D><<<cols, kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
+  auto d = [&](auto dt, auto qt) {
+    return a.pc.d == 64 ? attend<dt.value, qt.value, 64>(a, stream) : attend<dt.value, qt.value, 128>(a, stream);
+  };
+  auto q = [&](auto dt) {
+    return a.pc.qtype == kQtE4m3 ? d(dt, std::integral_constant<int, kQtE4m3>{})
+                                 : d(dt, std::integral_constant<int, kQtInt8>{});
+  };
+  return a.pc.dtype == kDtBf16 ? q(std::integral_constant<int, kDtBf16>{}) : q(std::integral_constant<int, kDtF32>{});
+}
+
+}  // namespace kv

@@ -1,0 +1,89 @@
+// Device side of the 8-bit paged cache: codes and scales.
+//
+// A scale is a power of two (or 0: a block of zeros), the least one with max|x| <= 448 s for e4m3
+// and 127 s for int8 over the block's finite values.  A value is code * s: exact in bf16, whatever the
+// code.  A power of two costs e4m3 nothing (its precision does not depend on the scale) and
+// int8 up to one bit of its range; in return a block whose scale grows with a later row moves its codes
+// by whole binades, so that e4m3's normal numbers stay as they were, and the codes of given rows are the
+// same on every path.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.h"
+#include "paged.h"
+
+namespace kv {
+
+typedef __bf16 __attribute__((ext_vector_type(2))) bf16x2_t;
+typedef uint32_t __attribute__((ext_vector_type(2))) u32x2_t;
+typedef uint32_t __attribute__((ext_vector_type(4))) u32x4_t;
+
+// The scale of a block whose largest finite |x| has these bits.
+template <int QT> __device__ __forceinline__ float block_scale(uint32_t amax_bits) {
+  // amax = (1 + f) 2^(x - 127): 448 = 1.75 2^8, 127 = 1.984375 2^6
+  constexpr int kTop = QT == kQtE4m3 ? 8 : 6;
+  constexpr uint32_t kFrac = QT == kQtE4m3 ? 0x600000u : 0x7E0000u;
+  if (amax_bits == 0) return 0.f;
+  const int e = (int)(amax_bits >> 23) - kTop + ((amax_bits & 0x7FFFFFu) > kFrac ? 1 : 0);
+  return __uint_as_float((uint32_t)max(e, 1) << 23);
+}
+
+// 1 / s (exact for a scale as block_scale gives it); 1 for 0, whose block has no finite value but 0.
+__device__ __forceinline__ float inv_scale(float s) { return s > 0.f ? 1.f / s : 1.f; }
+
+// Four values in units of the scale as codes, rounded to nearest even; infinities saturate, and a NaN
+// stays one in e4m3 and becomes 0 in int8.
+template <int QT> __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  const float x[4] = {a, b, c, d};
+  if constexpr (QT == kQtE4m3) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i], -448.f, 448.f);
+    uint32_t u = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    u = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], (int)u, true);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (x[i] != x[i]) u = (u & ~(0xFFu << (8 * i))) | (0x7Fu << (8 * i));
+    return u;
+  } else {
+    uint32_t u = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float y = x[i] == x[i] ? __builtin_amdgcn_fmed3f(__builtin_rintf(x[i]), -127.f, 127.f) : 0.f;
+      u |= ((uint32_t)(int)y & 0xFFu) << (8 * i);
+    }
+    return u;
+  }
+}
+
+// Four codes as fp32.
+template <int QT> __device__ __forceinline__ void decode4(uint32_t u, float (&f)[4]) {
+  if constexpr (QT == kQtE4m3) {
+    f[0] = __builtin_amdgcn_cvt_f32_fp8((int)u, 0);
+    f[1] = __builtin_amdgcn_cvt_f32_fp8((int)u, 1);
+    f[2] = __builtin_amdgcn_cvt_f32_fp8((int)u, 2);
+    f[3] = __builtin_amdgcn_cvt_f32_fp8((int)u, 3);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = (float)(int8_t)(u >> (8 * i));
+  }
+}
+
+// Four codes as bf16 pairs (0, 1) and (2, 3): exact, every code has at most 8 significant bits.
+template <int QT> __device__ __forceinline__ u32x2_t decode4_bf16(uint32_t u) {
+  u32x2_t r;
+  if constexpr (QT == kQtE4m3) {
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.f, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.f, true));
+  } else {
+    float f[4];
+    decode4<QT>(u, f);
+    r[0] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
+    r[1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+  }
+  return r;
+}
+
+}  // namespace kv
