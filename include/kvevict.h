@@ -404,6 +404,7 @@ int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, 
  *     127 s (KV_INT8) over the block's finite elements (at least 2^-126), 0 for zeros; a code is x / s
  *     rounded to nearest even.  An infinity takes the largest code of its sign; a NaN stays one
  *     in KV_E4M3 and becomes 0 in KV_INT8.
+ *     Attention and appending take scales of 0 and powers of two from 2^-126 on; others are undefined.
  *   - A table entry outside [0, n_blocks) is a missing block: its rows are not written, and not seen.
  *   - Rows of a block that no problem has written may hold anything.
  * dtype: of queries, new rows and outputs.  n_blocks * block_rows and table_stride * block_rows below
@@ -479,7 +480,8 @@ size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_to
  *   out[t,h,:] = sum_r softmax_r(scale <q[t,h], k[r]>) v[r],  kv head h / (h_q / h_kv);
  * 0 where it sees none.  q: token t at t * q_stride elements (0: h_q * d; at least that, whole 16-byte
  * chunks), [h_q][d]; out [n_tok][h_q][d] of the queries' type.  Logits, softmax and sums in fp32; the weights enter
- * the product with V with at least 16 significant bits (bf16 queries; 24 for fp32).  The outputs of
+ * the product with V with 24 significant bits (fp32 queries), 16 (bf16 and max_q h_q / h_kv <= 32) or as
+ * bf16 (more).  The outputs of
  * tokens outside every problem (a padded batch) stay as they were, and so do a problem's whose tok_off reaches outside
  * [0, n_tok] or spans more than max_q.  Calls that overlap on one workspace race. */
 int kv_paged_attention(const kv_paged_cache* pc, const void* q, int64_t q_stride, const int32_t* tok_off,

@@ -836,12 +836,12 @@ int check_stride(const kv::Paged& pc, int heads, int64_t* stride) {
   return KV_OK;
 }
 
-// Grid limits of an attention call: columns of a problem, and of the grid's axes.
-int check_tokens(const kv::Paged& pc, int32_t n_tok, int32_t max_q) {
+// Tokens of an attention call, and the launch they take.
+int check_tokens(const kv::Paged& pc, int32_t n_tok, int32_t max_q, kv::PagedPlan* plan) {
   if (n_tok < 1 || max_q < 1 || max_q > n_tok) return KV_ERR_ARG;
-  const int64_t groups = ((int64_t)max_q * pc.group() + 15) / 16;
-  if (max_q > kMaxLen || groups * pc.h_kv > kMaxGrid) return KV_ERR_SHAPE;
-  return KV_OK;
+  if (max_q > kMaxLen) return KV_ERR_SHAPE;
+  *plan = kv::paged_plan(pc, max_q);
+  return kv::paged_grid_y(pc, max_q, *plan) > kMaxGrid ? KV_ERR_SHAPE : KV_OK;
 }
 
 }  // namespace
@@ -901,8 +901,9 @@ int kv_paged_compact(const kv_problem* pr, const void* k, const void* v, const i
 
 size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* c, int32_t n_tok, int32_t max_q) {
   kv::Paged pc{};
-  if (check_paged(c, &pc) != KV_OK || check_tokens(pc, n_tok, max_q) != KV_OK) return 0;
-  return align_up(kv::paged_ws_bytes(pc, n_tok, kv::paged_plan(pc, max_q)));
+  kv::PagedPlan plan;
+  if (check_paged(c, &pc) != KV_OK || check_tokens(pc, n_tok, max_q, &plan) != KV_OK) return 0;
+  return align_up(kv::paged_ws_bytes(pc, n_tok, plan));
 }
 
 int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride, const int32_t* tok_off,
@@ -913,12 +914,12 @@ int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride,
   if (st != KV_OK) return st;
   if (!q || !out) return KV_ERR_NULL;
   if (!aligned16(q) || !aligned16(out) || !std::isfinite(scale)) return KV_ERR_ARG;
-  st = check_tokens(a.pc, n_tok, max_q);
+  kv::PagedPlan plan;
+  st = check_tokens(a.pc, n_tok, max_q, &plan);
   if (st != KV_OK) return st;
   if (!tok_off && (n_tok != a.pc.n_prob || max_q != 1)) return KV_ERR_ARG;
   st = check_stride(a.pc, a.pc.h_q, &q_stride);
   if (st != KV_OK) return st;
-  const kv::PagedPlan plan = kv::paged_plan(a.pc, max_q);
   const size_t need = align_up(kv::paged_ws_bytes(a.pc, n_tok, plan));
   if (need > 0 && (ws_bytes < need || !ws || (reinterpret_cast<uintptr_t>(ws) & (kWsAlign - 1))))
     return KV_ERR_WORKSPACE;
@@ -932,7 +933,7 @@ int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride,
   a.split_rows = plan.split_rows;
   a.n_split = plan.n_split;
   a.part = static_cast<float*>(ws);
-  return launch_status(kv::launch_paged_attention(a, static_cast<hipStream_t>(stream)));
+  return launch_status(kv::launch_paged_attention(a, plan, static_cast<hipStream_t>(stream)));
 }
 
 int kv_pyramid_budgets(int32_t budget, int32_t n_layers, double beta, int32_t* budgets_host) {

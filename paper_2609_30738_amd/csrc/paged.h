@@ -61,11 +61,15 @@ struct PagedAttnArgs {
   int split_rows, n_split;
   float* part;  // [n_tok][h_q][n_split][d + 2] when n_split > 1
 };
+// prompt_waves: 0 for paged_attention.hip's kernel, else the waves of paged_prompt.hip's (32 columns each).
 struct PagedPlan {
-  int split_rows, n_split;
+  int split_rows, n_split, prompt_waves;
 };
 PagedPlan paged_plan(const Paged& pc, int max_q);
+// Workgroups along the grid's second axis (at most 65535).
+int64_t paged_grid_y(const Paged& pc, int max_q, const PagedPlan& plan);
 size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan);
-hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t stream);
+hipError_t launch_paged_prompt(const PagedAttnArgs& a, int waves, hipStream_t stream);
 
 }  // namespace kv

@@ -24,6 +24,7 @@
 #include "common.h"
 #include "paged.h"
 #include "paged_codes.h"
+#include "paged_span.h"
 
 namespace kv {
 
@@ -34,10 +35,7 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kStep = 32;               // rows of a wave's step
 constexpr int kMaxSplitRows = 2048;     // the blocks and scales of a split are held in LDS
 constexpr int kMaxSplitBlocks = kMaxSplitRows / 16;
-constexpr float kSlack = 8.f;           // octaves a logit may exceed its reference
-constexpr float kSlackScale = 0x1p-8f;  // of the weights
 
-typedef __bf16 __attribute__((ext_vector_type(8))) bf16x8v;
 typedef float __attribute__((ext_vector_type(4))) f32x4v;
 
 __device__ __forceinline__ f32x4v mfma16(const u32x4_t& a, const u32x4_t& b, const f32x4v& c) {
@@ -45,13 +43,6 @@ __device__ __forceinline__ f32x4v mfma16(const u32x4_t& a, const u32x4_t& b, con
                                                  0, 0, 0);
 }
 
-// Two floats as a bf16 pair, rounded to nearest even.
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  bf16x2_t r;
-  r[0] = (__bf16)a;
-  r[1] = (__bf16)b;
-  return __builtin_bit_cast(uint32_t, r);
-}
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
 
@@ -84,35 +75,6 @@ __device__ __forceinline__ float column_sum(float v) {
   v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// Weight of a partial sum of reference m under the joint reference M: 0 where no finite logit came in.
-__device__ __forceinline__ float part_weight(float m, float M) {
-  return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-}
-
-// A / S, 0 for a token that sees no row (a NaN stays one).
-template <int DT> __device__ __forceinline__ void store_out(void* out, int64_t at, float A, float S) {
-  const float o = S == 0.f ? 0.f : A / S;
-  if constexpr (DT == kDtBf16) static_cast<__bf16*>(out)[at] = (__bf16)o;
-  else static_cast<float*>(out)[at] = o;
-}
-
-// What a problem's call sees: its tokens, and the cache rows that the batch's table can reach.
-struct Span {
-  int tok0, n_tok, len, cap;
-  // rows visible to token j
-  __device__ __forceinline__ int visible(int j) const { return max(0, min(len - n_tok + j + 1, cap)); }
-};
-__device__ __forceinline__ Span span_of(const PagedAttnArgs& a, int p) {
-  Span s;
-  s.tok0 = a.tok_off ? a.tok_off[p] : p;
-  const int end = a.tok_off ? a.tok_off[p + 1] : p + 1;
-  s.n_tok = end - s.tok0;
-  if (s.tok0 < 0 || end > a.n_tok || s.n_tok > a.max_q) s.n_tok = 0;  // offsets outside the call's rows
-  s.len = a.pc.len[p];
-  s.cap = (int)min((int64_t)a.pc.table_stride << a.pc.shift, (int64_t)a.pc.max_len);
-  return s;
 }
 
 }  // namespace
@@ -465,23 +427,38 @@ namespace {
 int column_tiles(int max_q, int group) { return max_q * group <= 16 ? 1 : 2; }
 int column_groups(int max_q, int group) {
   const int w = 16 * column_tiles(max_q, group);
-  return (max_q * group + w - 1) / w;
+  return (int)(((int64_t)max_q * group + w - 1) / w);
 }
 
 }  // namespace
 
 PagedPlan paged_plan(const Paged& pc, int max_q) {
-  constexpr int64_t kRound = 768, kMinSplit = 256;
-  const int64_t units = (int64_t)pc.n_prob * pc.h_kv * column_groups(max_q, pc.group());
   const int64_t rows = std::max<int64_t>(1, std::min<int64_t>(pc.max_len, (int64_t)pc.table_stride << pc.shift));
-  int64_t n = 1;
-  if (rows > 512) n = std::max<int64_t>(1, std::min(3 * kRound / units, (rows + kMinSplit - 1) / kMinSplit));
-  int64_t split = ((rows + n - 1) / n + 127) / 128 * 128;
-  split = std::min<int64_t>(split, kMaxSplitRows);
+  const int64_t cols = (int64_t)max_q * pc.group();
   PagedPlan plan;
+  plan.prompt_waves = 0;
+  int64_t n = 1, units;
+  if (pc.dtype == kDtBf16 && cols > 32) {
+    plan.prompt_waves = cols <= 128 ? 4 : 8;
+    units = (int64_t)pc.n_prob * pc.h_kv * ((cols + 32 * plan.prompt_waves - 1) / (32 * plan.prompt_waves));
+    constexpr int64_t kFill = 512, kMinSplit = 512;
+    if (units < kFill) n = std::max<int64_t>(1, std::min(kFill / units, (rows + kMinSplit - 1) / kMinSplit));
+  } else {
+    constexpr int64_t kRound = 768, kMinSplit = 256;
+    units = (int64_t)pc.n_prob * pc.h_kv * column_groups(max_q, pc.group());
+    if (rows > 512) n = std::max<int64_t>(1, std::min(3 * kRound / units, (rows + kMinSplit - 1) / kMinSplit));
+  }
+  int64_t split = ((rows + n - 1) / n + 127) / 128 * 128;
+  if (!plan.prompt_waves) split = std::min<int64_t>(split, kMaxSplitRows);
   plan.split_rows = (int)split;
   plan.n_split = (int)((rows + split - 1) / split);
   return plan;
+}
+
+int64_t paged_grid_y(const Paged& pc, int max_q, const PagedPlan& plan) {
+  const int64_t cols = (int64_t)max_q * pc.group();
+  if (plan.prompt_waves) return (cols + 32 * plan.prompt_waves - 1) / (32 * plan.prompt_waves) * plan.n_split;
+  return (int64_t)pc.h_kv * column_groups(max_q, pc.group());
 }
 
 size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan) {
@@ -497,16 +474,19 @@ template <int DT, int QT, int D> hipError_t attend(const PagedAttnArgs& a, hipSt
   const size_t lds = (size_t)kWaves * std::min(a.max_q * G, 16) * D * sizeof(float);
   if (nt == 1) paged_attn_kernel<DT, QT, D, 1><<<grid, kThreads, lds, stream>>>(a, groups);
   else paged_attn_kernel<DT, QT, D, 2><<<grid, kThreads, lds, stream>>>(a, groups);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.n_split == 1) return e;
-  const dim3 cols((unsigned)(a.max_q * G), (unsigned)a.pc.h_kv, (unsigned)a.pc.n_prob);
+  return hipGetLastError();
+}
+
+template <int DT, int D> hipError_t combine(const PagedAttnArgs& a, hipStream_t stream) {
+  const dim3 cols((unsigned)(a.max_q * a.pc.group()), (unsigned)a.pc.h_kv, (unsigned)a.pc.n_prob);
   paged_combine_kernel<DT, D><<<cols, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t stream) {
+  const bool bf16 = a.pc.dtype == kDtBf16;
   auto d = [&](auto dt, auto qt) {
     return a.pc.d == 64 ? attend<dt.value, qt.value, 64>(a, stream) : attend<dt.value, qt.value, 128>(a, stream);
   };
@@ -514,7 +494,12 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, hipStream_t stream) {
     return a.pc.qtype == kQtE4m3 ? d(dt, std::integral_constant<int, kQtE4m3>{})
                                  : d(dt, std::integral_constant<int, kQtInt8>{});
   };
-  return a.pc.dtype == kDtBf16 ? q(std::integral_constant<int, kDtBf16>{}) : q(std::integral_constant<int, kDtF32>{});
+  const hipError_t e = plan.prompt_waves ? launch_paged_prompt(a, plan.prompt_waves, stream)
+                       : bf16            ? q(std::integral_constant<int, kDtBf16>{})
+                                         : q(std::integral_constant<int, kDtF32>{});
+  if (e != hipSuccess || a.n_split == 1) return e;
+  if (bf16) return a.pc.d == 64 ? combine<kDtBf16, 64>(a, stream) : combine<kDtBf16, 128>(a, stream);
+  return a.pc.d == 64 ? combine<kDtF32, 64>(a, stream) : combine<kDtF32, 128>(a, stream);
 }
 
 }  // namespace kv

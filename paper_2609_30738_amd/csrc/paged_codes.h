@@ -71,17 +71,18 @@ template <int QT> __device__ __forceinline__ void decode4(uint32_t u, float (&f)
   }
 }
 
-// Four codes as bf16 pairs (0, 1) and (2, 3): exact, every code has at most 8 significant bits.
-template <int QT> __device__ __forceinline__ u32x2_t decode4_bf16(uint32_t u) {
+// Four codes times a power of two as bf16 pairs (0, 1) and (2, 3): exact, every code has at most 8
+// significant bits.
+template <int QT> __device__ __forceinline__ u32x2_t decode4_bf16(uint32_t u, float scale = 1.f) {
   u32x2_t r;
   if constexpr (QT == kQtE4m3) {
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.f, false));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.f, true));
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, scale, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, scale, true));
   } else {
     float f[4];
     decode4<QT>(u, f);
-    r[0] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
-    r[1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+    r[0] = __builtin_amdgcn_perm(__float_as_uint(f[1] * scale), __float_as_uint(f[0] * scale), 0x07060302u);
+    r[1] = __builtin_amdgcn_perm(__float_as_uint(f[3] * scale), __float_as_uint(f[2] * scale), 0x07060302u);
   }
   return r;
 }

@@ -1,0 +1,369 @@
+// Attention of many tokens of a problem over its 8-bit paged cache (kv_paged_attention with bf16 queries and
+// more columns, (token, query head) pairs of a kv head, than paged_attention.hip's kernel takes at once).
+//
+// paged_prompt_kernel: one workgroup of W waves per (32 W columns, split of the rows, kv head, problem), each
+//   wave 32 columns.  Tiles of 64 rows go through LDS in bf16, which holds code * scale exactly (a scale is a
+//   power of two), K as it lies and V transposed; the next tile's codes are in flight meanwhile, and the one
+//   after's table entries.  With v_mfma_f32_32x32x16_bf16,
+//     S^T = K Q^T,  O^T = V^T P^T:
+//   a lane of the accumulator holds one column and 16 of a tile's 32 rows, so the running maximum and sum
+//   stay in the lane, and its weights are, eight at a time, its own operand of the second product;
+//   V^T lies in LDS in the order of that operand's rows.
+//   Weights are rounded to bf16 for that product (2^-9 of each, the step of the bf16 output); their sum
+//   is taken of the unrounded ones.
+//   The grid's fastest axis is the kv head: workgroups go to the 8 XCDs in turn, so that with 8 heads one L2
+//   holds one head's rows.  The last columns, which see the most rows, come first.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "paged.h"
+#include "paged_codes.h"
+#include "paged_span.h"
+
+namespace kv {
+
+namespace {
+
+constexpr int kTile = 64;  // rows of a tile
+
+typedef float __attribute__((ext_vector_type(16))) f32x16v;
+
+__device__ __forceinline__ f32x16v mfma32(const u32x4_t& a, const u32x4_t& b, const f32x16v& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8v, a), __builtin_bit_cast(bf16x8v, b), c,
+                                                 0, 0, 0);
+}
+
+__device__ __forceinline__ float half_max(float v) {  // over the lanes l and l ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A tile in LDS: K rows of D + 8 elements (so that eight rows' 16-byte reads fall on all banks), V^T rows of
+// 64 + 8.  The 16 bytes (u, h) of V^T's row hold rows 16 u + 4 h + {0..3, 8..11} of the tile, and lie at place
+// (2 u + h) ^ (element / 16 % 8): the transposing writes of eight times four elements then share no bank.
+template <int D> struct Tile {
+  static constexpr int KS = D + 8, VS = kTile + 8;
+  uint16_t k[kTile * KS];
+  uint16_t v[D * VS];
+  int32_t has[kTile / 16];  // whether the 16 rows have a block
+  int32_t nan[8];           // whether a wave found a NaN in V
+};
+
+}  // namespace
+
+template <int QT, int D, int W>
+__global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a, int n_groups) {
+  constexpr int NS = D / 16;  // matrix steps over the head dimension
+  constexpr int ND = D / 32;  // 32-wide tiles of the output
+  constexpr int NTHREADS = 64 * W;
+  constexpr int KTASKS = kTile * (D / 16), VTASKS = (kTile / 4) * (D / 4);
+  constexpr int KT = (KTASKS + NTHREADS - 1) / NTHREADS, VT = (VTASKS + NTHREADS - 1) / NTHREADS;
+  using T = Tile<D>;
+  extern __shared__ __align__(16) char lds[];
+  T* const tiles = reinterpret_cast<T*>(lds);
+
+  const int g = blockIdx.x, split = blockIdx.y % a.n_split, cg = n_groups - 1 - blockIdx.y / a.n_split;
+  const int p = blockIdx.z, G = a.pc.h_q / a.pc.h_kv;
+  const Span sp = span_of(a, p);
+  const int col0 = cg * 32 * W;
+  const int n_cols = min(sp.n_tok * G - col0, 32 * W);
+  if (n_cols <= 0) return;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, h = lane >> 5;
+  const int shift = a.pc.shift, R = 1 << shift;
+  const int r0 = split * a.split_rows;
+  const int vis_max = sp.visible((col0 + n_cols - 1) / G);
+  const int r1 = min(vis_max, r0 + a.split_rows);
+  if (r0 >= r1 && a.n_split > 1) return;
+  const int n_tiles = r1 > r0 ? (r1 - r0 + kTile - 1) / kTile : 0;
+
+  // this lane's column, and its wave's
+  const int wcol = col0 + 32 * wave;
+  const int wcols = min(n_cols - 32 * wave, 32);  // may be 0 or less
+  const bool live = n < wcols;
+  const int col = live ? wcol + n : col0;
+  const int vis = live ? sp.visible(col / G) : 0;
+  const int wvis_max = wcols > 0 ? sp.visible((wcol + wcols - 1) / G) : 0;
+  const int wvis_min = wcols > 0 ? sp.visible(wcol / G) : 0;
+  const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
+  // a negative scale turns the queries' signs; a scale of 0 gives equal weights, as the least number does
+  const float c = fmaxf(fabsf(a.c), 0x1p-126f);
+  u32x4_t qf[NS];
+  {
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)(sp.tok0 + col / G) * a.q_stride +
+                        (int64_t)(g * G + col % G) * D;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      qf[s] = *reinterpret_cast<const u32x4_t*>(q + 16 * s + 8 * h);
+      if (a.c < 0.f) qf[s] ^= 0x80008000u;
+    }
+  }
+
+  // staging: K in 16-byte pieces of a row, V in four rows by four elements
+  int32_t kid[KT], vid[VT];
+  u32x4_t kc[KT];
+  uint32_t vc[VT][4];
+  float ksc[KT], vsc[VT];
+  bool khas[KT];  // of kc (kid is a tile ahead of it by then)
+  const int32_t* table = a.pc.table + (int64_t)p * a.pc.table_stride;
+  auto k_row = [&](int i) { return (tid + i * NTHREADS) / (D / 16); };
+  auto v_row = [&](int i) { return (tid + i * NTHREADS) / (D / 4) * 4; };
+  auto ids = [&](int t) __attribute__((always_inline)) {
+    const int rb = r0 + t * kTile;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const int r = rb + k_row(i);
+      kid[i] = r < r1 ? table[r >> shift] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < VT; ++i) {
+      const int r = rb + v_row(i);
+      vid[i] = r < r1 ? table[r >> shift] : -1;
+    }
+  };
+  auto codes = [&](int t) __attribute__((always_inline)) {
+    const int rb = r0 + t * kTile;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      if (KTASKS % NTHREADS != 0 && tid + i * NTHREADS >= KTASKS) break;
+      khas[i] = (uint32_t)kid[i] < (uint32_t)a.pc.n_blocks;
+      const int64_t unit = (int64_t)(khas[i] ? kid[i] : 0) * a.pc.h_kv + g;
+      const int r = (rb + k_row(i)) & (R - 1);
+      kc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.k + ((unit << shift) + r) * D + (tid + i * NTHREADS) % (D / 16) * 16);
+      ksc[i] = a.pc.k_scale[unit];
+      if (!khas[i]) {
+        kc[i] = u32x4_t{0u, 0u, 0u, 0u};
+        ksc[i] = 1.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VT; ++i) {
+      if (VTASKS % NTHREADS != 0 && tid + i * NTHREADS >= VTASKS) break;
+      const bool has = (uint32_t)vid[i] < (uint32_t)a.pc.n_blocks;
+      const int64_t unit = (int64_t)(has ? vid[i] : 0) * a.pc.h_kv + g;
+      const int r = (rb + v_row(i)) & (R - 1);
+      const uint8_t* src = a.pc.v + ((unit << shift) + r) * D + (tid + i * NTHREADS) % (D / 4) * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vc[i][j] = *reinterpret_cast<const uint32_t*>(src + j * D);
+      vsc[i] = a.pc.v_scale[unit];
+      if (!has) vsc[i] = 1.f;
+      // a row that no column sees holds anything: zero its values, so that 0 times them is 0
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (!has || rb + v_row(i) + j >= r1) vc[i][j] = 0u;
+    }
+  };
+  auto stage = [&](int t) __attribute__((always_inline)) {
+    T& x = tiles[t & 1];
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const int task = tid + i * NTHREADS;
+      if (KTASKS % NTHREADS != 0 && task >= KTASKS) break;
+      const int r = task / (D / 16), e = task % (D / 16) * 16;
+      u32x4_t lo, hi;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const u32x2_t y = decode4_bf16<QT>(kc[i][w], ksc[i]), z = decode4_bf16<QT>(kc[i][2 + w], ksc[i]);
+        lo[2 * w] = y[0];
+        lo[2 * w + 1] = y[1];
+        hi[2 * w] = z[0];
+        hi[2 * w + 1] = z[1];
+      }
+      *reinterpret_cast<u32x4_t*>(&x.k[r * T::KS + e]) = lo;
+      *reinterpret_cast<u32x4_t*>(&x.k[r * T::KS + e + 8]) = hi;
+      if (e == 0 && r % 16 == 0) x.has[r / 16] = khas[i];
+    }
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < VT; ++i) {
+      const int task = tid + i * NTHREADS;
+      if (VTASKS % NTHREADS != 0 && task >= VTASKS) break;
+      const int quad = task / (D / 4), e = task % (D / 4) * 4;
+      const int place = ((2 * (quad >> 2) + (quad & 1)) ^ ((e >> 4) & 7)) * 8 + ((quad >> 1) & 1) * 4;
+      u32x2_t b[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (QT == kQtE4m3) nan = nan || (((vc[i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+        b[j] = decode4_bf16<QT>(vc[i][j], vsc[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+        u32x2_t y;
+        y[0] = __builtin_amdgcn_perm(b[1][j >> 1], b[0][j >> 1], sel);
+        y[1] = __builtin_amdgcn_perm(b[3][j >> 1], b[2][j >> 1], sel);
+        *reinterpret_cast<u32x2_t*>(&x.v[(e + j) * T::VS + place]) = y;
+      }
+    }
+    if (QT == kQtE4m3) {
+      const uint64_t any = __ballot(nan);
+      if (lane == 0) x.nan[wave] = any != 0;
+    }
+  };
+
+  float m = -INFINITY, mu = kSlack, sum = 0.f;  // mu: m (0 before the first finite logit) + kSlack
+  f32x16v acc[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) acc[i] = 0.f;
+
+  auto compute = [&](int t) __attribute__((always_inline)) {
+    const T& x = tiles[t & 1];
+    const int rb = r0 + t * kTile;
+    f32x16v s[2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      s[kt] = 0.f;
+#pragma unroll
+      for (int d = 0; d < NS; ++d) {
+        const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(&x.k[(32 * kt + n) * T::KS + 16 * d + 8 * h]);
+        s[kt] = mfma32(kf, qf[d], s[kt]);
+      }
+    }
+    bool nan_rows = false;
+    const int has = x.has[0] & x.has[1] & x.has[2] & x.has[3];
+    if (rb + kTile > wvis_min || !has) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int r = 32 * kt + 8 * (j >> 2) + 4 * h + (j & 3);
+          if (rb + r >= vis || !x.has[2 * kt + (j >> 3)]) s[kt][j] = -INFINITY;
+        }
+      if (QT == kQtE4m3) {
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) any |= x.nan[w];
+        nan_rows = __builtin_amdgcn_readfirstlane(any) != 0;
+      }
+    }
+    float tm = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int j = 1; j < 16; ++j) tm = fmaxf(tm, fmaxf(s[0][j], s[1][j]));
+    tm *= c;
+    if (__ballot(tm > m + kSlack)) {
+      const float mn = fmaxf(m, half_max(tm));
+      const float f = part_weight(m, mn);
+      m = mn;
+      mu = (mn == -INFINITY ? 0.f : mn) + kSlack;
+      sum *= f;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) acc[i] *= f;
+    }
+    u32x4_t pf[4];  // weights of rows 16 u + 4 h + {0..3, 8..11}
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) {
+        const float w0 = __builtin_amdgcn_exp2f(fmaf(s[kt][j], c, -mu));
+        const float w1 = __builtin_amdgcn_exp2f(fmaf(s[kt][j + 1], c, -mu));
+        sum += w0;
+        sum += w1;
+        pf[2 * kt + (j >> 3)][(j & 7) >> 1] = pack_bf16(w0, w1);
+      }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        const int e = 32 * i + n;
+        u32x4_t vf = *reinterpret_cast<const u32x4_t*>(&x.v[e * T::VS + ((2 * u + h) ^ ((e >> 4) & 7)) * 8]);
+        if (QT == kQtE4m3 && nan_rows) {
+          // a NaN counts for the columns that see its row alone: it leaves the products, and the columns
+          // that see one are marked by a product of indicators
+          u32x4_t nf, seen;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            nf[w] = ((vf[w] & 0x7FFFu) > 0x7F80u ? 0x3F80u : 0u) | ((vf[w] & 0x7FFF0000u) > 0x7F800000u ? 0x3F800000u : 0u);
+            vf[w] &= ((nf[w] & 0xFFFFu) ? 0u : 0xFFFFu) | ((nf[w] >> 16) ? 0u : 0xFFFF0000u);
+            const int r = rb + 16 * u + 8 * (w >> 1) + 4 * h + 2 * (w & 1);
+            seen[w] = (r < vis ? 0x3F80u : 0u) | (r + 1 < vis ? 0x3F800000u : 0u);
+          }
+          f32x16v hit;
+          hit = 0.f;
+          hit = mfma32(nf, seen, hit);
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (hit[j] > 0.f) acc[i][j] = NAN;
+        }
+        acc[i] = mfma32(vf, pf[u], acc[i]);
+      }
+  };
+
+  if (n_tiles > 0) {
+    ids(0);
+    codes(0);
+    if (n_tiles > 1) ids(1);
+    stage(0);
+    if (n_tiles > 1) codes(1);
+    if (n_tiles > 2) ids(2);
+    __syncthreads();
+    for (int t = 0; t < n_tiles; ++t) {
+      if (r0 + t * kTile < wvis_max) compute(t);
+      if (t + 1 < n_tiles) {
+        stage(t + 1);
+        if (t + 2 < n_tiles) codes(t + 2);
+        if (t + 3 < n_tiles) ids(t + 3);
+      }
+      __syncthreads();
+    }
+  }
+
+  if (!live) return;
+  sum = half_sum(sum);
+  if (a.n_split == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t* out = static_cast<uint16_t*>(a.out) + row * D;
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        u32x2_t y;
+        y[0] = pack_bf16(acc[i][j] * inv, acc[i][j + 1] * inv);
+        y[1] = pack_bf16(acc[i][j + 2] * inv, acc[i][j + 3] * inv);
+        *reinterpret_cast<u32x2_t*>(out + 32 * i + 2 * j + 4 * h) = y;
+      }
+  } else {
+    float* pt = a.part + (row * a.n_split + split) * (D + 2);
+    if (h == 0) {
+      pt[0] = m;
+      pt[1] = sum;
+    }
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; j += 2)
+        *reinterpret_cast<float2*>(pt + 2 + 32 * i + 8 * (j >> 2) + 4 * h + (j & 3)) = make_float2(acc[i][j], acc[i][j + 1]);
+  }
+}
+
+namespace {
+
+template <int QT, int D, int W> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
+  const int groups = (a.max_q * a.pc.group() + 32 * W - 1) / (32 * W);
+  const dim3 grid((unsigned)a.pc.h_kv, (unsigned)(groups * a.n_split), (unsigned)a.pc.n_prob);
+  constexpr int lds = 2 * (int)sizeof(Tile<D>);
+  auto kernel = paged_prompt_kernel<QT, D, W>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  kernel<<<grid, 64 * W, lds, stream>>>(a, groups);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_prompt(const PagedAttnArgs& a, int waves, hipStream_t stream) {
+  auto w = [&](auto qt, auto d) {
+    return waves == 4 ? attend<qt.value, d.value, 4>(a, stream) : attend<qt.value, d.value, 8>(a, stream);
+  };
+  auto d = [&](auto qt) {
+    return a.pc.d == 64 ? w(qt, std::integral_constant<int, 64>{}) : w(qt, std::integral_constant<int, 128>{});
+  };
+  return a.pc.qtype == kQtE4m3 ? d(std::integral_constant<int, kQtE4m3>{}) : d(std::integral_constant<int, kQtInt8>{});
+}
+
+}  // namespace kv

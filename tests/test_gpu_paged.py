@@ -6,7 +6,8 @@ rounding of an exact quotient.
 Attention.  The kernels multiply exact codes with exact (or split) operands and accumulate in fp32:
   - a logit errs by at most d 2^-24 sum |q k| (any order of d products), and its scaling and the
     exponential's argument by 4 2^-24 |t|, so a weight by the factor of both and 2 2^-24 of v_exp_f32;
-  - a weight enters the product with V with 16 bits (bf16 queries, 2^-16) or 24 (fp32, 2^-23);
+  - a weight enters the product with V with 16 bits (bf16 queries of up to 32 columns, 2^-16), rounded to
+    bf16 (more columns, half a step of 2^-8) or with 24 bits (fp32, 2^-23);
   - sums of n terms of one sign, n 2^-24 (weights) and n 2^-24 of sum w |v| (output).
 The error is at most the sum of these times sum w |v|, and for bf16 outputs half a step, 2^-8 |o|.
 Below the normal numbers it is absolute: a weight (and each of its terms, at most three, and its product with the
@@ -369,7 +370,7 @@ def _attend(pc, q, scale, n_q=None, max_q=None, fill=7.0):
     return out
 
 
-def _check(pc, q, scale, n_q, out, where, cap=None):
+def _check(pc, q, scale, n_q, out, where, max_q=None):
     """Every token's output against float64, within the bounds derived above."""
     dtype, qtype = pc.dtype_name, "e4m3" if pc.struct.qtype == _lib.KV_E4M3 else "int8"
     codes, scales = _image(pc)
@@ -378,6 +379,8 @@ def _check(pc, q, scale, n_q, out, where, cap=None):
     cap = min(table.shape[1] * pc.struct.block_rows, pc.struct.max_len)
     n_q = np.ones(len(lens), int) if n_q is None else np.asarray(n_q)
     at, eps = 0, 2.0 ** -24
+    cols = max(1, int(n_q.max()) if max_q is None else max_q) * pc.struct.h_q // pc.struct.h_kv
+    weight = 2.0 ** -23 if dtype == "f32" else 2.0 ** -16 if cols <= 32 else 2.0 ** -8
     for p, (L, n) in enumerate(zip(lens, n_q)):
         if n:
             rows = min(int(L), cap)
@@ -385,7 +388,7 @@ def _check(pc, q, scale, n_q, out, where, cap=None):
             v, _ = paged.cache_rows(codes[1], scales[1], table[p], rows, qtype)
             k, v = np.where(has[:, None], k, 0.0), np.where(has[:, None], v, 0.0)
             ref, mag, qk = paged.attention(qh[at:at + n], k, v, has, scale, int(L))
-            rel = 2 * (d + 4) * eps * qk + (2 * rows + 8) * eps + (2.0 ** -16 if dtype == "bf16" else 2.0 ** -23)
+            rel = 2 * (d + 4) * eps * qk + (2 * rows + 8) * eps + weight
             bound = rel * mag + (2.0 ** -8 * np.abs(ref) if dtype == "bf16" else eps * np.abs(ref))
             bound = bound + rows * 2.0 ** -116 * ((np.nanmax(np.abs(v)) if rows else 0.0) + 448)
             got = oh[at:at + n]
@@ -457,6 +460,23 @@ def test_attention_prompt_turn(dtype, qtype, d, R, G):
     q = _q(rng, sum(n_q) + 3, 2 * G, d, dtype)
     _say("attention turn", dtype, qtype, d, R, G)
     _check(pc, q, d ** -0.5, n_q, _attend(pc, q, d ** -0.5, n_q), "turn")
+
+
+@pytest.mark.parametrize("qtype,d,h_q,n_tok", [("e4m3", 128, 16, 40), ("int8", 128, 8, 33), ("e4m3", 64, 64, 70)])
+def test_attention_turns_of_many_problems(qtype, d, h_q, n_tok):
+    """Enough problems that no rows are split: ragged lengths and tokens, a padded batch, negative and zero
+    scales."""
+    rng = _rng(d, h_q)
+    n = 66
+    lens = rng.integers(0, 200, n)
+    n_q = np.minimum(rng.integers(0, n_tok + 1, n), lens)
+    n_q[7] = n_tok
+    pc = _cache(rng, "bf16", qtype, h_q, 8, d, 32, lens)
+    assert _lib.paged_attention_workspace_bytes(pc, int(n_q.sum()) + 1, n_tok) == 0
+    q = _q(rng, int(n_q.sum()) + 1, h_q, d, "bf16")
+    for scale in (d ** -0.5, -0.2, 0.0):
+        _say("attention many turns", qtype, d, h_q, scale)
+        _check(pc, q, scale, n_q, _attend(pc, q, scale, n_q), f"many turns {scale}")
 
 
 @pytest.mark.parametrize("n", [1, 3, 70])
@@ -565,7 +585,7 @@ def test_attention_strided_queries_and_wide_bounds():
     q = wide[:, :8]
     n_q = [5, 3, 2]
     out = _attend(pc, q, 0.08, n_q, max_q=11)
-    _check(pc, q, 0.08, n_q, out, "strided")
+    _check(pc, q, 0.08, n_q, out, "strided", max_q=11)
     plain = _attend(pc, q.contiguous(), 0.08, n_q, max_q=11)
     assert torch.equal(out, plain)
     off = torch.tensor([0, 5, 13, 13], dtype=torch.int32, device="cuda")  # the second reaches past 12 rows

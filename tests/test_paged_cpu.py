@@ -104,7 +104,10 @@ def test_attention_checks():
         assert _lib.lib().kv_paged_attention_workspace_bytes(c, n_tok, max_q) == 0
     assert _attend(c, off=NULL, n_tok=5) == _lib.KV_ERR_ARG       # one token each, but five of them
     assert _attend(c, off=NULL, n_tok=8, max_q=2) == _lib.KV_ERR_ARG
-    assert _attend(c, n_tok=1 << 20, max_q=1 << 20) == _lib.KV_ERR_SHAPE
+    assert _attend(c, n_tok=1 << 24, max_q=1 << 24) == _lib.KV_ERR_SHAPE
+    assert _attend(c, n_tok=1 << 25, max_q=(1 << 24) + 1) == _lib.KV_ERR_SHAPE
+    f = ctypes.byref(_cache(dtype=_lib.KV_F32))
+    assert _attend(f, n_tok=1 << 17, max_q=1 << 17) == _lib.KV_ERR_SHAPE
     assert _attend(c, stride=4095) == _attend(c, stride=4100) == _attend(c, stride=-8) == _lib.KV_ERR_ARG
 
 
