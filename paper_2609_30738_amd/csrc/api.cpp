@@ -895,7 +895,7 @@ int kv_paged_compact(const kv_problem* pr, const void* k, const void* v, const i
     const int64_t rows = (int64_t)(budget_host ? budget_host[p] : budget) + keep_tail;
     if (rows > (int64_t)pc.table_stride << pc.shift) return KV_ERR_SHAPE;
   }
-  return launch_status(kv::launch_paged_compact(pc, s.lens, s.tok_off, k, v, sel_idx, budget, budget_dev,
+  return launch_status(kv::launch_paged_compact(pc, s.lens, s.max_len, s.tok_off, k, v, sel_idx, budget, budget_dev,
                                                 keep_tail, static_cast<hipStream_t>(stream)));
 }
 

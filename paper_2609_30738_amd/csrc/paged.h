@@ -45,9 +45,9 @@ hipError_t launch_paged_tables(const Paged& pc, const TablesArgs& a, hipStream_t
 // Rows into the blocks (paged_store.hip).  tok_stride: elements between the rows of two tokens.
 hipError_t launch_paged_append(const Paged& pc, const void* k_new, const void* v_new, int64_t tok_stride,
                                const int32_t* slots, int n_tok, hipStream_t stream);
-hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, const int64_t* tok_off, const void* k,
-                                const void* v, const int32_t* sel_idx, int budget, const int32_t* budgets,
-                                int keep_tail, hipStream_t stream);
+hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, int max_len, const int64_t* tok_off,
+                                const void* k, const void* v, const int32_t* sel_idx, int budget,
+                                const int32_t* budgets, int keep_tail, hipStream_t stream);
 
 // Attention over the blocks (paged_attention.hip).
 struct PagedAttnArgs {

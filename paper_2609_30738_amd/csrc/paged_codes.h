@@ -33,28 +33,32 @@ template <int QT> __device__ __forceinline__ float block_scale(uint32_t amax_bit
 // 1 / s (exact for a scale as block_scale gives it); 1 for 0, whose block has no finite value but 0.
 __device__ __forceinline__ float inv_scale(float s) { return s > 0.f ? 1.f / s : 1.f; }
 
-// Four values in units of the scale as codes, rounded to nearest even; infinities saturate, and a NaN
-// stays one in e4m3 and becomes 0 in int8.
-template <int QT> __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
-  const float x[4] = {a, b, c, d};
+// Four values in units of the scale as codes, rounded to nearest even.  kFinite: the values are finite and
+// at most the largest code; else infinities saturate, and a NaN stays one in e4m3 and becomes 0 in int8.
+template <int QT, bool kFinite> __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  float x[4] = {a, b, c, d};
   if constexpr (QT == kQtE4m3) {
-    float y[4];
+    uint32_t nan = 0;
+    if constexpr (!kFinite) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i], -448.f, 448.f);
-    uint32_t u = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    u = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], (int)u, true);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (x[i] != x[i]) u = (u & ~(0xFFu << (8 * i))) | (0x7Fu << (8 * i));
-    return u;
+      for (int i = 0; i < 4; ++i) {
+        nan |= x[i] != x[i] ? 0xFFu << (8 * i) : 0u;
+        x[i] = __builtin_amdgcn_fmed3f(x[i], -448.f, 448.f);
+      }
+    }
+    uint32_t u = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    u = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], (int)u, true);
+    return kFinite ? u : (u & ~nan) | (0x7F7F7F7Fu & nan);
   } else {
-    uint32_t u = 0;
+    int y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float y = x[i] == x[i] ? __builtin_amdgcn_fmed3f(__builtin_rintf(x[i]), -127.f, 127.f) : 0.f;
-      u |= ((uint32_t)(int)y & 0xFFu) << (8 * i);
+      if constexpr (!kFinite) x[i] = x[i] == x[i] ? __builtin_amdgcn_fmed3f(x[i], -127.f, 127.f) : 0.f;
+      y[i] = (int)__builtin_rintf(x[i]);
     }
-    return u;
+    const uint32_t lo = __builtin_amdgcn_perm((uint32_t)y[1], (uint32_t)y[0], 0x0C0C0400u);
+    const uint32_t hi = __builtin_amdgcn_perm((uint32_t)y[3], (uint32_t)y[2], 0x04000C0Cu);
+    return lo | hi;
   }
 }
 

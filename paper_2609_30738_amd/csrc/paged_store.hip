@@ -1,8 +1,8 @@
 // Rows into the 8-bit blocks of a paged cache: new tokens (kv_paged_append) and the rows that an
 // eviction keeps (kv_paged_compact).
 //
-// A wave takes the rows of one (block, kv head) of K or of V: the largest |x| over them, the scale, the
-// codes.  16-byte loads: a row is CH chunks, a pass 64 / CH rows.
+// A wave takes the rows of one (block, kv head) of K or of V, 16 bytes a lane and load, and holds them in
+// registers: the largest |x| over them, the scale, the codes.  Bound by the rows' reads.
 #include <limits.h>
 #include <math.h>
 
@@ -20,12 +20,15 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
+typedef uint16_t __attribute__((ext_vector_type(2))) u16x2_t;
+
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
   return v;
 }
 
+// The values of a 16-byte chunk.
 template <int DT> __device__ __forceinline__ void chunk_values(const u32x4_t& u, float (&f)[16 / sizeof(typename Elem<DT>::T)]) {
   if constexpr (DT == kDtBf16) {
 #pragma unroll
@@ -39,15 +42,48 @@ template <int DT> __device__ __forceinline__ void chunk_values(const u32x4_t& u,
   }
 }
 
-// Rows row0 .. row0 + n - 1 of one block and head from `source` (its i-th row's 16-byte chunks, or null: a
-// row of zeros); the block holds row0 rows already, which move to a larger scale if these need one.
-// Every lane of the wave calls it.
+template <int QT, bool kFinite, int EPT> __device__ __forceinline__ void store_chunk(uint8_t* dst, const float (&f)[EPT], float inv) {
+  if constexpr (EPT == 8) {
+    u32x2_t u;
+    u[0] = encode4<QT, kFinite>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+    u[1] = encode4<QT, kFinite>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
+    *reinterpret_cast<u32x2_t*>(dst) = u;
+  } else {
+    *reinterpret_cast<uint32_t*>(dst) = encode4<QT, kFinite>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+  }
+}
+
+// Chunks of a lane in a block of 1 << SHIFT rows.
+template <int DT, int D, int SHIFT> constexpr int kChunks = ((D * (int)sizeof(typename Elem<DT>::T)) << SHIFT) / 1024;
+// Chunks that a lane holds in registers; blocks of more (fp32, 128 rows of 128) are read twice.
+constexpr int kHeldChunks = 32;
+
+// The scale of a block that holds row0 rows at scale `old` and gets rows whose own scale is s: the held codes move
+// by whole binades where s is larger.  Every lane of the wave calls it.
+template <int QT, int D> __device__ __forceinline__ float grown_scale(uint8_t* codes, int row0, float old, float s) {
+  if (row0 == 0) return s;
+  if (old >= s && old < INFINITY) return old;
+  const float f = old > 0.f && old < s ? old * inv_scale(s) : 0.f;
+  u32x4_t* at = reinterpret_cast<u32x4_t*>(codes);
+  for (int i = threadIdx.x & 63; i < row0 * D / 16; i += 64) {
+    u32x4_t u = at[i];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      float y[4];
+      decode4<QT>(u[w], y);
+      u[w] = encode4<QT, false>(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+    }
+    at[i] = u;
+  }
+  return s;
+}
+
+// store_rows for any values: read twice, infinities and NaNs apart.
 template <int DT, int QT, int D, typename Source>
-__device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row0, int n, Source source) {
-  constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T);
-  constexpr int CH = D / EPT;
-  constexpr int RPP = 64 / CH;
+__device__ __forceinline__ void store_rows_any(uint8_t* codes, float* scale, int row0, int n, Source source) {
+  constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH;
   const int lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
+  const float old = row0 > 0 ? *scale : 0.f;
   const u32x4_t zero = {0u, 0u, 0u, 0u};
   uint32_t amax = 0;
 #pragma unroll 4
@@ -61,43 +97,69 @@ __device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row
       amax = max(amax, u < 0x7F800000u ? u : 0u);
     }
   }
-  float s = block_scale<QT>(wave_max_u32(amax));
-  if (row0 > 0) {
-    const float old = *scale;
-    if (!(old >= s && old < INFINITY)) {  // the held codes move by whole binades
-      const float f = old > 0.f && old < s ? old * inv_scale(s) : 0.f;
-      u32x4_t* at = reinterpret_cast<u32x4_t*>(codes);
-      for (int i = lane; i < row0 * D / 16; i += 64) {
-        u32x4_t u = at[i];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          float x[4];
-          decode4<QT>(u[w], x);
-          u[w] = encode4<QT>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-        }
-        at[i] = u;
-      }
-    } else {
-      s = old;
-    }
-  }
-  const float inv = inv_scale(s);
+  const float s = grown_scale<QT, D>(codes, row0, old, block_scale<QT>(wave_max_u32(amax))), inv = inv_scale(s);
 #pragma unroll 4
   for (int i = rr; i < n; i += RPP) {
     const u32x4_t* src = source(i);
     float f[EPT];
     chunk_values<DT>(src ? src[c] : zero, f);
-    uint8_t* dst = codes + (row0 + i) * D + c * EPT;
-    if constexpr (EPT == 8) {
-      u32x2_t u;
-      u[0] = encode4<QT>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-      u[1] = encode4<QT>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
-      *reinterpret_cast<u32x2_t*>(dst) = u;
-    } else {
-      *reinterpret_cast<uint32_t*>(dst) = encode4<QT>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-    }
+    store_chunk<QT, false>(codes + (row0 + i) * D + c * EPT, f, inv);
   }
   if (lane == 0) *scale = s;
+}
+
+// Rows row0 .. row0 + n - 1 of one block and head from `source` (its i-th row's 16-byte chunks, or null: a
+// row of zeros); the block holds row0 rows already.  Every lane of the wave calls it.
+template <int DT, int QT, int D, int SHIFT, typename Source>
+__device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row0, int n, Source source) {
+  constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH;
+  constexpr int NC = kChunks<DT, D, SHIFT>;
+  if constexpr (NC > kHeldChunks) {
+    store_rows_any<DT, QT, D>(codes, scale, row0, n, source);
+    return;
+  } else {
+    const int lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
+    const float old = row0 > 0 ? *scale : 0.f;
+    u32x4_t x[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      x[i] = u32x4_t{0u, 0u, 0u, 0u};
+      if (i * RPP + rr < n) {
+        const u32x4_t* src = source(i * RPP + rr);
+        if (src) x[i] = src[c];
+      }
+    }
+    uint32_t amax = 0;  // without the signs; two bf16 at a time
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        if constexpr (DT == kDtBf16) {
+          const u16x2_t u = __builtin_bit_cast(u16x2_t, x[i][w] & 0x7FFF7FFFu);
+          amax = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, amax), u));
+        } else {
+          amax = max(amax, x[i][w] & 0x7FFFFFFFu);
+        }
+      }
+    if constexpr (DT == kDtBf16) amax = max(amax << 16, amax & 0xFFFF0000u);
+    amax = wave_max_u32(amax);
+    if (amax >= 0x7F800000u) {  // an infinity or a NaN among them
+      store_rows_any<DT, QT, D>(codes, scale, row0, n, source);
+      return;
+    }
+    const float s = grown_scale<QT, D>(codes, row0, old, block_scale<QT>(amax)), inv = inv_scale(s);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      // (a value's conversion is not kept from the first pass over the chunks: registers)
+      asm volatile("" : "+v"(x[i][0]), "+v"(x[i][1]), "+v"(x[i][2]), "+v"(x[i][3]));
+      if (i * RPP + rr < n) {
+        float f[EPT];
+        chunk_values<DT>(x[i], f);
+        store_chunk<QT, true>(codes + (row0 + i * RPP + rr) * D + c * EPT, f, inv);
+      }
+    }
+    if (lane == 0) *scale = s;
+  }
 }
 
 }  // namespace
@@ -113,7 +175,7 @@ struct AppendArgs {
 
 // A run: consecutive tokens in consecutive slots of one block.  A wave looks at 64 tokens' slots at once and
 // takes every n_share-th of the runs that begin among them.
-template <int DT, int QT, int D>
+template <int DT, int QT, int D, int SHIFT>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
   constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16;
   const int lane = threadIdx.x & 63;
@@ -125,8 +187,8 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
   const int share = (int)(id % a.n_share);
   const int64_t first = id / a.n_share * 64;
   if (first >= a.n_tok) return;
-  const int R = 1 << a.pc.shift;
-  const int n_slots = a.pc.n_blocks << a.pc.shift;
+  constexpr int R = 1 << SHIFT;
+  const int n_slots = a.pc.n_blocks << SHIFT;
   const int t = (int)first + lane;
   const int slot = t < a.n_tok ? a.slots[t] : -1;
   const int before = t > 0 && t < a.n_tok ? a.slots[t - 1] : -1;
@@ -148,10 +210,10 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
       }
       n += 64;
     }
-    const int64_t unit = (int64_t)(s0 >> a.pc.shift) * a.pc.h_kv + g;
+    const int64_t unit = (int64_t)(s0 >> SHIFT) * a.pc.h_kv + g;
     const u32x4_t* src = static_cast<const u32x4_t*>(kv ? a.v_new : a.k_new) + (int64_t)t0 * a.tok_chunks + g * CH;
-    store_rows<DT, QT, D>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit, row0, n,
-                          [&](int i) { return src + i * a.tok_chunks; });
+    store_rows<DT, QT, D, SHIFT>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit,
+                                 row0, n, [&](int i) { return src + i * a.tok_chunks; });
   }
 }
 
@@ -162,30 +224,110 @@ struct PagedCompactArgs {
   const void* k;
   const void* v;
   const int32_t* sel_idx;
-  int budget, keep_tail, wg_blocks;
+  int budget, keep_tail, wg_blocks, bitmap_words;
   const int32_t* budgets;
 };
 
-// One workgroup per (wg_blocks blocks, kv head, problem): the admitted positions sorted in LDS, then a wave
-// for each block of K and of V.
-template <int DT, int QT, int D>
+namespace {
+
+// Budgets up to which a position's rank is counted against all others, and the longest problem whose positions
+// are ranked through a bitmap (32 KB); beyond, or where a position is given twice, they are sorted.
+constexpr int kCountBudget = 256;
+constexpr int kBitmapLen = 1 << 18;
+
+// pos[0, n): the positions of rows first .. first + n - 1 of the unit, first + n <= bp: the ascending order of
+// sel[0, bp).  lds: work space (see compact_lds).  Starts and ends synchronised.
+__device__ __forceinline__ void kept_positions(const int32_t* sel, int bp, int L, int first, int n, int32_t* pos,
+                                               int32_t* work, int words) {
+  __shared__ int32_t sums[kWaves], below, twice;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (bp <= kCountBudget) {
+    const int mine = tid < bp ? sel[tid] : INT_MAX;
+    work[tid] = mine;
+    __syncthreads();
+    int rank = 0;
+    for (int j = 0; j < bp; j += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(work + j);
+      rank += (o.x < mine || (o.x == mine && j < tid)) + (o.y < mine || (o.y == mine && j + 1 < tid)) +
+              (o.z < mine || (o.z == mine && j + 2 < tid)) + (o.w < mine || (o.w == mine && j + 3 < tid));
+    }
+    if (tid < bp && rank >= first && rank < first + n) pos[rank - first] = mine;
+    __syncthreads();
+    return;
+  }
+  if (words > 0) {
+    const int used = (L + 31) >> 5;
+    for (int i = tid; i < used; i += kThreads) work[i] = 0;
+    if (tid == 0) below = twice = 0;
+    __syncthreads();
+    int low = 0, again = 0;
+    for (int i = tid; i < bp; i += kThreads) {
+      const int x = sel[i];
+      if (x < 0) ++low;
+      else if (x < L) again |= (atomicOr(reinterpret_cast<uint32_t*>(work) + (x >> 5), 1u << (x & 31)) >> (x & 31)) & 1;
+    }
+    if (low) atomicAdd(&below, low);
+    if (again) twice = 1;
+    __syncthreads();
+    if (!twice) {
+      // positions below 0 first, then the bitmap's, then those past the problem: a thread takes consecutive words
+      const int per = (used + kThreads - 1) / kThreads, w0 = min(tid * per, used), w1 = min(w0 + per, used);
+      int count = 0;
+      for (int w = w0; w < w1; ++w) count += __popc((uint32_t)work[w]);
+      int incl = count;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += u;
+      }
+      if (lane == 63) sums[wave] = incl;
+      __syncthreads();
+      int rank = below + incl - count, total = below;
+      for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) rank += sums[w];
+        total += sums[w];
+      }
+      if (rank < first + n && rank + count > first) {
+        for (int w = w0; w < w1; ++w)
+          for (uint32_t bits = (uint32_t)work[w]; bits; bits &= bits - 1, ++rank)
+            if (rank >= first && rank < first + n) pos[rank - first] = 32 * w + __ffs((int)bits) - 1;
+      }
+      for (int i = tid; i < n; i += kThreads)
+        if (first + i < below || first + i >= total) pos[i] = -1;
+      __syncthreads();
+      return;
+    }
+  }
+  int n2 = 1;
+  while (n2 < bp) n2 <<= 1;
+  __syncthreads();
+  for (int i = tid; i < n2; i += kThreads) work[i] = i < bp ? sel[i] : INT_MAX;
+  __syncthreads();
+  sort_positions(work, n2, tid, kThreads);
+  for (int i = tid; i < n; i += kThreads) pos[i] = work[first + i];
+  __syncthreads();
+}
+
+}  // namespace
+
+// One workgroup per (wg_blocks blocks, kv head, problem): the ranks of the admitted positions, then a wave for
+// each block of K and of V.
+template <int DT, int QT, int D, int SHIFT>
 __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArgs a) {
-  constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16;
-  extern __shared__ int32_t srt[];
-  const int g = blockIdx.y, p = blockIdx.z, R = 1 << a.pc.shift;
+  constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16, R = 1 << SHIFT;
+  extern __shared__ __align__(16) int32_t lds[];  // positions of the workgroup's rows, then work space
+  const int g = blockIdx.y, p = blockIdx.z;
   const int L = a.lens[p];
   const int bp = a.budgets ? min(a.budgets[p], a.budget) : a.budget;
   const int rows = bp + a.keep_tail;
-  const int j0 = blockIdx.x * a.wg_blocks;
-  if (j0 << a.pc.shift >= rows) return;
-  int n2 = 1;
-  while (n2 < bp) n2 <<= 1;
-  const int32_t* sel = a.sel_idx + ((int64_t)p * a.pc.h_kv + g) * a.budget;
-  for (int i = threadIdx.x; i < n2; i += kThreads) srt[i] = i < bp ? sel[i] : INT_MAX;
-  __syncthreads();
-  sort_positions(srt, n2, threadIdx.x, kThreads);
+  const int j0 = blockIdx.x * a.wg_blocks, first = j0 << SHIFT;
+  if (first >= rows) return;
+  const int n = min(max(bp - first, 0), a.wg_blocks << SHIFT);  // admitted rows among the workgroup's
+  if (n > 0)
+    kept_positions(a.sel_idx + ((int64_t)p * a.pc.h_kv + g) * a.budget, bp, L, first, n, lds,
+                   lds + (a.wg_blocks << SHIFT), L <= a.bitmap_words * 32 ? a.bitmap_words : 0);
   const int64_t base = (a.tok_off[p] * a.pc.h_kv + (int64_t)g * L) * CH;
-  const int blocks = min((rows + R - 1) >> a.pc.shift, a.pc.table_stride);
+  const int blocks = min((rows + R - 1) >> SHIFT, a.pc.table_stride);
   for (int task = threadIdx.x >> 6; task < 2 * a.wg_blocks; task += kWaves) {
     const int j = j0 + (task >> 1), kv = task & 1;
     if (j >= blocks) break;
@@ -193,28 +335,33 @@ __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArg
     if (block < 0 || block >= a.pc.n_blocks) continue;
     const u32x4_t* src = static_cast<const u32x4_t*>(kv ? a.v : a.k) + base;
     const int64_t unit = (int64_t)block * a.pc.h_kv + g;
-    const int r0 = j << a.pc.shift;
-    store_rows<DT, QT, D>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit, 0,
-                          min(R, rows - r0), [&](int i) -> const u32x4_t* {
-                            const int r = r0 + i;
-                            const int pos = r < bp ? srt[r] : L - a.keep_tail + (r - bp);
-                            return pos < 0 || pos >= L ? nullptr : src + (int64_t)pos * CH;
-                          });
+    const int r0 = j << SHIFT;
+    store_rows<DT, QT, D, SHIFT>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit, 0,
+                                 min(R, rows - r0), [&](int i) -> const u32x4_t* {
+                                   const int r = r0 + i;
+                                   const int pos = r < bp ? lds[r - first] : L - a.keep_tail + (r - bp);
+                                   return pos < 0 || pos >= L ? nullptr : src + (int64_t)pos * CH;
+                                 });
   }
 }
 
 namespace {
 
-// f<dtype, qtype, d>()
+template <int V> using Int = std::integral_constant<int, V>;
+
+// f(dtype, qtype, d, shift) of integral constants.
 template <typename F> hipError_t dispatch(const Paged& pc, F f) {
-  auto d = [&](auto dt, auto qt) {
-    return pc.d == 64 ? f(dt, qt, std::integral_constant<int, 64>{}) : f(dt, qt, std::integral_constant<int, 128>{});
+  auto shift = [&](auto dt, auto qt, auto d) {
+    switch (pc.shift) {
+      case 4: return f(dt, qt, d, Int<4>{});
+      case 5: return f(dt, qt, d, Int<5>{});
+      case 6: return f(dt, qt, d, Int<6>{});
+      default: return f(dt, qt, d, Int<7>{});
+    }
   };
-  auto q = [&](auto dt) {
-    return pc.qtype == kQtE4m3 ? d(dt, std::integral_constant<int, kQtE4m3>{})
-                               : d(dt, std::integral_constant<int, kQtInt8>{});
-  };
-  return pc.dtype == kDtBf16 ? q(std::integral_constant<int, kDtBf16>{}) : q(std::integral_constant<int, kDtF32>{});
+  auto d = [&](auto dt, auto qt) { return pc.d == 64 ? shift(dt, qt, Int<64>{}) : shift(dt, qt, Int<128>{}); };
+  auto q = [&](auto dt) { return pc.qtype == kQtE4m3 ? d(dt, Int<kQtE4m3>{}) : d(dt, Int<kQtInt8>{}); };
+  return pc.dtype == kDtBf16 ? q(Int<kDtBf16>{}) : q(Int<kDtF32>{});
 }
 
 }  // namespace
@@ -222,28 +369,34 @@ template <typename F> hipError_t dispatch(const Paged& pc, F f) {
 hipError_t launch_paged_append(const Paged& pc, const void* k_new, const void* v_new, int64_t tok_stride,
                                const int32_t* slots, int n_tok, hipStream_t stream) {
   AppendArgs a{pc, k_new, v_new, tok_stride / (pc.dtype == kDtBf16 ? 8 : 4), slots, n_tok, 1};
-  const int64_t chunks = (n_tok + 63) / 64, units = chunks * pc.h_kv * 2;
+  const int64_t chunks = ((int64_t)n_tok + 63) / 64, units = chunks * pc.h_kv * 2;
   // single rows of many requests are runs of their own: as many waves to 64 tokens as fill the chip
   constexpr int64_t kFill = 16384;
   a.n_share = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(n_tok, 64), kFill / units));
   const unsigned wgs = (unsigned)((units * a.n_share + kWaves - 1) / kWaves);
-  return dispatch(pc, [&](auto dt, auto qt, auto d) {
-    paged_append_kernel<dt.value, qt.value, d.value><<<wgs, kThreads, 0, stream>>>(a);
+  return dispatch(pc, [&](auto dt, auto qt, auto d, auto shift) {
+    paged_append_kernel<dt.value, qt.value, d.value, shift.value><<<wgs, kThreads, 0, stream>>>(a);
     return hipGetLastError();
   });
 }
 
-hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, const int64_t* tok_off, const void* k,
-                                const void* v, const int32_t* sel_idx, int budget, const int32_t* budgets,
-                                int keep_tail, hipStream_t stream) {
-  PagedCompactArgs a{pc, lens, tok_off, k, v, sel_idx, budget, keep_tail, 1, budgets};
+hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, int max_len, const int64_t* tok_off,
+                                const void* k, const void* v, const int32_t* sel_idx, int budget,
+                                const int32_t* budgets, int keep_tail, hipStream_t stream) {
+  PagedCompactArgs a{pc, lens, tok_off, k, v, sel_idx, budget, keep_tail, 1, 0, budgets};
   const int blocks = (budget + keep_tail + (1 << pc.shift) - 1) >> pc.shift;
-  a.wg_blocks = std::max(2, 128 >> pc.shift);
-  int n2 = 1;
-  while (n2 < budget) n2 <<= 1;
+  a.wg_blocks = budget <= kCountBudget ? 2 : std::max(2, 256 >> pc.shift);
+  int work = kThreads;  // words: the counted positions, the bitmap, the sorted positions
+  if (budget > kCountBudget) {
+    if (max_len <= kBitmapLen) a.bitmap_words = (max_len + 31) / 32;
+    int n2 = 1;
+    while (n2 < budget) n2 <<= 1;
+    work = std::max(a.bitmap_words, n2);
+  }
+  const size_t bytes = ((size_t)(a.wg_blocks << pc.shift) + work) * sizeof(int32_t);
   const dim3 grid((unsigned)((blocks + a.wg_blocks - 1) / a.wg_blocks), (unsigned)pc.h_kv, (unsigned)pc.n_prob);
-  return dispatch(pc, [&](auto dt, auto qt, auto d) {
-    paged_compact_kernel<dt.value, qt.value, d.value><<<grid, kThreads, n2 * sizeof(int32_t), stream>>>(a);
+  return dispatch(pc, [&](auto dt, auto qt, auto d, auto shift) {
+    paged_compact_kernel<dt.value, qt.value, d.value, shift.value><<<grid, kThreads, bytes, stream>>>(a);
     return hipGetLastError();
   });
 }
