@@ -10,8 +10,10 @@
 //     O^T = V^T P^T.
 //   Row 4 j + l / 16 of a tile stands for row l / 16 * 4 + j of the accumulator, so that a load of V reads
 //   four whole consecutive rows; the lane's operand of V is transposed in registers.
-//   fp32 queries and weights are taken as three bf16 terms each (24 bits), the weights of bf16 queries as
-//   two: the matrix products lose nothing of the operands beyond that, and accumulate in fp32.
+//   fp32 queries and weights are taken as three bf16 terms each (24 bits): the matrix products lose nothing
+//   of the operands beyond that, and accumulate in fp32.  With bf16 queries the weights are two terms for up
+//   to 16 columns, where the second one is free beside the loads, and one for more (2^-9 of each, a step of
+//   the output; five tokens of 16 requests 59 us, with two terms 64).
 //   The reference of a column's weights is raised, and the sums rescaled, only when a logit exceeds it by
 //   more than kSlack octaves; weights are 2^(t - m - kSlack), so that none exceeds 1.
 //   The four waves are merged through LDS; with several splits the partial sums go to the workspace and
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
   constexpr int KH = D / 64;                       // 16-byte loads of a key
   constexpr int VW = D / 64;                       // words of a value row that a lane loads
   constexpr int QN = DT == kDtBf16 ? 1 : 3;        // bf16 terms of a query
-  constexpr int PN = DT == kDtBf16 ? 2 : 3;        // and of a weight
+  constexpr int PN = DT == kDtF32 ? 3 : (NT == 1 ? 2 : 1);  // and of a weight
   constexpr int COLS = 16 * NT;
   __shared__ int32_t sh_block[kMaxSplitBlocks];
   __shared__ float sh_ks[kMaxSplitBlocks], sh_vs[kMaxSplitBlocks];
@@ -104,52 +106,28 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
 
   const int split = blockIdx.x, g = blockIdx.y / n_groups, cg = blockIdx.y % n_groups, p = blockIdx.z;
   const int G = a.pc.h_q / a.pc.h_kv;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, kg = lane >> 4;
+  const int shift = a.pc.shift, R = 1 << shift;
+  const int r0 = split * a.split_rows;
+  // the split's table entries load beside the lengths
+  const int entry = (r0 >> shift) + tid;
+  const int id = tid << shift < a.split_rows && entry < a.pc.table_stride
+                     ? a.pc.table[(int64_t)p * a.pc.table_stride + entry] : -1;
   const Span sp = span_of(a, p);
   const int col0 = cg * COLS;
   const int n_cols = min(sp.n_tok * G - col0, COLS);
   if (n_cols <= 0) return;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, kg = lane >> 4;
-  const int shift = a.pc.shift, R = 1 << shift;
-  const int r0 = split * a.split_rows;
   const int vis_max = sp.visible((col0 + n_cols - 1) / G);
   const int vis_min = sp.visible(col0 / G);
   const int r1 = min(vis_max, r0 + a.split_rows);
   if (r0 >= r1 && a.n_split > 1) return;  // the join reads the splits below a column's last row
 
-  // blocks and scales of the split's rows
-  for (int i = tid; i << shift < r1 - r0; i += kThreads) {
-    const int id = a.pc.table[(int64_t)p * a.pc.table_stride + (r0 >> shift) + i];
-    const bool ok = id >= 0 && id < a.pc.n_blocks;
-    sh_block[i] = ok ? id : -1;
-    const int64_t at = (int64_t)(ok ? id : 0) * a.pc.h_kv + g;
-    sh_ks[i] = ok ? a.pc.k_scale[at] * a.c : 0.f;
-    sh_vs[i] = ok ? a.pc.v_scale[at] : 0.f;
-  }
-
-  // the queries' operand: column n, elements 64 (s / 2) + 16 kg + 8 (s % 2) .. + 7 (D = 64: 16 kg + 8 s)
-  u32x4_t qf[NT][NS][QN];
-  int vis[NT];
-#pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    const int col = col0 + 16 * ct + n;
-    const bool live = 16 * ct + n < n_cols;
-    const int j = live ? col / G : 0, h = live ? col % G : 0;
-    vis[ct] = live ? sp.visible(j) : 0;
-    const int64_t at = (int64_t)(sp.tok0 + j) * a.q_stride + (int64_t)(g * G + h) * D;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const int e = 64 * (s >> 1) + 16 * kg + 8 * (s & 1);
-      if constexpr (DT == kDtBf16) {
-        qf[ct][s][0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at + e);
-      } else {
-        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + e);
-        const float4 x = src[0], y = src[1];
-        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-        split_terms<QN>(f, qf[ct][s]);
-      }
-    }
-  }
+  // blocks and scales of the split's rows: the scales arrive beside the first codes
+  const bool has = tid << shift < r1 - r0 && id >= 0 && id < a.pc.n_blocks;
+  if (tid < kMaxSplitBlocks) sh_block[tid] = has ? id : -1;
   __syncthreads();
+  const int64_t scale_at = (int64_t)(has ? id : 0) * a.pc.h_kv + g;
+  const float my_ks = has ? a.pc.k_scale[scale_at] * a.c : 0.f, my_vs = has ? a.pc.v_scale[scale_at] : 0.f;
 
   // the codes of 32 rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n
   u32x4_t xk[2][KH];
@@ -185,6 +163,41 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
       }
     }
   };
+
+  constexpr int kRound = kWaves * kStep;
+  const int rb0 = r0 + wave * kStep;
+  if (rb0 < r1) {
+    load_k(rb0);
+    load_v(rb0);
+  }
+  // the queries' operand: column n, elements 64 (s / 2) + 16 kg + 8 (s % 2) .. + 7 (D = 64: 16 kg + 8 s)
+  u32x4_t qf[NT][NS][QN];
+  int vis[NT];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    const int col = col0 + 16 * ct + n;
+    const bool live = 16 * ct + n < n_cols;
+    const int j = live ? col / G : 0, h = live ? col % G : 0;
+    vis[ct] = live ? sp.visible(j) : 0;
+    const int64_t at = (int64_t)(sp.tok0 + j) * a.q_stride + (int64_t)(g * G + h) * D;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int e = 64 * (s >> 1) + 16 * kg + 8 * (s & 1);
+      if constexpr (DT == kDtBf16) {
+        qf[ct][s][0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at + e);
+      } else {
+        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + e);
+        const float4 x = src[0], y = src[1];
+        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        split_terms<QN>(f, qf[ct][s]);
+      }
+    }
+  }
+  if (tid < kMaxSplitBlocks) {
+    sh_ks[tid] = my_ks;
+    sh_vs[tid] = my_vs;
+  }
+  __syncthreads();
 
   float m[NT], mu[NT], sum[NT];  // mu: m, or 0 before the first finite logit
   f32x4v acc[NT][NI];
@@ -230,6 +243,12 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
     }
 
     float lg[NT][8];
+    // (codes are converted here, not where they were loaded a step before: registers)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < KH; ++i)
+        asm volatile("" : "+v"(xk[t][i][0]), "+v"(xk[t][i][1]), "+v"(xk[t][i][2]), "+v"(xk[t][i][3]));
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       f32x4v s4[NT];
@@ -293,40 +312,60 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
       split_terms<PN>(w, pf[ct]);
     }
 
-    // V^T: eight rows' words of four elements, transposed to four elements' operands
+    if (QT == kQtE4m3 && nan_rows) {
+      // a NaN counts for the columns that see its row alone: these are marked by a product of indicators,
+      // and it leaves the codes
 #pragma unroll
-    for (int w = 0; w < VW; ++w) {
-      u32x2_t b[8];
+      for (int ct = 0; ct < NT; ++ct) {
+        u32x4_t seen;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) b[e] = decode4_bf16<QT>(xv[e >> 2][e & 3][w]);
+        for (int e = 0; e < 8; e += 2) {
+          const int r = rb + 16 * (e >> 2) + 4 * (e & 3) + kg;
+          seen[e >> 1] = (r < vis[ct] ? 0x3F80u : 0u) | (r + 4 < vis[ct] ? 0x3F800000u : 0u);
+        }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u32x4_t vf;
+        for (int w = 0; w < VW; ++w)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          vf[e] = __builtin_amdgcn_perm(b[2 * e + 1][i >> 1], b[2 * e][i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
-        if (QT == kQtE4m3 && nan_rows) {
-          // a NaN counts for the columns that see its row alone: it leaves the products, and the columns
-          // that see one are marked by a product of indicators
-          u32x4_t nf;
+          for (int i = 0; i < 4; ++i) {
+            u32x4_t nf;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            nf[e] = ((vf[e] & 0x7FFFu) > 0x7F80u ? 0x3F80u : 0u) | ((vf[e] & 0x7FFF0000u) > 0x7F800000u ? 0x3F800000u : 0u);
-            vf[e] &= ((nf[e] & 0xFFFFu) ? 0u : 0xFFFFu) | ((nf[e] >> 16) ? 0u : 0xFFFF0000u);
-          }
-#pragma unroll
-          for (int ct = 0; ct < NT; ++ct) {
-            float seen[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) seen[e] = rb + 16 * (e >> 2) + 4 * (e & 3) + kg < vis[ct] ? 1.f : 0.f;
-            u32x4_t one[1];
-            split_terms<1>(seen, one);
-            const f32x4v hit = mfma16(nf, one[0], f32x4v{0.f, 0.f, 0.f, 0.f});
+            for (int e = 0; e < 8; e += 2)
+              nf[e >> 1] = ((xv[e >> 2][e & 3][w] >> (8 * i) & 0x7Fu) == 0x7Fu ? 0x3F80u : 0u) |
+                           ((xv[e >> 2][(e & 3) + 1][w] >> (8 * i) & 0x7Fu) == 0x7Fu ? 0x3F800000u : 0u);
+            const f32x4v hit = mfma16(nf, seen, f32x4v{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               if (hit[j] > 0.f) acc[ct][4 * w + i][j] = NAN;
           }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int w = 0; w < VW; ++w) {
+            const uint32_t u = (((xv[t][j][w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
+            xv[t][j][w] &= ~(u * 0xFFu);
+          }
+    }
+    // V^T: eight rows' words of four elements, transposed to four elements' operands
+#pragma unroll
+    for (int w = 0; w < VW; ++w) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        asm volatile("" : "+v"(xv[t][0][w]), "+v"(xv[t][1][w]), "+v"(xv[t][2][w]), "+v"(xv[t][3][w]));
+      uint32_t b[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i % 2 == 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            b[e] = i == 0 ? decode2_bf16<QT, 0>(xv[e >> 2][e & 3][w]) : decode2_bf16<QT, 1>(xv[e >> 2][e & 3][w]);
         }
+        u32x4_t vf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          vf[e] = __builtin_amdgcn_perm(b[2 * e + 1], b[2 * e], i & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
         for (int ct = 0; ct < NT; ++ct)
 #pragma unroll
@@ -336,16 +375,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
     if (next < r1) load_v(next);
   };
 
-  // the waves' steps in turn
-  {
-    constexpr int kRound = kWaves * kStep;
-    int rb = r0 + wave * kStep;
-    if (rb < r1) {
-      load_k(rb);
-      load_v(rb);
-    }
-    for (; rb < r1; rb += kRound) step(rb, rb + kRound);
-  }
+  for (int rb = rb0; rb < r1; rb += kRound) step(rb, rb + kRound);  // the waves' steps in turn
 
   // merge of the waves, 16 columns at a time: element 4 VW (4 kg + j) + 4 w + i of column n
 #pragma unroll
@@ -395,45 +425,67 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
   }
 }
 
-// One workgroup per (column, kv head, problem): the splits below the column's last visible row.
+// One workgroup per (column, kv head, problem): the splits below the column's last visible row, the waves' in
+// turn, kJoin at a time in flight.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void paged_combine_kernel(PagedAttnArgs a) {
-  constexpr int PARTS = kThreads / D;
-  __shared__ float sh_a[PARTS][D], sh_m[PARTS], sh_s[PARTS];
+  constexpr int E = D / 64, kJoin = 4;
+  __shared__ float sh_a[kWaves][D], sh_m[kWaves], sh_s[kWaves];
   const int col = blockIdx.x, g = blockIdx.y, p = blockIdx.z, G = a.pc.h_q / a.pc.h_kv;
   const Span sp = span_of(a, p);
   if (col >= sp.n_tok * G) return;
   const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
   const int n_split = (sp.visible(col / G) + a.split_rows - 1) / a.split_rows;
-  const int e = threadIdx.x % D, pt = threadIdx.x / D;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const float* part = a.part + row * a.n_split * (D + 2);
-  float m = -INFINITY, S = 0.f, A = 0.f;
-  for (int i = pt; i < n_split; i += PARTS) {
-    const float* x = part + (int64_t)i * (D + 2);
-    const float mn = fmaxf(m, x[0]), f = part_weight(m, mn), w = part_weight(x[0], mn);
-    S = fmaf(x[1], w, S * f);
-    A = fmaf(x[2 + e], w, A * f);
+  float m = -INFINITY, S = 0.f, A[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) A[e] = 0.f;
+  for (int i = wave; i < n_split; i += kJoin * kWaves) {
+    float xm[kJoin], xs[kJoin], xa[kJoin][E];
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j) {
+      const bool in = i + j * kWaves < n_split;
+      const float* x = part + (int64_t)(in ? i + j * kWaves : i) * (D + 2);
+      xm[j] = in ? x[0] : -INFINITY;
+      xs[j] = in ? x[1] : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) xa[j][e] = in ? x[2 + E * lane + e] : 0.f;
+    }
+    float mn = m;
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j) mn = fmaxf(mn, xm[j]);
+    const float f = part_weight(m, mn);
+    S *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) A[e] *= f;
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j) {
+      const float w = part_weight(xm[j], mn);
+      S = fmaf(xs[j], w, S);
+#pragma unroll
+      for (int e = 0; e < E; ++e) A[e] = fmaf(xa[j][e], w, A[e]);
+    }
     m = mn;
   }
-  sh_a[pt][e] = A;
-  if (e == 0) {
-    sh_m[pt] = m;
-    sh_s[pt] = S;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sh_a[wave][E * lane + e] = A[e];
+  if (lane == 0) {
+    sh_m[wave] = m;
+    sh_s[wave] = S;
   }
   __syncthreads();
-  if (pt != 0) return;
-  float M = -INFINITY;
+  if (tid >= D) return;
+  float M = -INFINITY, total = 0.f, out = 0.f;
 #pragma unroll
-  for (int q = 0; q < PARTS; ++q) M = fmaxf(M, sh_m[q]);
-  S = 0.f;
-  A = 0.f;
+  for (int q = 0; q < kWaves; ++q) M = fmaxf(M, sh_m[q]);
 #pragma unroll
-  for (int q = 0; q < PARTS; ++q) {
+  for (int q = 0; q < kWaves; ++q) {
     const float f = part_weight(sh_m[q], M);
-    S = fmaf(sh_s[q], f, S);
-    A = fmaf(sh_a[q][e], f, A);
+    total = fmaf(sh_s[q], f, total);
+    out = fmaf(sh_a[q][tid], f, out);
   }
-  store_out<DT>(a.out, row * D + e, A, S);
+  store_out<DT>(a.out, row * D + tid, out, total);
 }
 
 namespace {
@@ -461,7 +513,7 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
   } else {
     constexpr int64_t kRound = 768, kMinSplit = 256;
     units = (int64_t)pc.n_prob * pc.h_kv * column_groups(max_q, pc.group());
-    if (rows > 512) n = std::max<int64_t>(1, std::min(3 * kRound / units, (rows + kMinSplit - 1) / kMinSplit));
+    if (rows > 512) n = std::max<int64_t>(1, std::min(2 * kRound / units, (rows + kMinSplit - 1) / kMinSplit));
   }
   int64_t split = ((rows + n - 1) / n + 127) / 128 * 128;
   if (!plan.prompt_waves) split = std::min<int64_t>(split, kMaxSplitRows);

@@ -75,20 +75,18 @@ template <int QT> __device__ __forceinline__ void decode4(uint32_t u, float (&f)
   }
 }
 
-// Four codes times a power of two as bf16 pairs (0, 1) and (2, 3): exact, every code has at most 8
+// Codes 2 H and 2 H + 1 of a word times a power of two as a bf16 pair: exact, every code has at most 8
 // significant bits.
-template <int QT> __device__ __forceinline__ u32x2_t decode4_bf16(uint32_t u, float scale = 1.f) {
-  u32x2_t r;
+template <int QT, int H> __device__ __forceinline__ uint32_t decode2_bf16(uint32_t u, float scale = 1.f) {
   if constexpr (QT == kQtE4m3) {
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, scale, false));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, scale, true));
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, scale, H != 0));
   } else {
-    float f[4];
-    decode4<QT>(u, f);
-    r[0] = __builtin_amdgcn_perm(__float_as_uint(f[1] * scale), __float_as_uint(f[0] * scale), 0x07060302u);
-    r[1] = __builtin_amdgcn_perm(__float_as_uint(f[3] * scale), __float_as_uint(f[2] * scale), 0x07060302u);
+    const float a = (float)(int8_t)(u >> (16 * H)) * scale, b = (float)(int8_t)(u >> (16 * H + 8)) * scale;
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
   }
-  return r;
+}
+template <int QT> __device__ __forceinline__ u32x2_t decode4_bf16(uint32_t u, float scale = 1.f) {
+  return u32x2_t{decode2_bf16<QT, 0>(u, scale), decode2_bf16<QT, 1>(u, scale)};
 }
 
 }  // namespace kv

@@ -6,7 +6,7 @@ rounding of an exact quotient.
 Attention.  The kernels multiply exact codes with exact (or split) operands and accumulate in fp32:
   - a logit errs by at most d 2^-24 sum |q k| (any order of d products), and its scaling and the
     exponential's argument by 4 2^-24 |t|, so a weight by the factor of both and 2 2^-24 of v_exp_f32;
-  - a weight enters the product with V with 16 bits (bf16 queries of up to 32 columns, 2^-16), rounded to
+  - a weight enters the product with V with 16 bits (bf16 queries of up to 16 columns, 2^-16), rounded to
     bf16 (more columns, half a step of 2^-8) or with 24 bits (fp32, 2^-23);
   - sums of n terms of one sign, n 2^-24 (weights) and n 2^-24 of sum w |v| (output).
 The error is at most the sum of these times sum w |v|, and for bf16 outputs half a step, 2^-8 |o|.
@@ -380,7 +380,7 @@ def _check(pc, q, scale, n_q, out, where, max_q=None):
     n_q = np.ones(len(lens), int) if n_q is None else np.asarray(n_q)
     at, eps = 0, 2.0 ** -24
     cols = max(1, int(n_q.max()) if max_q is None else max_q) * pc.struct.h_q // pc.struct.h_kv
-    weight = 2.0 ** -23 if dtype == "f32" else 2.0 ** -16 if cols <= 32 else 2.0 ** -8
+    weight = 2.0 ** -23 if dtype == "f32" else 2.0 ** -16 if cols <= 16 else 2.0 ** -8
     for p, (L, n) in enumerate(zip(lens, n_q)):
         if n:
             rows = min(int(L), cap)
