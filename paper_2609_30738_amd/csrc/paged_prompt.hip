@@ -27,7 +27,9 @@ namespace kv {
 
 namespace {
 
-constexpr int kTile = 64;  // rows of a tile
+constexpr int kTile = 64;            // rows of a tile
+constexpr float kOctaves = 24.f;     // of the weights below 1 when a reference is taken
+constexpr float kLowest = 0x1p126f;  // minus it: below every logit
 
 typedef float __attribute__((ext_vector_type(16))) f32x16v;
 
@@ -207,7 +209,10 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
     }
   };
 
-  float m = -INFINITY, mu = kSlack, sum = 0.f;  // mu: m (0 before the first finite logit) + kSlack
+  // Weights are 2^(t - mu), mu = reference + kOctaves: at most 1 until a logit exceeds the reference by more.  A
+  // tile whose weights sum to more than 1 in some lane raises the reference to its largest logit (the first
+  // tile does: it starts below every logit); no maximum is taken otherwise.
+  float mu = -kLowest, sum = 0.f;
   f32x16v acc[ND];
 #pragma unroll
   for (int i = 0; i < ND; ++i) acc[i] = 0.f;
@@ -226,7 +231,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       }
     }
     bool nan_rows = false;
-    const int has = x.has[0] & x.has[1] & x.has[2] & x.has[3];
+    const int has = __builtin_amdgcn_readfirstlane(x.has[0] & x.has[1] & x.has[2] & x.has[3]);
     if (rb + kTile > wvis_min || !has) {
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
@@ -242,40 +247,50 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
         nan_rows = __builtin_amdgcn_readfirstlane(any) != 0;
       }
     }
-    float tm = fmaxf(s[0][0], s[1][0]);
+    u32x4_t pf[4];  // weights of rows 16 u + 4 h + {0..3, 8..11}
+    float part[4];
+    auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 1; j < 16; ++j) tm = fmaxf(tm, fmaxf(s[0][j], s[1][j]));
-    tm *= c;
-    if (__ballot(tm > m + kSlack)) {
-      const float mn = fmaxf(m, half_max(tm));
-      const float f = part_weight(m, mn);
-      m = mn;
-      mu = (mn == -INFINITY ? 0.f : mn) + kSlack;
+      for (int u = 0; u < 4; ++u) {
+        part[u] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const float w0 = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + j], c, -mu));
+          const float w1 = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + j + 1], c, -mu));
+          part[u] += w0;
+          part[u] += w1;
+          pf[u][j >> 1] = pack_bf16(w0, w1);
+        }
+      }
+      return (part[0] + part[1]) + (part[2] + part[3]);
+    };
+    float ts = weigh();
+    if (__ballot(ts > 1.f)) {
+      float tm = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+      for (int j = 1; j < 16; ++j) tm = fmaxf(tm, fmaxf(s[0][j], s[1][j]));
+      // a column whose logits are all -inf so far keeps the lowest reference
+      const float top = fmaxf(half_max(tm) * c, -kLowest), mn = fmaxf(mu, top + kOctaves);
+      const float f = __builtin_amdgcn_exp2f(mu - mn);
+      mu = mn;
       sum *= f;
 #pragma unroll
       for (int i = 0; i < ND; ++i) acc[i] *= f;
+      ts = weigh();
     }
-    u32x4_t pf[4];  // weights of rows 16 u + 4 h + {0..3, 8..11}
+    sum += ts;
+    auto v_frag = [&](int u, int i) __attribute__((always_inline)) {
+      const int e = 32 * i + n;
+      return *reinterpret_cast<const u32x4_t*>(&x.v[e * T::VS + ((2 * u + h) ^ ((e >> 4) & 7)) * 8]);
+    };
+    if (QT == kQtE4m3 && nan_rows) {
+      // a NaN counts for the columns that see its row alone: it leaves the products, and the columns that
+      // see one are marked by a product of indicators
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int j = 0; j < 16; j += 2) {
-        const float w0 = __builtin_amdgcn_exp2f(fmaf(s[kt][j], c, -mu));
-        const float w1 = __builtin_amdgcn_exp2f(fmaf(s[kt][j + 1], c, -mu));
-        sum += w0;
-        sum += w1;
-        pf[2 * kt + (j >> 3)][(j & 7) >> 1] = pack_bf16(w0, w1);
-      }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int i = 0; i < ND; ++i) {
-        const int e = 32 * i + n;
-        u32x4_t vf = *reinterpret_cast<const u32x4_t*>(&x.v[e * T::VS + ((2 * u + h) ^ ((e >> 4) & 7)) * 8]);
-        if (QT == kQtE4m3 && nan_rows) {
-          // a NaN counts for the columns that see its row alone: it leaves the products, and the columns
-          // that see one are marked by a product of indicators
-          u32x4_t nf, seen;
+        for (int i = 0; i < ND; ++i) {
+          u32x4_t vf = v_frag(u, i), nf, seen;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             nf[w] = ((vf[w] & 0x7FFFu) > 0x7F80u ? 0x3F80u : 0u) | ((vf[w] & 0x7FFF0000u) > 0x7F800000u ? 0x3F800000u : 0u);
@@ -289,9 +304,14 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             if (hit[j] > 0.f) acc[i][j] = NAN;
+          acc[i] = mfma32(vf, pf[u], acc[i]);
         }
-        acc[i] = mfma32(vf, pf[u], acc[i]);
-      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < ND; ++i) acc[i] = mfma32(v_frag(u, i), pf[u], acc[i]);
+    }
   };
 
   if (n_tiles > 0) {
@@ -330,7 +350,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
   } else {
     float* pt = a.part + (row * a.n_split + split) * (D + 2);
     if (h == 0) {
-      pt[0] = m;
+      pt[0] = mu > -kLowest ? mu : -INFINITY;
       pt[1] = sum;
     }
 #pragma unroll

@@ -11,9 +11,9 @@ Attention.  The kernels multiply exact codes with exact (or split) operands and 
   - sums of n terms of one sign, n 2^-24 (weights) and n 2^-24 of sum w |v| (output).
 The error is at most the sum of these times sum w |v|, and for bf16 outputs half a step, 2^-8 |o|.
 Below the normal numbers it is absolute: a weight (and each of its terms, at most three, and its product with the
-block's scale) under 2^-126 may become 0.  The kernels' weights are 2^(t - m - 8) with t - m <= 8, the
-largest at least 2^-8, so their sum is at least 2^-8 and a row's share of the output errs by at most
-4 2^-126 / 2^-8 (|v| + 448), 448 being the largest code: rows 2^-116 (max |v| + 448) in all.
+block's scale) under 2^-126 may become 0.  The kernels' weights are 2^(t - m - o) with t - m <= o, o = 8 or
+24 octaves, the largest at least 2^-24, so their sum is at least 2^-24 and a row's share of the output errs
+by at most 4 2^-126 / 2^-24 (|v| + 448), 448 being the largest code: rows 2^-100 (max |v| + 448) in all.
 """
 import numpy as np
 import pytest
@@ -390,7 +390,7 @@ def _check(pc, q, scale, n_q, out, where, max_q=None):
             ref, mag, qk = paged.attention(qh[at:at + n], k, v, has, scale, int(L))
             rel = 2 * (d + 4) * eps * qk + (2 * rows + 8) * eps + weight
             bound = rel * mag + (2.0 ** -8 * np.abs(ref) if dtype == "bf16" else eps * np.abs(ref))
-            bound = bound + rows * 2.0 ** -116 * ((np.nanmax(np.abs(v)) if rows else 0.0) + 448)
+            bound = bound + rows * 2.0 ** -100 * ((np.nanmax(np.abs(v)) if rows else 0.0) + 448)
             got = oh[at:at + n]
             assert np.array_equal(np.isnan(got), np.isnan(ref)), f"{where} p={p}: NaN in other places"
             err = np.abs(np.nan_to_num(got) - np.nan_to_num(ref)) - np.nan_to_num(bound)
