@@ -49,7 +49,8 @@ __device__ __forceinline__ float half_sum(float v) {
 
 // A tile in LDS: K rows of D + 8 elements (so that eight rows' 16-byte reads fall on all banks), V^T rows of
 // 64 + 8.  The 16 bytes (u, h) of V^T's row hold rows 16 u + 4 h + {0..3, 8..11} of the tile, and lie at place
-// (2 u + h) ^ (element / 16 % 8): the transposing writes of eight times four elements then share no bank.
+// (2 u + h) ^ (element / 32 % 4): the transposing writes of 32 times four elements then spread over the banks
+// too.
 template <int D> struct Tile {
   static constexpr int KS = D + 8, VS = kTile + 8;
   uint16_t k[kTile * KS];
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       const int task = tid + i * NTHREADS;
       if (VTASKS % NTHREADS != 0 && task >= VTASKS) break;
       const int quad = task / (D / 4), e = task % (D / 4) * 4;
-      const int place = ((2 * (quad >> 2) + (quad & 1)) ^ ((e >> 4) & 7)) * 8 + ((quad >> 1) & 1) * 4;
+      const int place = ((2 * (quad >> 2) + (quad & 1)) ^ ((e >> 5) & 3)) * 8 + ((quad >> 1) & 1) * 4;
       u32x2_t b[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -220,14 +221,27 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
   auto compute = [&](int t) __attribute__((always_inline)) {
     const T& x = tiles[t & 1];
     const int rb = r0 + t * kTile;
+    // Operands are read from LDS NS products ahead: the order below is kept as it stands.
+    auto k_frag = [&](int kt, int d) __attribute__((always_inline)) {
+      return *reinterpret_cast<const u32x4_t*>(&x.k[(32 * kt + n) * T::KS + 16 * d + 8 * h]);
+    };
+    auto v_frag = [&](int q) __attribute__((always_inline)) {  // of product q = ND u + i
+      const int u = q / ND, i = q % ND;
+      return *reinterpret_cast<const u32x4_t*>(&x.v[(32 * i + n) * T::VS + ((2 * u + h) ^ (i & 3)) * 8]);
+    };
     f32x16v s[2];
+    u32x4_t f[NS];
+#pragma unroll
+    for (int d = 0; d < NS; ++d) f[d] = k_frag(0, d);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       s[kt] = 0.f;
 #pragma unroll
       for (int d = 0; d < NS; ++d) {
-        const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(&x.k[(32 * kt + n) * T::KS + 16 * d + 8 * h]);
-        s[kt] = mfma32(kf, qf[d], s[kt]);
+        s[kt] = mfma32(f[d], qf[d], s[kt]);
+        f[d] = kt == 0 ? k_frag(1, d) : v_frag(d);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     bool nan_rows = false;
@@ -279,10 +293,6 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       ts = weigh();
     }
     sum += ts;
-    auto v_frag = [&](int u, int i) __attribute__((always_inline)) {
-      const int e = 32 * i + n;
-      return *reinterpret_cast<const u32x4_t*>(&x.v[e * T::VS + ((2 * u + h) ^ ((e >> 4) & 7)) * 8]);
-    };
     if (QT == kQtE4m3 && nan_rows) {
       // a NaN counts for the columns that see its row alone: it leaves the products, and the columns that
       // see one are marked by a product of indicators
@@ -290,7 +300,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
-          u32x4_t vf = v_frag(u, i), nf, seen;
+          u32x4_t vf = v_frag(ND * u + i), nf, seen;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             nf[w] = ((vf[w] & 0x7FFFu) > 0x7F80u ? 0x3F80u : 0u) | ((vf[w] & 0x7FFF0000u) > 0x7F800000u ? 0x3F800000u : 0u);
@@ -307,10 +317,13 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
           acc[i] = mfma32(vf, pf[u], acc[i]);
         }
     } else {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int i = 0; i < ND; ++i) acc[i] = mfma32(v_frag(u, i), pf[u], acc[i]);
+      for (int q = 0; q < 4 * ND; ++q) {
+        acc[q % ND] = mfma32(f[q % NS], pf[q / ND], acc[q % ND]);
+        if (q + NS < 4 * ND) f[q % NS] = v_frag(q + NS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
 
