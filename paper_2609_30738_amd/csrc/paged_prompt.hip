@@ -47,17 +47,23 @@ __device__ __forceinline__ float half_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A tile in LDS: K rows of D + 8 elements (so that eight rows' 16-byte reads fall on all banks), V^T rows of
-// 64 + 8.  The 16 bytes (u, h) of V^T's row hold rows 16 u + 4 h + {0..3, 8..11} of the tile, and lie at place
-// (2 u + h) ^ (element / 32 % 4): the transposing writes of 32 times four elements then spread over the banks
-// too.
+// A tile in LDS, rows as in the cache: K rows are D + 8 elements apart, so that the 16-byte reads of eight rows
+// fall on all banks, V rows D + 32, so that the transposing reads of 64 bytes of four rows do.
 template <int D> struct Tile {
-  static constexpr int KS = D + 8, VS = kTile + 8;
+  static constexpr int KS = D + 8, VS = D + 32;
   uint16_t k[kTile * KS];
-  uint16_t v[D * VS];
+  uint16_t v[kTile * VS];
   int32_t has[kTile / 16];  // whether the 16 rows have a block
   int32_t nan[8];           // whether a wave found a NaN in V
 };
+
+typedef short __attribute__((ext_vector_type(4))) s16x4_t;
+
+// Of the 4 x 16 elements whose row j the lanes 4 j .. 4 j + 3 of a group of 16 point into, four each: column l % 16.
+__device__ __forceinline__ u32x2_t read_transposed(const uint16_t* p) {
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) s16x4_t*)p));
+}
 
 }  // namespace
 
@@ -65,9 +71,6 @@ template <int QT, int D, int W>
 __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a, int n_groups) {
   constexpr int NS = D / 16;  // matrix steps over the head dimension
   constexpr int ND = D / 32;  // 32-wide tiles of the output
-  constexpr int NTHREADS = 64 * W;
-  constexpr int KTASKS = kTile * (D / 16), VTASKS = (kTile / 4) * (D / 4);
-  constexpr int KT = (KTASKS + NTHREADS - 1) / NTHREADS, VT = (VTASKS + NTHREADS - 1) / NTHREADS;
   using T = Tile<D>;
   extern __shared__ __align__(16) char lds[];
   T* const tiles = reinterpret_cast<T*>(lds);
@@ -81,7 +84,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, h = lane >> 5;
   const int shift = a.pc.shift, R = 1 << shift;
   const int r0 = split * a.split_rows;
-  const int vis_max = sp.visible((col0 + n_cols - 1) / G);
+  const int vis_max = sp.visible((col0 + n_cols - 1) / G), vis_min = sp.visible(col0 / G);
   const int r1 = min(vis_max, r0 + a.split_rows);
   if (r0 >= r1 && a.n_split > 1) return;
   const int n_tiles = r1 > r0 ? (r1 - r0 + kTile - 1) / kTile : 0;
@@ -108,103 +111,66 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
     }
   }
 
-  // staging: K in 16-byte pieces of a row, V in four rows by four elements
-  int32_t kid[KT], vid[VT];
-  u32x4_t kc[KT];
-  uint32_t vc[VT][4];
-  float ksc[KT], vsc[VT];
-  bool khas[KT];  // of kc (kid is a tile ahead of it by then)
+  // Staging: a wave takes the rows of 1 KB of K and of V, 16 bytes a lane.  They lie in one 16-row group, so
+  // block, scale and address are the wave's.
+  constexpr int ROWS = 1024 / D, NTASK = kTile / (ROWS * W) > 0 ? kTile / (ROWS * W) : 1;
+  static_assert(ROWS <= 16, "a task lies in one block");
+  const int wv = __builtin_amdgcn_readfirstlane(wave), lane_row = lane / (D / 16), lane_e = lane % (D / 16) * 16;
+  int32_t id[NTASK];  // table entries of the tile after the codes'
+  u32x4_t kc[NTASK], vc[NTASK];
+  float ksc[NTASK], vsc[NTASK];
+  bool has[NTASK];
   const int32_t* table = a.pc.table + (int64_t)p * a.pc.table_stride;
-  auto k_row = [&](int i) { return (tid + i * NTHREADS) / (D / 16); };
-  auto v_row = [&](int i) { return (tid + i * NTHREADS) / (D / 4) * 4; };
+  auto task_row = [&](int i) { return (wv + i * W) * ROWS; };
   auto ids = [&](int t) __attribute__((always_inline)) {
-    const int rb = r0 + t * kTile;
 #pragma unroll
-    for (int i = 0; i < KT; ++i) {
-      const int r = rb + k_row(i);
-      kid[i] = r < r1 ? table[r >> shift] : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < VT; ++i) {
-      const int r = rb + v_row(i);
-      vid[i] = r < r1 ? table[r >> shift] : -1;
+    for (int i = 0; i < NTASK; ++i) {
+      const int r = r0 + t * kTile + task_row(i);
+      id[i] = task_row(i) < kTile && r < r1 ? table[r >> shift] : -1;
     }
   };
   auto codes = [&](int t) __attribute__((always_inline)) {
-    const int rb = r0 + t * kTile;
 #pragma unroll
-    for (int i = 0; i < KT; ++i) {
-      if (KTASKS % NTHREADS != 0 && tid + i * NTHREADS >= KTASKS) break;
-      khas[i] = (uint32_t)kid[i] < (uint32_t)a.pc.n_blocks;
-      const int64_t unit = (int64_t)(khas[i] ? kid[i] : 0) * a.pc.h_kv + g;
-      const int r = (rb + k_row(i)) & (R - 1);
-      kc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.k + ((unit << shift) + r) * D + (tid + i * NTHREADS) % (D / 16) * 16);
+    for (int i = 0; i < NTASK; ++i) {
+      if (task_row(i) >= kTile) break;
+      has[i] = (uint32_t)id[i] < (uint32_t)a.pc.n_blocks;
+      const int64_t unit = (int64_t)(has[i] ? id[i] : 0) * a.pc.h_kv + g;
+      const int64_t at = ((unit << shift) + ((r0 + t * kTile + task_row(i)) & (R - 1))) * D;
+      kc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.k + at + 16 * (uint32_t)lane);
+      vc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.v + at + 16 * (uint32_t)lane);
       ksc[i] = a.pc.k_scale[unit];
-      if (!khas[i]) {
-        kc[i] = u32x4_t{0u, 0u, 0u, 0u};
-        ksc[i] = 1.f;
-      }
+      vsc[i] = has[i] ? a.pc.v_scale[unit] : 1.f;
     }
+  };
+  auto put = [&](uint16_t* to, const u32x4_t& c, float scale) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < VT; ++i) {
-      if (VTASKS % NTHREADS != 0 && tid + i * NTHREADS >= VTASKS) break;
-      const bool has = (uint32_t)vid[i] < (uint32_t)a.pc.n_blocks;
-      const int64_t unit = (int64_t)(has ? vid[i] : 0) * a.pc.h_kv + g;
-      const int r = (rb + v_row(i)) & (R - 1);
-      const uint8_t* src = a.pc.v + ((unit << shift) + r) * D + (tid + i * NTHREADS) % (D / 4) * 4;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) vc[i][j] = *reinterpret_cast<const uint32_t*>(src + j * D);
-      vsc[i] = a.pc.v_scale[unit];
-      if (!has) vsc[i] = 1.f;
-      // a row that no column sees holds anything: zero its values, so that 0 times them is 0
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (!has || rb + v_row(i) + j >= r1) vc[i][j] = 0u;
+    for (int w = 0; w < 2; ++w) {
+      const u32x2_t y = decode4_bf16<QT>(c[2 * w], scale), z = decode4_bf16<QT>(c[2 * w + 1], scale);
+      *reinterpret_cast<u32x4_t*>(to + 8 * w) = u32x4_t{y[0], y[1], z[0], z[1]};
     }
   };
   auto stage = [&](int t) __attribute__((always_inline)) {
     T& x = tiles[t & 1];
-#pragma unroll
-    for (int i = 0; i < KT; ++i) {
-      const int task = tid + i * NTHREADS;
-      if (KTASKS % NTHREADS != 0 && task >= KTASKS) break;
-      const int r = task / (D / 16), e = task % (D / 16) * 16;
-      u32x4_t lo, hi;
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const u32x2_t y = decode4_bf16<QT>(kc[i][w], ksc[i]), z = decode4_bf16<QT>(kc[i][2 + w], ksc[i]);
-        lo[2 * w] = y[0];
-        lo[2 * w + 1] = y[1];
-        hi[2 * w] = z[0];
-        hi[2 * w + 1] = z[1];
-      }
-      *reinterpret_cast<u32x4_t*>(&x.k[r * T::KS + e]) = lo;
-      *reinterpret_cast<u32x4_t*>(&x.k[r * T::KS + e + 8]) = hi;
-      if (e == 0 && r % 16 == 0) x.has[r / 16] = khas[i];
-    }
+    const int rb = r0 + t * kTile;
     bool nan = false;
 #pragma unroll
-    for (int i = 0; i < VT; ++i) {
-      const int task = tid + i * NTHREADS;
-      if (VTASKS % NTHREADS != 0 && task >= VTASKS) break;
-      const int quad = task / (D / 4), e = task % (D / 4) * 4;
-      const int place = ((2 * (quad >> 2) + (quad & 1)) ^ ((e >> 5) & 3)) * 8 + ((quad >> 1) & 1) * 4;
-      u32x2_t b[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (QT == kQtE4m3) nan = nan || (((vc[i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
-        b[j] = decode4_bf16<QT>(vc[i][j], vsc[i]);
+    for (int i = 0; i < NTASK; ++i) {
+      if (task_row(i) >= kTile) break;
+      const int r = task_row(i) + lane_row;
+      // (a missing block's or a later row's K may be anything: its logits are masked)
+      put(&x.k[r * T::KS + lane_e], kc[i], ksc[i]);
+      if (!has[i] || rb + task_row(i) + ROWS > r1) {
+        // a row that no column sees holds anything: zero its values, so that 0 times them is 0
+        if (!has[i] || rb + r >= r1) vc[i] = u32x4_t{0u, 0u, 0u, 0u};
       }
+      if (QT == kQtE4m3 && rb + kTile > vis_min) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
-        u32x2_t y;
-        y[0] = __builtin_amdgcn_perm(b[1][j >> 1], b[0][j >> 1], sel);
-        y[1] = __builtin_amdgcn_perm(b[3][j >> 1], b[2][j >> 1], sel);
-        *reinterpret_cast<u32x2_t*>(&x.v[(e + j) * T::VS + place]) = y;
+        for (int j = 0; j < 4; ++j) nan = nan || (((vc[i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
       }
+      put(&x.v[r * T::VS + lane_e], vc[i], vsc[i]);
+      if (lane == 0 && task_row(i) % 16 == 0) x.has[task_row(i) / 16] = has[i];
     }
-    if (QT == kQtE4m3) {
+    if (QT == kQtE4m3 && rb + kTile > vis_min) {
       const uint64_t any = __ballot(nan);
       if (lane == 0) x.nan[wave] = any != 0;
     }
@@ -227,7 +193,10 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
     };
     auto v_frag = [&](int q) __attribute__((always_inline)) {  // of product q = ND u + i
       const int u = q / ND, i = q % ND;
-      return *reinterpret_cast<const u32x4_t*>(&x.v[(32 * i + n) * T::VS + ((2 * u + h) ^ (i & 3)) * 8]);
+      // rows 16 u + 4 h + {0..3, 8..11} of element 32 i + n
+      const uint16_t* p = &x.v[(16 * u + 4 * h + (lane & 15) / 4) * T::VS + 32 * i + (lane & 16) + 4 * (lane & 3)];
+      const u32x2_t y = read_transposed(p), z = read_transposed(p + 8 * T::VS);
+      return u32x4_t{y[0], y[1], z[0], z[1]};
     };
     f32x16v s[2];
     u32x4_t f[NS];
@@ -254,7 +223,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
           const int r = 32 * kt + 8 * (j >> 2) + 4 * h + (j & 3);
           if (rb + r >= vis || !x.has[2 * kt + (j >> 3)]) s[kt][j] = -INFINITY;
         }
-      if (QT == kQtE4m3) {
+      if (QT == kQtE4m3 && rb + kTile > wvis_min) {
         int any = 0;
 #pragma unroll
         for (int w = 0; w < W; ++w) any |= x.nan[w];
