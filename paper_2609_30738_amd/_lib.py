@@ -511,28 +511,32 @@ class PagedCache:
         n_blocks, h_kv, block_rows, d = k.shape
         if k.dtype not in (torch.float8_e4m3fn, torch.int8) or v.dtype != k.dtype or v.shape != k.shape:
             raise ValueError("k and v must be float8_e4m3fn or int8 tensors of one shape")
-        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or \
-                k_scale.numel() != n_blocks * h_kv or v_scale.numel() != n_blocks * h_kv:
-            raise ValueError("k_scale and v_scale must be float32 [n_blocks, h_kv]")
+        if dtype not in ("bf16", "f32"):
+            raise ValueError("dtype must be bf16 or f32")
         self._tables(table, lens, n_blocks, block_rows)
         self.dtype_name = dtype
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.rows_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         s = self.struct
         s.dtype = KV_BF16 if dtype == "bf16" else KV_F32
         s.qtype = KV_E4M3 if k.dtype == torch.float8_e4m3fn else KV_INT8
-        s.h_q, s.h_kv, s.d = int(h_q), h_kv, d
+        s.h_q, s.h_kv, s.d = self.h_q, self.h_kv, self.d = int(h_q), h_kv, d
         s.max_len = min(table.shape[1] * block_rows, 1 << 24) if max_len is None else int(max_len)
-        s.k, s.v = _ptr(k).value, _ptr(v).value
-        s.k_scale, s.v_scale = _ptr(k_scale).value, _ptr(v_scale).value
+        s.k, s.v = self._arg(k, k.dtype, 0, "k"), self._arg(v, k.dtype, 0, "v")
+        s.k_scale = self._arg(k_scale, torch.float32, n_blocks * h_kv, "k_scale")
+        s.v_scale = self._arg(v_scale, torch.float32, n_blocks * h_kv, "v_scale")
 
     def _tables(self, table, lens, n_blocks, block_rows):
-        _int32(table, "table")
-        _int32(lens, "lens")
+        import torch
         if table.dim() != 2 or lens.numel() != table.shape[0]:
             raise ValueError("table must be [n_prob, table_stride] and lens [n_prob]")
-        self.table, self.lens = table, lens
-        self.struct = KvPagedCache(n_prob=table.shape[0], block_rows=int(block_rows), n_blocks=int(n_blocks),
-                                   table_stride=table.shape[1], table=_ptr(table).value, len=_ptr(lens).value)
+        self.table, self.lens, self.device = table, lens, table.device
+        self._int32, self._torch_c = torch.int32, torch._C
+        self.n_prob = table.shape[0]
+        self.struct = KvPagedCache(n_prob=self.n_prob, block_rows=int(block_rows), n_blocks=int(n_blocks),
+                                   table_stride=table.shape[1], table=self._arg(table, torch.int32, 0, "table"),
+                                   len=self._arg(lens, torch.int32, 0, "lens"))
+        self._ref = ctypes.byref(self.struct)
 
     @classmethod
     def for_tables(cls, block_rows: int, n_blocks: int, table, lens) -> "PagedCache":
@@ -554,29 +558,35 @@ class PagedCache:
                    torch.full((n_prob, table_stride), -1, dtype=torch.int32, device=dev),
                    torch.zeros(n_prob, dtype=torch.int32, device=dev), max_len)
 
-    @property
-    def n_prob(self) -> int:
-        return self.struct.n_prob
-
     def ref(self):
-        return ctypes.byref(self.struct)
+        return self._ref
 
+    def _arg(self, t, dtype, n: int, name: str):
+        """Address of a contiguous tensor of at least n elements on the cache's device (None: NULL)."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or not t.is_cuda or t.device != self.device or not t.is_contiguous() or t.numel() < n:
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of at least {n} elements on {self.device}")
+        return t.data_ptr()
 
-def _int32(t, name: str):
-    import torch
-    if t is not None and t.dtype != torch.int32:
-        raise ValueError(f"{name} must be an int32 tensor")
+    def _rows(self, t, heads: int, name: str):
+        """Address and token stride of [tokens, heads, d] rows; tokens may lie apart (slices of a projection)."""
+        d = self.d
+        shape = t.shape
+        if t.dtype is not self.rows_dtype or t.device != self.device or len(shape) != 3 or shape[1] != heads or shape[2] != d:
+            raise ValueError(f"{name} must be a {self.rows_dtype} tensor [tokens, {heads}, {d}] on {self.device}")
+        st = t.stride()
+        if st[2] != 1 or (st[1] != d and heads > 1):
+            raise ValueError(f"the heads of a token must be contiguous in {name}")
+        return t.data_ptr(), (st[0] if shape[0] > 1 else heads * d)
 
-
-def _token_rows(pc: PagedCache, t, heads: int, name: str):
-    """Address and token stride of [n, heads, d] rows; tokens may lie apart (a slice of a projection)."""
-    import torch
-    want = torch.bfloat16 if pc.struct.dtype == KV_BF16 else torch.float32
-    if not t.is_cuda or t.dtype != want or t.dim() != 3 or t.shape[1:] != (heads, pc.struct.d):
-        raise ValueError(f"{name} must be a device tensor [tokens, {heads}, {pc.struct.d}] of {want}")
-    if (t.stride(2) != 1 or t.stride(1) != pc.struct.d) and t.numel() > 0:
-        raise ValueError(f"the heads of a token must be contiguous in {name}")
-    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else heads * pc.struct.d)
+    def _stream(self, stream):
+        """The stream to launch on: kernels go to the current device, which has to be the cache's."""
+        index = self.device.index
+        if index != self._torch_c._cuda_getDevice():
+            raise ValueError(f"the cache is on {self.device}, which is not the current device")
+        # (torch.cuda.current_stream() makes an object of it: 3 us of a call of 9)
+        return self._torch_c._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
 
 def paged_tables(pc: PagedCache, len_in, add, free_blocks, taken_in, taken_out, tok_off, blk_off, slots,
@@ -584,30 +594,28 @@ def paged_tables(pc: PagedCache, len_in, add, free_blocks, taken_in, taken_out, 
     """kv_paged_tables: writes pc.table, pc.lens, tok_off, blk_off [n_prob + 1], slots and taken_out.
     len_in None: empty caches; add None: one row each; free_blocks None: n_free blocks 0, 1, 2, ..
     (default: the pool's)."""
-    for t, name, n in ((len_in, "len_in", pc.n_prob), (add, "add", pc.n_prob), (tok_off, "tok_off", pc.n_prob + 1),
-                       (blk_off, "blk_off", pc.n_prob + 1), (taken_in, "taken_in", 1),
-                       (taken_out, "taken_out", 1), (free_blocks, "free_blocks", 0), (slots, "slots", 0)):
-        _int32(t, name)
-        if t is not None and t.numel() < n:
-            raise ValueError(f"{name} must have {n} elements")
+    n, i32, arg = pc.n_prob, pc._int32, pc._arg
     if free_blocks is not None:
         n_free = free_blocks.numel() if n_free is None else min(int(n_free), free_blocks.numel())
     elif n_free is None:
         n_free = pc.struct.n_blocks
-    _check(lib().kv_paged_tables(pc.ref(), _ptr(len_in), _ptr(add), _ptr(free_blocks), int(n_free),
-                                 _ptr(taken_in), _ptr(taken_out), _ptr(tok_off), _ptr(blk_off), _ptr(slots),
-                                 0 if slots is None else slots.numel(), _stream(stream)), "kv_paged_tables")
+    _check(lib().kv_paged_tables(pc._ref, arg(len_in, i32, n, "len_in"), arg(add, i32, n, "add"),
+                                 arg(free_blocks, i32, 0, "free_blocks"), int(n_free),
+                                 arg(taken_in, i32, 1, "taken_in"), arg(taken_out, i32, 1, "taken_out"),
+                                 arg(tok_off, i32, n + 1, "tok_off"), arg(blk_off, i32, n + 1, "blk_off"),
+                                 arg(slots, i32, 0, "slots"), 0 if slots is None else slots.numel(),
+                                 pc._stream(stream)), "kv_paged_tables")
 
 
 def paged_append(pc: PagedCache, k_new, v_new, slots, stream=None) -> None:
     """kv_paged_append: k_new, v_new [tokens, h_kv, d], tokens of one stride (slices of a projection's
     output, for instance); slots [tokens] int32."""
-    kp, ks = _token_rows(pc, k_new, pc.struct.h_kv, "k_new")
-    vp, vs = _token_rows(pc, v_new, pc.struct.h_kv, "v_new")
-    _int32(slots, "slots")
-    if k_new.shape != v_new.shape or ks != vs or slots.numel() < k_new.shape[0]:
-        raise ValueError("k_new and v_new must have one shape and token stride, slots an entry per token")
-    _check(lib().kv_paged_append(pc.ref(), kp, vp, ks, _ptr(slots), k_new.shape[0], _stream(stream)),
+    kp, ks = pc._rows(k_new, pc.h_kv, "k_new")
+    vp, vs = pc._rows(v_new, pc.h_kv, "v_new")
+    n = k_new.shape[0]
+    if v_new.shape[0] != n or ks != vs:
+        raise ValueError("k_new and v_new must have one shape and token stride")
+    _check(lib().kv_paged_append(pc._ref, kp, vp, ks, pc._arg(slots, pc._int32, n, "slots"), n, pc._stream(stream)),
            "kv_paged_append")
 
 
@@ -615,28 +623,30 @@ def paged_compact(batch: Batch, k, v, sel_idx, budget: int, keep_tail: int, pc: 
                   budgets: Optional[Budgets] = None, stream=None) -> None:
     """kv_paged_compact: the selected rows of k and v and the tail into pc's blocks."""
     bh, bd = budgets.pointers() if budgets is not None else (None, None)
-    _check(lib().kv_paged_compact(batch.ref(), _ptr(k), _ptr(v), _ptr(sel_idx), int(budget), int(keep_tail),
-                                  bh, bd, pc.ref(), _stream(stream)), "kv_paged_compact")
+    n = batch.total_tokens * batch.h_kv * batch.d
+    _check(lib().kv_paged_compact(batch.ref(), pc._arg(k, pc.rows_dtype, n, "k"), pc._arg(v, pc.rows_dtype, n, "v"),
+                                  pc._arg(sel_idx, pc._int32, batch.n_prob * batch.h_kv * int(budget), "sel_idx"),
+                                  int(budget), int(keep_tail), bh, bd, pc._ref, pc._stream(stream)),
+           "kv_paged_compact")
 
 
 def paged_attention_workspace_bytes(pc: PagedCache, n_tok: Optional[int] = None, max_q: int = 1) -> int:
     n_tok = pc.n_prob if n_tok is None else n_tok
-    return int(lib().kv_paged_attention_workspace_bytes(pc.ref(), int(n_tok), int(max_q)))
+    return int(lib().kv_paged_attention_workspace_bytes(pc._ref, int(n_tok), int(max_q)))
 
 
 def paged_attention(pc: PagedCache, q, scale: float, out, tok_off=None, max_q: int = 1, ws=None,
                     stream=None) -> None:
     """kv_paged_attention: q [tokens, h_q, d] (tokens of one stride), out the same shape, contiguous;
     tok_off [n_prob + 1] int32 for several tokens to a problem, at most max_q each."""
-    qp, qs = _token_rows(pc, q, pc.struct.h_q, "q")
-    _int32(tok_off, "tok_off")
-    if out.dtype != q.dtype or out.shape != q.shape:
-        raise ValueError("out must have the shape and type of q")
-    if tok_off is not None and tok_off.numel() < pc.n_prob + 1:
-        raise ValueError("tok_off must have n_prob + 1 elements")
-    _check(lib().kv_paged_attention(pc.ref(), qp, qs, _ptr(tok_off), q.shape[0], int(max_q), float(scale),
-                                    _ptr(out), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                    _stream(stream)), "kv_paged_attention")
+    qp, qs = pc._rows(q, pc.h_q, "q")
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    _check(lib().kv_paged_attention(pc._ref, qp, qs, pc._arg(tok_off, pc._int32, pc.n_prob + 1, "tok_off"),
+                                    q.shape[0], max_q, scale, pc._arg(out, pc.rows_dtype, 0, "out"),
+                                    None if ws is None else pc._arg(ws, ws.dtype, 0, "ws"),
+                                    0 if ws is None else ws.numel() * ws.element_size(), pc._stream(stream)),
+           "kv_paged_attention")
 
 
 def pyramid_budgets(budget: int, n_layers: int, beta: float) -> np.ndarray:

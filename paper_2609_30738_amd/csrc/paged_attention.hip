@@ -516,7 +516,7 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
     if (rows > 512) n = std::max<int64_t>(1, std::min(2 * kRound / units, (rows + kMinSplit - 1) / kMinSplit));
   }
   int64_t split = ((rows + n - 1) / n + 127) / 128 * 128;
-  if (!plan.prompt_waves) split = std::min<int64_t>(split, kMaxSplitRows);
+  split = std::min<int64_t>(split, plan.prompt_waves ? (int64_t)prompt_split_blocks(plan.prompt_waves) << pc.shift : kMaxSplitRows);
   plan.split_rows = (int)split;
   plan.n_split = (int)((rows + split - 1) / split);
   return plan;

@@ -56,6 +56,12 @@ template <int D> struct Tile {
   int32_t has[kTile / 16];  // whether the 16 rows have a block
   int32_t nan[8];           // whether a wave found a NaN in V
 };
+// Behind the two tiles: the split's blocks and their scales.
+template <int W> struct Blocks {
+  static constexpr int N = prompt_split_blocks(W);
+  int32_t id[N];  // -1: missing
+  float k_scale[N], v_scale[N];
+};
 
 typedef short __attribute__((ext_vector_type(4))) s16x4_t;
 
@@ -74,6 +80,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
   using T = Tile<D>;
   extern __shared__ __align__(16) char lds[];
   T* const tiles = reinterpret_cast<T*>(lds);
+  Blocks<W>& blocks = *reinterpret_cast<Blocks<W>*>(lds + 2 * sizeof(T));
 
   const int g = blockIdx.x, split = blockIdx.y % a.n_split, cg = n_groups - 1 - blockIdx.y / a.n_split;
   const int p = blockIdx.z, G = a.pc.h_q / a.pc.h_kv;
@@ -112,34 +119,50 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
   }
 
   // Staging: a wave takes the rows of 1 KB of K and of V, 16 bytes a lane.  They lie in one 16-row group, so
-  // block, scale and address are the wave's.
+  // block, scale and address are the wave's.  Blocks and scales come from LDS: scalar loads return out of order
+  // with the reads of the products' operands, which then have to be waited for all at once (177 us of 1900).
   constexpr int ROWS = 1024 / D, NTASK = kTile / (ROWS * W) > 0 ? kTile / (ROWS * W) : 1;
   static_assert(ROWS <= 16, "a task lies in one block");
   const int wv = __builtin_amdgcn_readfirstlane(wave), lane_row = lane / (D / 16), lane_e = lane % (D / 16) * 16;
-  int32_t id[NTASK];  // table entries of the tile after the codes'
+  int32_t id[NTASK];  // the block of the tile after the codes', and its scales
+  float next_ks[NTASK], next_vs[NTASK];
   u32x4_t kc[NTASK], vc[NTASK];
   float ksc[NTASK], vsc[NTASK];
   bool has[NTASK];
-  const int32_t* table = a.pc.table + (int64_t)p * a.pc.table_stride;
+  for (int i = tid; i << shift < r1 - r0; i += 64 * W) {
+    int block = a.pc.table[(int64_t)p * a.pc.table_stride + (r0 >> shift) + i];
+    if ((uint32_t)block >= (uint32_t)a.pc.n_blocks) block = -1;
+    const int64_t unit = (int64_t)max(block, 0) * a.pc.h_kv + g;
+    blocks.id[i] = block;
+    blocks.k_scale[i] = a.pc.k_scale[unit];
+    blocks.v_scale[i] = block < 0 ? 1.f : a.pc.v_scale[unit];
+  }
+  __syncthreads();
   auto task_row = [&](int i) { return (wv + i * W) * ROWS; };
   auto ids = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NTASK; ++i) {
-      const int r = r0 + t * kTile + task_row(i);
-      id[i] = task_row(i) < kTile && r < r1 ? table[r >> shift] : -1;
+      if (task_row(i) >= kTile) break;
+      const int r = t * kTile + task_row(i);
+      const int at = min(r, r1 - r0 - 1) >> shift;
+      id[i] = blocks.id[at];
+      next_ks[i] = blocks.k_scale[at];
+      next_vs[i] = blocks.v_scale[at];
+      if (r0 + r >= r1) id[i] = -1;
     }
   };
   auto codes = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < NTASK; ++i) {
       if (task_row(i) >= kTile) break;
-      has[i] = (uint32_t)id[i] < (uint32_t)a.pc.n_blocks;
-      const int64_t unit = (int64_t)(has[i] ? id[i] : 0) * a.pc.h_kv + g;
+      const int block = __builtin_amdgcn_readfirstlane(id[i]);
+      has[i] = block >= 0;
+      const int64_t unit = (int64_t)max(block, 0) * a.pc.h_kv + g;
       const int64_t at = ((unit << shift) + ((r0 + t * kTile + task_row(i)) & (R - 1))) * D;
       kc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.k + at + 16 * (uint32_t)lane);
       vc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.v + at + 16 * (uint32_t)lane);
-      ksc[i] = a.pc.k_scale[unit];
-      vsc[i] = has[i] ? a.pc.v_scale[unit] : 1.f;
+      ksc[i] = next_ks[i];
+      vsc[i] = next_vs[i];
     }
   };
   auto put = [&](uint16_t* to, const u32x4_t& c, float scale) __attribute__((always_inline)) {
@@ -157,6 +180,11 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
     for (int i = 0; i < NTASK; ++i) {
       if (task_row(i) >= kTile) break;
       const int r = task_row(i) + lane_row;
+      if constexpr (QT == kQtInt8) {
+        // (an int8 code takes a register once converted: not where it was loaded, a tile before)
+        asm volatile("" : "+v"(kc[i][0]), "+v"(kc[i][1]), "+v"(kc[i][2]), "+v"(kc[i][3]));
+        asm volatile("" : "+v"(vc[i][0]), "+v"(vc[i][1]), "+v"(vc[i][2]), "+v"(vc[i][3]));
+      }
       // (a missing block's or a later row's K may be anything: its logits are masked)
       put(&x.k[r * T::KS + lane_e], kc[i], ksc[i]);
       if (!has[i] || rb + task_row(i) + ROWS > r1) {
@@ -348,7 +376,7 @@ namespace {
 template <int QT, int D, int W> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
   const int groups = (a.max_q * a.pc.group() + 32 * W - 1) / (32 * W);
   const dim3 grid((unsigned)a.pc.h_kv, (unsigned)(groups * a.n_split), (unsigned)a.pc.n_prob);
-  constexpr int lds = 2 * (int)sizeof(Tile<D>);
+  constexpr int lds = 2 * (int)sizeof(Tile<D>) + (int)sizeof(Blocks<W>);
   auto kernel = paged_prompt_kernel<QT, D, W>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
