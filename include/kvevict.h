@@ -451,7 +451,7 @@ int kv_paged_tables(const kv_paged_cache* pc, const int32_t* len_in, const int32
                     int32_t n_slots, void* stream);
 
 /* New rows into the blocks: token t's row of head g, k_new / v_new + t * tok_stride + g * d elements
- * (tok_stride 0: h_kv * d; at least that, and whole 16-byte chunks), into slot slots[t] (as
+ * (tok_stride 0: h_kv * d; at least that, at most 2^26, and whole 16-byte chunks), into slot slots[t] (as
  * kv_paged_tables gives them; one outside [0, n_blocks * block_rows) is skipped).  Tokens of one block have to be
  * consecutive in the batch, in consecutive slots, the first behind the block's rows in use; each block
  * once in a call.  A block's first row sets its scale; where later rows need a larger scale, the codes
@@ -478,8 +478,8 @@ size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_to
  * one token each, then n_tok = n_prob and max_q = 1).  Token j of problem p sees the rows
  * r <= len[p] - n_p + j:
  *   out[t,h,:] = sum_r softmax_r(scale <q[t,h], k[r]>) v[r],  kv head h / (h_q / h_kv);
- * 0 where it sees none.  q: token t at t * q_stride elements (0: h_q * d; at least that, whole 16-byte
- * chunks), [h_q][d]; out [n_tok][h_q][d] of the queries' type.  Logits, softmax and sums in fp32; the weights enter
+ * 0 where it sees none.  q: token t at t * q_stride elements (0: h_q * d; at least that, at most 2^26, whole
+ * 16-byte chunks), [h_q][d]; out [n_tok][h_q][d] of the queries' type.  Logits, softmax and sums in fp32; the weights enter
  * the product with V with 24 significant bits (fp32 queries), 16 (bf16 and max_q h_q / h_kv <= 16) or as
  * bf16 (more).  The outputs of
  * tokens outside every problem (a padded batch) stay as they were, and so do a problem's whose tok_off reaches outside

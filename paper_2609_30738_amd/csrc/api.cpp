@@ -21,6 +21,7 @@ constexpr int kMaxCompactBudget = 8192;
 constexpr float kLog2eF = 1.4426950408889634f;  // log2(e): kernels take logits in base 2
 constexpr int kMaxPool = 63;  // widest max-pool window of kv_mmr_select_ex
 constexpr size_t kWsAlign = 256;
+constexpr int64_t kMaxTokenStride = (int64_t)1 << 26;
 
 size_t align_up(size_t x) { return (x + kWsAlign - 1) & ~(kWsAlign - 1); }
 
@@ -828,11 +829,12 @@ int check_paged(const kv_paged_cache* c, kv::Paged* pc, bool tables = false) {
   return KV_OK;
 }
 
-// Elements between two tokens' rows of `heads` heads: 0 is packed; whole 16-byte chunks.
+// Elements between two tokens' rows of `heads` heads: 0 is packed; whole 16-byte chunks, and at most kMaxTokenStride
+// (the kernels' offsets within a few tokens are 32-bit).
 int check_stride(const kv::Paged& pc, int heads, int64_t* stride) {
   const int64_t packed = (int64_t)heads * pc.d;
   if (*stride == 0) *stride = packed;
-  if (*stride < packed || *stride % (pc.dtype == kv::kDtBf16 ? 8 : 4) != 0) return KV_ERR_ARG;
+  if (*stride < packed || *stride > kMaxTokenStride || *stride % (pc.dtype == kv::kDtBf16 ? 8 : 4) != 0) return KV_ERR_ARG;
   return KV_OK;
 }
 
@@ -855,7 +857,8 @@ int kv_paged_tables(const kv_paged_cache* c, const int32_t* len_in, const int32_
   if (st != KV_OK) return st;
   if (!tok_off || !blk_off || (!slots && n_slots > 0)) return KV_ERR_NULL;
   if (n_free < 0 || n_slots < 0) return KV_ERR_ARG;
-  const kv::TablesArgs a{len_in, add, free_blocks, n_free, taken_in, taken_out, tok_off, blk_off, slots, n_slots};
+  const kv::TablesArgs a{len_in, add, free_blocks, n_free, taken_in, taken_out, tok_off, blk_off, slots, n_slots,
+                         aligned16(slots)};
   return launch_status(kv::launch_paged_tables(pc, a, static_cast<hipStream_t>(stream)));
 }
 

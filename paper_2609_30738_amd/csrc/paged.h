@@ -39,6 +39,7 @@ struct TablesArgs {
   int32_t* blk_off;         // [n_prob + 1]
   int32_t* slots;           // [n_slots]
   int n_slots;
+  bool slots_aligned;       // 16 bytes
 };
 hipError_t launch_paged_tables(const Paged& pc, const TablesArgs& a, hipStream_t stream);
 

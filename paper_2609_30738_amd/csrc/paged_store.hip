@@ -79,18 +79,16 @@ template <int QT, int D> __device__ __forceinline__ float grown_scale(uint8_t* c
 }
 
 // store_rows for any values: read twice, infinities and NaNs apart.
-template <int DT, int QT, int D, typename Source>
-__device__ __forceinline__ void store_rows_any(uint8_t* codes, float* scale, int row0, int n, Source source) {
+template <int DT, int QT, int D, typename Load>
+__device__ __forceinline__ void store_rows_any(uint8_t* codes, float* scale, int row0, int n, Load load) {
   constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH;
   const int lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
   const float old = row0 > 0 ? *scale : 0.f;
-  const u32x4_t zero = {0u, 0u, 0u, 0u};
   uint32_t amax = 0;
 #pragma unroll 4
-  for (int i = rr; i < n; i += RPP) {
-    const u32x4_t* src = source(i);
+  for (int i = 0; i * RPP < n; ++i) {
     float f[EPT];
-    chunk_values<DT>(src ? src[c] : zero, f);
+    chunk_values<DT>(load(i), f);
 #pragma unroll
     for (int e = 0; e < EPT; ++e) {
       const uint32_t u = __float_as_uint(f[e]) & 0x7FFFFFFFu;
@@ -99,23 +97,23 @@ __device__ __forceinline__ void store_rows_any(uint8_t* codes, float* scale, int
   }
   const float s = grown_scale<QT, D>(codes, row0, old, block_scale<QT>(wave_max_u32(amax))), inv = inv_scale(s);
 #pragma unroll 4
-  for (int i = rr; i < n; i += RPP) {
-    const u32x4_t* src = source(i);
+  for (int i = 0; i * RPP < n; ++i) {
     float f[EPT];
-    chunk_values<DT>(src ? src[c] : zero, f);
-    store_chunk<QT, false>(codes + (row0 + i) * D + c * EPT, f, inv);
+    chunk_values<DT>(load(i), f);
+    if (i * RPP + rr < n) store_chunk<QT, false>(codes + (row0 + i * RPP + rr) * D + c * EPT, f, inv);
   }
   if (lane == 0) *scale = s;
 }
 
-// Rows row0 .. row0 + n - 1 of one block and head from `source` (its i-th row's 16-byte chunks, or null: a
-// row of zeros); the block holds row0 rows already.  Every lane of the wave calls it.
-template <int DT, int QT, int D, int SHIFT, typename Source>
-__device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row0, int n, Source source) {
+// Rows row0 .. row0 + n - 1 of one block and head; the block holds row0 rows already.  load(i): the lane's 16-byte
+// chunk, number lane % CH of row i RPP + lane / CH of the new ones (zeros past the last).  Every lane of the wave
+// calls it.
+template <int DT, int QT, int D, int SHIFT, typename Load>
+__device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row0, int n, Load load) {
   constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH;
   constexpr int NC = kChunks<DT, D, SHIFT>;
   if constexpr (NC > kHeldChunks) {
-    store_rows_any<DT, QT, D>(codes, scale, row0, n, source);
+    store_rows_any<DT, QT, D>(codes, scale, row0, n, load);
     return;
   } else {
     const int lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
@@ -124,10 +122,7 @@ __device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       x[i] = u32x4_t{0u, 0u, 0u, 0u};
-      if (i * RPP + rr < n) {
-        const u32x4_t* src = source(i * RPP + rr);
-        if (src) x[i] = src[c];
-      }
+      if (i * RPP < n) x[i] = load(i);
     }
     uint32_t amax = 0;  // without the signs; two bf16 at a time
 #pragma unroll
@@ -144,10 +139,11 @@ __device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row
     if constexpr (DT == kDtBf16) amax = max(amax << 16, amax & 0xFFFF0000u);
     amax = wave_max_u32(amax);
     if (amax >= 0x7F800000u) {  // an infinity or a NaN among them
-      store_rows_any<DT, QT, D>(codes, scale, row0, n, source);
+      store_rows_any<DT, QT, D>(codes, scale, row0, n, load);
       return;
     }
     const float s = grown_scale<QT, D>(codes, row0, old, block_scale<QT>(amax)), inv = inv_scale(s);
+    uint8_t* to = codes + row0 * D + rr * D + c * EPT;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       // (a value's conversion is not kept from the first pass over the chunks: registers)
@@ -155,7 +151,7 @@ __device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row
       if (i * RPP + rr < n) {
         float f[EPT];
         chunk_values<DT>(x[i], f);
-        store_chunk<QT, true>(codes + (row0 + i * RPP + rr) * D + c * EPT, f, inv);
+        store_chunk<QT, true>(to + i * RPP * D, f, inv);
       }
     }
     if (lane == 0) *scale = s;
@@ -168,7 +164,7 @@ struct AppendArgs {
   Paged pc;
   const void* k_new;
   const void* v_new;
-  int64_t tok_chunks;  // 16-byte chunks between two tokens' rows
+  uint32_t tok_bytes;  // between two tokens' rows: at most 2^28
   const int32_t* slots;
   int n_tok, n_share;  // waves that share the runs of 64 tokens
 };
@@ -177,7 +173,7 @@ struct AppendArgs {
 // takes every n_share-th of the runs that begin among them.
 template <int DT, int QT, int D, int SHIFT>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
-  constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16;
+  constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16, RPP = 64 / CH;
   const int lane = threadIdx.x & 63;
   int64_t id = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
   const int kv = (int)(id & 1);
@@ -211,9 +207,16 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
       n += 64;
     }
     const int64_t unit = (int64_t)(s0 >> SHIFT) * a.pc.h_kv + g;
-    const u32x4_t* src = static_cast<const u32x4_t*>(kv ? a.v_new : a.k_new) + (int64_t)t0 * a.tok_chunks + g * CH;
+    // a wave-uniform address and a lane's 32-bit offset
+    const uint8_t* src = static_cast<const uint8_t*>(kv ? a.v_new : a.k_new) + (int64_t)t0 * a.tok_bytes + g * (CH * 16);
+    const uint32_t mine = lane / CH * a.tok_bytes + lane % CH * 16;
     store_rows<DT, QT, D, SHIFT>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit,
-                                 row0, n, [&](int i) { return src + i * a.tok_chunks; });
+                                 row0, n, [&](int i) {
+                                   u32x4_t x = {0u, 0u, 0u, 0u};
+                                   if (i * RPP + lane / CH < n)
+                                     x = *reinterpret_cast<const u32x4_t*>(src + (int64_t)i * RPP * a.tok_bytes + mine);
+                                   return x;
+                                 });
   }
 }
 
@@ -314,7 +317,8 @@ __device__ __forceinline__ void kept_positions(const int32_t* sel, int bp, int L
 // each block of K and of V.
 template <int DT, int QT, int D, int SHIFT>
 __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArgs a) {
-  constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16, R = 1 << SHIFT;
+  constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16, RPP = 64 / CH, R = 1 << SHIFT;
+  const int lane = threadIdx.x & 63;
   extern __shared__ __align__(16) int32_t lds[];  // positions of the workgroup's rows, then work space
   const int g = blockIdx.y, p = blockIdx.z;
   const int L = a.lens[p];
@@ -337,10 +341,13 @@ __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArg
     const int64_t unit = (int64_t)block * a.pc.h_kv + g;
     const int r0 = j << SHIFT;
     store_rows<DT, QT, D, SHIFT>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit, 0,
-                                 min(R, rows - r0), [&](int i) -> const u32x4_t* {
-                                   const int r = r0 + i;
+                                 min(R, rows - r0), [&](int i) {
+                                   const int r = r0 + i * RPP + lane / CH;
+                                   u32x4_t x = {0u, 0u, 0u, 0u};
+                                   if (r >= rows) return x;
                                    const int pos = r < bp ? lds[r - first] : L - a.keep_tail + (r - bp);
-                                   return pos < 0 || pos >= L ? nullptr : src + (int64_t)pos * CH;
+                                   if (pos >= 0 && pos < L) x = src[(int64_t)pos * CH + lane % CH];
+                                   return x;
                                  });
   }
 }
@@ -368,7 +375,7 @@ template <typename F> hipError_t dispatch(const Paged& pc, F f) {
 
 hipError_t launch_paged_append(const Paged& pc, const void* k_new, const void* v_new, int64_t tok_stride,
                                const int32_t* slots, int n_tok, hipStream_t stream) {
-  AppendArgs a{pc, k_new, v_new, tok_stride / (pc.dtype == kDtBf16 ? 8 : 4), slots, n_tok, 1};
+  AppendArgs a{pc, k_new, v_new, (uint32_t)(tok_stride * (pc.dtype == kDtBf16 ? 2 : 4)), slots, n_tok, 1};
   const int64_t chunks = ((int64_t)n_tok + 63) / 64, units = chunks * pc.h_kv * 2;
   // single rows of many requests are runs of their own: as many waves to 64 tokens as fill the chip
   constexpr int64_t kFill = 16384;

@@ -128,6 +128,7 @@ def test_append_checks():
     assert _append(c, k=NULL) == _append(c, v=NULL) == _append(c, slots=NULL) == _lib.KV_ERR_NULL
     assert _append(c, k=ODD) == _append(c, v=ODD) == _append(c, n=0) == _lib.KV_ERR_ARG
     assert _append(c, stride=1020) == _append(c, stride=1028) == _lib.KV_ERR_ARG
+    assert _append(c, stride=(1 << 26) + 8) == _attend(c, stride=(1 << 26) + 8) == _lib.KV_ERR_ARG
     f = ctypes.byref(_cache(dtype=_lib.KV_F32))
     assert _append(f, stride=1026) == _lib.KV_ERR_ARG
 
