@@ -508,12 +508,19 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
   if (pc.dtype == kDtBf16 && cols > 32) {
     plan.prompt_waves = cols <= 128 ? 4 : 8;
     units = (int64_t)pc.n_prob * pc.h_kv * ((cols + 32 * plan.prompt_waves - 1) / (32 * plan.prompt_waves));
-    constexpr int64_t kFill = 512, kMinSplit = 512;
-    if (units < kFill) n = std::max<int64_t>(1, std::min(kFill / units, (rows + kMinSplit - 1) / kMinSplit));
+    // one round of 256 workgroups in splits of at least 512 rows: more splits cost more in the join than they even
+    // out (2048 tokens of one prompt 70 us whole, 153 in two splits; 40 tokens over 32768 rows 47 us in 32 splits,
+    // 61 in 64)
+    n = std::max<int64_t>(1, std::min<int64_t>(256 / units, (rows + 511) / 512));
   } else {
-    constexpr int64_t kRound = 768, kMinSplit = 256;
+    // Up to 512 rows a unit stays whole (500 rows of 64 units 8.2 us whole, 9.1 split and joined; of 512 units 15.1
+    // and 22.3).  Longer ones get two rounds of the 768 workgroups that fit the chip at once, so that caches of
+    // unequal length even out, in splits of at least 512 rows; or where these are few, 512 workgroups of at least
+    // 256 rows (8 units of 2000 rows 9.4 us, in splits of 512 rows 12.0; of 32768 rows in 128 splits 25.9 us, in
+    // 64 20.2).
     units = (int64_t)pc.n_prob * pc.h_kv * column_groups(max_q, pc.group());
-    if (rows > 512) n = std::max<int64_t>(1, std::min(2 * kRound / units, (rows + kMinSplit - 1) / kMinSplit));
+    auto splits = [&](int64_t wgs, int64_t least) { return std::min(wgs / units, (rows + least - 1) / least); };
+    if (rows > 512) n = std::max<int64_t>(1, std::max(splits(1536, 512), splits(512, 256)));
   }
   int64_t split = ((rows + n - 1) / n + 127) / 128 * 128;
   split = std::min<int64_t>(split, plan.prompt_waves ? (int64_t)prompt_split_blocks(plan.prompt_waves) << pc.shift : kMaxSplitRows);

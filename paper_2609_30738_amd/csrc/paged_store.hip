@@ -342,12 +342,13 @@ __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArg
     const int r0 = j << SHIFT;
     store_rows<DT, QT, D, SHIFT>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit, 0,
                                  min(R, rows - r0), [&](int i) {
-                                   const int r = r0 + i * RPP + lane / CH;
-                                   u32x4_t x = {0u, 0u, 0u, 0u};
-                                   if (r >= rows) return x;
-                                   const int pos = r < bp ? lds[r - first] : L - a.keep_tail + (r - bp);
-                                   if (pos >= 0 && pos < L) x = src[(int64_t)pos * CH + lane % CH];
-                                   return x;
+                                   // without a branch, so that the rows' loads are in flight together
+                                   const int r = min(r0 + i * RPP + lane / CH, rows - 1);
+                                   const int kept = n > 0 ? lds[min(r - first, n - 1)] : 0;
+                                   const int pos = r < bp ? kept : L - a.keep_tail + (r - bp);
+                                   const bool in = r0 + i * RPP + lane / CH < rows && (uint32_t)pos < (uint32_t)L;
+                                   const u32x4_t x = src[(int64_t)(in ? pos : 0) * CH + lane % CH];
+                                   return in ? x : u32x4_t{0u, 0u, 0u, 0u};
                                  });
   }
 }
@@ -392,7 +393,7 @@ hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, int max_le
                                 const int32_t* budgets, int keep_tail, hipStream_t stream) {
   PagedCompactArgs a{pc, lens, tok_off, k, v, sel_idx, budget, keep_tail, 1, 0, budgets};
   const int blocks = (budget + keep_tail + (1 << pc.shift) - 1) >> pc.shift;
-  a.wg_blocks = budget <= kCountBudget ? 2 : std::max(2, 256 >> pc.shift);
+  a.wg_blocks = budget <= kCountBudget ? 2 : std::max(2, 128 >> pc.shift);
   int work = kThreads;  // words: the counted positions, the bitmap, the sorted positions
   if (budget > kCountBudget) {
     if (max_len <= kBitmapLen) a.bitmap_words = (max_len + 31) / 32;
