@@ -578,6 +578,8 @@ class PagedCache:
         st = t.stride()
         if st[2] != 1 or (st[1] != d and heads > 1):
             raise ValueError(f"the heads of a token must be contiguous in {name}")
+        if shape[0] > 1 and st[0] < heads * d:
+            raise ValueError(f"the tokens overlap in {name}")
         return t.data_ptr(), (st[0] if shape[0] > 1 else heads * d)
 
     def _stream(self, stream):

@@ -71,8 +71,9 @@ PagedPlan paged_plan(const Paged& pc, int max_q);
 int64_t paged_grid_y(const Paged& pc, int max_q, const PagedPlan& plan);
 size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t stream);
-// Blocks of a split that the prompt kernel of so many waves holds in LDS.
-constexpr int prompt_split_blocks(int waves) { return waves == 4 ? 256 : 1024; }
+// Blocks of a split that the prompt kernel of so many waves holds in LDS beside its tiles
+// (two workgroups of four waves share a CU's 160 KB, one of eight has it alone).
+constexpr int prompt_split_blocks(int waves) { return waves == 4 ? 256 : 4096; }
 hipError_t launch_paged_prompt(const PagedAttnArgs& a, int waves, hipStream_t stream);
 
 }  // namespace kv

@@ -227,72 +227,80 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       return u32x4_t{y[0], y[1], z[0], z[1]};
     };
     f32x16v s[2];
-    u32x4_t f[NS];
+    u32x4_t f[NS], pf[4];  // pf: weights of rows 16 u + 4 h + {0..3, 8..11}
+    float part[4];
+    // weights of the logits j, j + 1 of half kt
+    auto weigh = [&](int kt, int j) __attribute__((always_inline)) {
+      const int u = 2 * kt + (j >> 3);
+      const float w0 = __builtin_amdgcn_exp2f(fmaf(s[kt][j], c, -mu)), w1 = __builtin_amdgcn_exp2f(fmaf(s[kt][j + 1], c, -mu));
+      part[u] = j & 7 ? part[u] + w0 : w0;
+      part[u] += w1;
+      pf[u][(j & 7) >> 1] = pack_bf16(w0, w1);
+    };
+    // the half's weights join the sum; where they are too large they are taken again from a higher reference
+    auto settle = [&](int kt) __attribute__((always_inline)) {
+      if (__ballot(part[2 * kt] + part[2 * kt + 1] > 1.f)) {
+        float tm = s[kt][0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) tm = fmaxf(tm, s[kt][j]);
+        // a column whose logits are all -inf so far keeps the lowest reference
+        const float top = fmaxf(half_max(tm) * c, -kLowest), mn = fmaxf(mu, top + kOctaves);
+        const float r = __builtin_amdgcn_exp2f(mu - mn);
+        mu = mn;
+        sum *= r;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) acc[i] *= r;
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) weigh(kt, j);
+      }
+      sum += part[2 * kt] + part[2 * kt + 1];
+    };
+    const int has = __builtin_amdgcn_readfirstlane(x.has[0] & x.has[1] & x.has[2] & x.has[3]);
+    const bool masked = rb + kTile > wvis_min || !has;
+    auto mask = [&](int kt) __attribute__((always_inline)) {
+      if (!masked) return;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int r = 32 * kt + 8 * (j >> 2) + 4 * h + (j & 3);
+        if (rb + r >= vis || !x.has[2 * kt + (j >> 3)]) s[kt][j] = -INFINITY;
+      }
+    };
+    bool nan_rows = false;
+    if (QT == kQtE4m3 && rb + kTile > wvis_min) {
+      int any = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) any |= x.nan[w];
+      nan_rows = __builtin_amdgcn_readfirstlane(any) != 0;
+    }
 #pragma unroll
     for (int d = 0; d < NS; ++d) f[d] = k_frag(0, d);
     __builtin_amdgcn_sched_barrier(0);
+    s[0] = 0.f;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      s[kt] = 0.f;
-#pragma unroll
-      for (int d = 0; d < NS; ++d) {
-        s[kt] = mfma32(f[d], qf[d], s[kt]);
-        f[d] = kt == 0 ? k_frag(1, d) : v_frag(d);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+    for (int d = 0; d < NS; ++d) {
+      s[0] = mfma32(f[d], qf[d], s[0]);
+      f[d] = k_frag(1, d);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    bool nan_rows = false;
-    const int has = __builtin_amdgcn_readfirstlane(x.has[0] & x.has[1] & x.has[2] & x.has[3]);
-    if (rb + kTile > wvis_min || !has) {
+    mask(0);
+    // the second half's products beside the first one's weights
+    s[1] = 0.f;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+    for (int d = 0; d < NS; ++d) {
+      s[1] = mfma32(f[d], qf[d], s[1]);
+      f[d] = v_frag(d);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int r = 32 * kt + 8 * (j >> 2) + 4 * h + (j & 3);
-          if (rb + r >= vis || !x.has[2 * kt + (j >> 3)]) s[kt][j] = -INFINITY;
-        }
-      if (QT == kQtE4m3 && rb + kTile > wvis_min) {
-        int any = 0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) any |= x.nan[w];
-        nan_rows = __builtin_amdgcn_readfirstlane(any) != 0;
-      }
+      for (int j = 16 * d / NS; j < 16 * (d + 1) / NS; j += 2) weigh(0, j);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    u32x4_t pf[4];  // weights of rows 16 u + 4 h + {0..3, 8..11}
-    float part[4];
-    auto weigh = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        part[u] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-          const float w0 = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + j], c, -mu));
-          const float w1 = __builtin_amdgcn_exp2f(fmaf(s[u >> 1][8 * (u & 1) + j + 1], c, -mu));
-          part[u] += w0;
-          part[u] += w1;
-          pf[u][j >> 1] = pack_bf16(w0, w1);
-        }
-      }
-      return (part[0] + part[1]) + (part[2] + part[3]);
-    };
-    float ts = weigh();
-    if (__ballot(ts > 1.f)) {
-      float tm = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-      for (int j = 1; j < 16; ++j) tm = fmaxf(tm, fmaxf(s[0][j], s[1][j]));
-      // a column whose logits are all -inf so far keeps the lowest reference
-      const float top = fmaxf(half_max(tm) * c, -kLowest), mn = fmaxf(mu, top + kOctaves);
-      const float f = __builtin_amdgcn_exp2f(mu - mn);
-      mu = mn;
-      sum *= f;
-#pragma unroll
-      for (int i = 0; i < ND; ++i) acc[i] *= f;
-      ts = weigh();
-    }
-    sum += ts;
+    settle(0);
+    mask(1);
     if (QT == kQtE4m3 && nan_rows) {
       // a NaN counts for the columns that see its row alone: it leaves the products, and the columns that
       // see one are marked by a product of indicators
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) weigh(1, j);
+      settle(1);
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -317,8 +325,13 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int q = 0; q < 4 * ND; ++q) {
+        if (q == 2 * ND) settle(1);
         acc[q % ND] = mfma32(f[q % NS], pf[q / ND], acc[q % ND]);
         if (q + NS < 4 * ND) f[q % NS] = v_frag(q + NS);
+        if (q < 2 * ND) {
+#pragma unroll
+          for (int j = 8 * q / ND; j < 8 * (q + 1) / ND; j += 2) weigh(1, j);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }

@@ -479,6 +479,22 @@ def test_attention_turns_of_many_problems(qtype, d, h_q, n_tok):
         _check(pc, q, scale, n_q, _attend(pc, q, scale, n_q), f"many turns {scale}")
 
 
+def test_attention_turn_over_more_blocks_than_a_split_holds():
+    """5000 rows in blocks of 16 are more than a split of the four-wave prompt kernel takes (256 blocks): two
+    splits although the batch fills the chip."""
+    rng = _rng(31)
+    lens = np.full(40, 30)
+    lens[[3, 17]] = 5000, 4097
+    n_q = np.zeros(40, int)
+    n_q[[3, 9, 17]] = 12, 5, 3
+    pc = _cache(rng, "bf16", "e4m3", 32, 8, 64, 16, lens)
+    q = _q(rng, 20, 32, 64, "bf16")
+    need = _lib.paged_attention_workspace_bytes(pc, 20, 12)
+    assert need == -(-20 * 32 * 2 * 66 * 4 // 256) * 256
+    _say("attention many blocks")
+    _check(pc, q, 0.125, n_q, _attend(pc, q, 0.125, n_q), "many blocks")
+
+
 @pytest.mark.parametrize("n", [1, 3, 70])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_missing_blocks(dtype, n):
@@ -593,6 +609,32 @@ def test_attention_strided_queries_and_wide_bounds():
     ws = torch.empty(max(256, _lib.paged_attention_workspace_bytes(pc, 12, 11)), dtype=torch.uint8, device="cuda")
     _lib.paged_attention(pc, q, 0.08, o, off, 11, ws)
     assert torch.equal(o[:5], out[:5]) and (o[5:] == 7).all()
+
+
+def test_binding_refuses_overlapping_tokens_and_other_types():
+    import torch
+    rng = _rng(32)
+    pc = _cache(rng, "bf16", "e4m3", 4, 2, 64, 16, [20, 30])
+    q = _q(rng, 2, 4, 64, "bf16")
+    out = torch.empty_like(q)
+    rows = torch.zeros(2, 2, 64, dtype=torch.bfloat16, device="cuda")
+    slots = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in (q[:1].expand(2, 4, 64), q.float(), q[:, :2], q.transpose(0, 1).contiguous().transpose(0, 1), q.cpu()):
+        with pytest.raises(ValueError):
+            _lib.paged_attention(pc, bad, 0.1, out)
+    for bad in (out.float(), out[:1], torch.empty(2, 8, 64, dtype=torch.bfloat16, device="cuda")[:, :4]):
+        with pytest.raises(ValueError):
+            _lib.paged_attention(pc, q, 0.1, bad)
+    with pytest.raises(ValueError):
+        _lib.paged_append(pc, rows, rows[:1], slots)
+    with pytest.raises(ValueError):
+        _lib.paged_append(pc, rows, rows, slots.long())
+    with pytest.raises(ValueError):
+        _lib.paged_append(pc, rows, torch.zeros(2, 6, 64, dtype=torch.bfloat16, device="cuda")[:, :2], slots)
+    with pytest.raises(_lib.KvError):  # a workspace too small
+        pc.struct.max_len = 30
+        far = _lib.PagedCache("bf16", 4, pc.k, pc.v, pc.k_scale, pc.v_scale, torch.zeros(2, 400, dtype=torch.int32, device="cuda"), pc.lens)
+        _lib.paged_attention(far, q, 0.1, out, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
 
 
 def test_attention_past_32_bit_offsets():
@@ -720,3 +762,37 @@ def test_captured_step():
         if i % 7 == 0:
             _check(a, qkv[:, :h_q], 0.125, None, xa["out"], f"replay {i}")
     assert a.lens.tolist() == [x + 20 for x in lens]
+
+
+@pytest.mark.parametrize("n", [4, 60])
+def test_captured_turns_share_a_workspace(n):
+    """Two captured calls of several tokens each that share a workspace (one after the other on their stream),
+    replayed three times over other queries with eager work between, against eager calls."""
+    import torch
+    rng = _rng(22, n)
+    h_q, h_kv, d = 8, 2, 128
+    pcs = [_cache(rng, "bf16", "e4m3", h_q, h_kv, d, 32, lens) for lens in ([1500, 300], [900, 1200])]
+    n_q = [n, n - 1]
+    T = 2 * n - 1
+    off = _dev(np.asarray([0, n, T], np.int32))
+    q = [_q(rng, T, h_q, d, "bf16") for _ in range(2)]
+    out = [torch.zeros_like(x) for x in q]
+    need = max(_lib.paged_attention_workspace_bytes(pc, T, n) for pc in pcs)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            for pc, x, o in zip(pcs, q, out):
+                _lib.paged_attention(pc, x, 0.09, o, off, n, ws)
+    torch.cuda.synchronize()
+    for i in range(3):
+        for x in q:
+            x.copy_(_q(rng, T, h_q, d, "bf16"))
+        _say("captured turns", n, i)
+        graph.replay()
+        torch.cuda.synchronize()
+        for pc, x, o in zip(pcs, q, out):
+            assert torch.equal(_attend(pc, x, 0.09, n_q), o), i
+    _check(pcs[1], q[1], 0.09, n_q, out[1], "captured")
