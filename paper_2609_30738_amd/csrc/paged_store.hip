@@ -2,7 +2,12 @@
 // eviction keeps (kv_paged_compact).
 //
 // A wave takes the rows of one (block, kv head) of K or of V, 16 bytes a lane and load, and holds them in
-// registers: the largest |x| over them, the scale, the codes.  Bound by the rows' reads.
+// registers: the largest |x| over them, the scale, the codes.  So a row is read once, and the wave needs no other.
+//   paged_append_kernel: 195,000 rows of 8 heads of 128 (bf16 to e4m3, K and V: 800 MB read, 400 MB written) 285 us,
+//     4.2 TB/s of HBM, a copy's 4.7 (365 us with the rows' addresses per lane, 695 a row at a time); 64 single rows
+//     6.6 us: a chain of loads (slots, the row and the block's scale) and the launch.
+//   paged_compact_kernel: 96 rows of 32 layers and 8 heads 7.4 us (lengths, positions, their ranks and rows are a
+//     chain of loads); 1792 to 256 rows of 32 layers of 32768, in int8, 63 us for 207 MB, read in single rows of 256 bytes.
 #include <limits.h>
 #include <math.h>
 
@@ -235,8 +240,11 @@ namespace {
 
 // Budgets up to which a position's rank is counted against all others, and the longest problem whose positions
 // are ranked through a bitmap (32 KB); beyond, or where a position is given twice, they are sorted.
+// Counted and through the bitmap: 64 of 131072 positions 4.6 and 8.5 us, 250 of 4096 9.4 and 7.7, of 32768 (32 layers)
+// 18.3 and 18.1, of 262144 9.4 and 22.9; sorted 7.4, 13.3, 22.2 and 13.3.  Bitmap and sorted, 1024 on average of
+// 32768 (32 layers): 63 and 138 us.
 constexpr int kCountBudget = 256;
-constexpr int kBitmapLen = 1 << 18;
+constexpr int kCountLen = (1 << 24) - 1, kBitmapLen = 1 << 18;
 
 // pos[0, n): the positions of rows first .. first + n - 1 of the unit, first + n <= bp: the ascending order of
 // sel[0, bp).  lds: work space (see compact_lds).  Starts and ends synchronised.
@@ -244,15 +252,20 @@ __device__ __forceinline__ void kept_positions(const int32_t* sel, int bp, int L
                                                int32_t* work, int words) {
   __shared__ int32_t sums[kWaves], below, twice;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (bp <= kCountBudget) {
+  if (bp <= kCountBudget && L < kCountLen) {
+    // keys of 24 bits of the position (below 0: the lowest, past the problem: the highest) and 8 of its place
     const int mine = tid < bp ? sel[tid] : INT_MAX;
-    work[tid] = mine;
+    const uint32_t key = (uint32_t)(min(max(mine, -1), kCountLen - 1) + 1) << 8 | tid;
+    uint32_t* keys = reinterpret_cast<uint32_t*>(work);
+    keys[tid] = key;
     __syncthreads();
     int rank = 0;
-    for (int j = 0; j < bp; j += 4) {
-      const int4 o = *reinterpret_cast<const int4*>(work + j);
-      rank += (o.x < mine || (o.x == mine && j < tid)) + (o.y < mine || (o.y == mine && j + 1 < tid)) +
-              (o.z < mine || (o.z == mine && j + 2 < tid)) + (o.w < mine || (o.w == mine && j + 3 < tid));
+    for (int j0 = 0; j0 < bp; j0 += 32) {  // (past bp: the highest, with later places)
+#pragma unroll
+      for (int j = j0; j < j0 + 32; j += 4) {
+        const u32x4_t o = *reinterpret_cast<const u32x4_t*>(keys + j);
+        rank += (o[0] < key) + (o[1] < key) + (o[2] < key) + (o[3] < key);
+      }
     }
     if (tid < bp && rank >= first && rank < first + n) pos[rank - first] = mine;
     __syncthreads();
@@ -378,8 +391,9 @@ hipError_t launch_paged_append(const Paged& pc, const void* k_new, const void* v
                                const int32_t* slots, int n_tok, hipStream_t stream) {
   AppendArgs a{pc, k_new, v_new, (uint32_t)(tok_stride * (pc.dtype == kDtBf16 ? 2 : 4)), slots, n_tok, 1};
   const int64_t chunks = ((int64_t)n_tok + 63) / 64, units = chunks * pc.h_kv * 2;
-  // single rows of many requests are runs of their own: as many waves to 64 tokens as fill the chip
-  constexpr int64_t kFill = 16384;
+  // single rows of many requests are runs of their own: as many waves to 64 tokens as fill the chip.  4096 single rows
+  // of 8 heads 34 us, with 2048 waves 49, with 8192 38; 60 prompts of up to 50 rows 5.4, 6.4 and 6.5
+  constexpr int64_t kFill = 4096;
   a.n_share = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(n_tok, 64), kFill / units));
   const unsigned wgs = (unsigned)((units * a.n_share + kWaves - 1) / kWaves);
   return dispatch(pc, [&](auto dt, auto qt, auto d, auto shift) {
@@ -393,6 +407,9 @@ hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, int max_le
                                 const int32_t* budgets, int keep_tail, hipStream_t stream) {
   PagedCompactArgs a{pc, lens, tok_off, k, v, sel_idx, budget, keep_tail, 1, 0, budgets};
   const int blocks = (budget + keep_tail + (1 << pc.shift) - 1) >> pc.shift;
+  // a workgroup ranks for its blocks alone: few of them where ranking is short (96 rows 8.4 us, with one block 9.7
+  // before ranks were counted by keys), else as many as pay for it (falling budgets 64 us; half the rows a workgroup 65,
+  // twice 81)
   a.wg_blocks = budget <= kCountBudget ? 2 : std::max(2, 128 >> pc.shift);
   int work = kThreads;  // words: the counted positions, the bitmap, the sorted positions
   if (budget > kCountBudget) {

@@ -21,8 +21,9 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kFillThreads = 256;
 constexpr int kWaveRows = 256;  // of a wave of the fill kernel, four a lane
 constexpr int kMaxRows = 1 << 24;  // of a problem
-// Slots up to which one workgroup fills them where lengths are updated in place, a launch less, and slots for
-// each further workgroup where they are not.
+// Slots up to which one workgroup fills them where lengths are updated in place, a launch less (4096 slots of 64
+// requests 6.9 us, of 1024 requests 8.5, by two launches 9.5 and 12.5; 16384 of 1024 requests 20.7 and 13.8), and slots
+// for each further workgroup where they are not.
 constexpr int kFillInScan = 4096, kScanRows = 2048;
 
 __device__ __forceinline__ int64_t wave_scan(int64_t v) {  // inclusive
