@@ -479,7 +479,7 @@ size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_to
  * r <= len[p] - n_p + j:
  *   out[t,h,:] = sum_r softmax_r(scale <q[t,h], k[r]>) v[r],  kv head h / (h_q / h_kv);
  * 0 where it sees none.  q: token t at t * q_stride elements (0: h_q * d; at least that, at most 2^26, whole
- * 16-byte chunks), [h_q][d]; out [n_tok][h_q][d] of the queries' type.  Logits, softmax and sums in fp32; the weights enter
+ * 16-byte chunks), [h_q][d]; out [n_tok][h_q][d] of the queries' type.  scale times log2(e) finite (KV_ERR_ARG).  Logits, softmax and sums in fp32; the weights enter
  * the product with V with 24 significant bits (fp32 queries), 16 (bf16 and max_q h_q / h_kv <= 16) or as
  * bf16 (more).  The outputs of
  * tokens outside every problem (a padded batch) stay as they were, and so do a problem's whose tok_off reaches outside

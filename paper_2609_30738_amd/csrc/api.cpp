@@ -916,7 +916,8 @@ int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride,
   int st = check_paged(c, &a.pc);
   if (st != KV_OK) return st;
   if (!q || !out) return KV_ERR_NULL;
-  if (!aligned16(q) || !aligned16(out) || !std::isfinite(scale)) return KV_ERR_ARG;
+  // (the kernels take powers of two: the scale times log2(e))
+  if (!aligned16(q) || !aligned16(out) || !std::isfinite(scale * kLog2eF)) return KV_ERR_ARG;
   kv::PagedPlan plan;
   st = check_tokens(a.pc, n_tok, max_q, &plan);
   if (st != KV_OK) return st;

@@ -18,6 +18,10 @@
 //   more than kSlack octaves; weights are 2^(t - m - kSlack), so that none exceeds 1.
 //   The four waves are merged through LDS; with several splits the partial sums go to the workspace and
 //   paged_combine_kernel joins them.
+//   Bound by the cache's reads: one token over 32 caches of 32768 rows (e4m3, 8 heads of 128, 2.0 GB) 340 us, 5.9 TB/s
+//   of the 6.9 that streaming reads reach here; 24 ragged ones of up to 24001 rows (int8, eight query heads to a
+//   kv head) 150 us, where a code's conversion costs nearly as much as its load (int8 goes through fp32); over 32
+//   caches of 100 rows 6.3 us, fp32 over four of 4097 rows 11.7 us with the join: latency.
 #include <math.h>
 
 #include <algorithm>
@@ -505,7 +509,7 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
   PagedPlan plan;
   plan.prompt_waves = 0;
   int64_t n = 1, units;
-  if (pc.dtype == kDtBf16 && cols > 32) {
+  if (pc.dtype == kDtBf16 && cols > 32) {  // (20 columns 51 us in paged_attn_kernel, 85 in the other)
     plan.prompt_waves = cols <= 128 ? 4 : 8;
     units = (int64_t)pc.n_prob * pc.h_kv * ((cols + 32 * plan.prompt_waves - 1) / (32 * plan.prompt_waves));
     // one round of 256 workgroups in splits of at least 512 rows: more splits cost more in the join than they even

@@ -3,16 +3,27 @@
 //
 // paged_prompt_kernel: one workgroup of W waves per (32 W columns, split of the rows, kv head, problem), each
 //   wave 32 columns.  Tiles of 64 rows go through LDS in bf16, which holds code * scale exactly (a scale is a
-//   power of two), K as it lies and V transposed; the next tile's codes are in flight meanwhile, and the one
-//   after's table entries.  With v_mfma_f32_32x32x16_bf16,
+//   power of two), both as they lie; the next tile's codes are in flight meanwhile, and the one after's blocks.
+//   With v_mfma_f32_32x32x16_bf16,
 //     S^T = K Q^T,  O^T = V^T P^T:
-//   a lane of the accumulator holds one column and 16 of a tile's 32 rows, so the running maximum and sum
-//   stay in the lane, and its weights are, eight at a time, its own operand of the second product;
-//   V^T lies in LDS in the order of that operand's rows.
-//   Weights are rounded to bf16 for that product (2^-9 of each, the step of the bf16 output); their sum
-//   is taken of the unrounded ones.
+//   a lane of the accumulator holds one column and 16 of 32 rows, so the column's sum stays in the lane, and its
+//   weights are, eight at a time, its own operand of the second product; V's operand is read with the transposing
+//   LDS loads, in the order of those rows.
+//   The weights are 2^(t - reference) without a running maximum: the reference moves only where they grow past 1.
+//   They are rounded to bf16 for the second product (2^-9 of each, the step of the bf16 output); their sum is taken of
+//   the unrounded ones.  The exponentials of a half of the tile run beside the matrix products of the other.
 //   The grid's fastest axis is the kv head: workgroups go to the 8 XCDs in turn, so that with 8 heads one L2
 //   holds one head's rows.  The last columns, which see the most rows, come first.
+//
+//   Bound by the matrix units, 43 % busy, and by the LDS beside them, whose operands a wave reads for itself.  Three
+//   prompts of up to 4096 tokens over caches of up to 16384 rows (32 heads over 8, d = 128): 1842 us, 1.05 PFLOP/s of
+//   the 1.58 that a large product reaches; 1144 us at d = 64, 1921 from int8.  At an earlier step (1900 us) the same
+//   without staging took 1612, without the operands' reads 1685, without both 1303, the products alone 785.
+//   Measured and left: V transposed as it is staged 2020 (then 1900), both halves' logits before the weights 1890
+//   (then 1842), masked and unmasked tiles as two copies of the code 2905 (then 2372), raised wave priority around the
+//   products 2005 (then 1900), the staging spread over the second product 1908, 64 columns a wave (half the operand
+//   reads, but one wave a SIMD with its sums in the accumulation registers) 4612.
+//   W: 4 waves for up to 128 columns, 8 beyond: 64 columns 54 us with 4 and 57 with 8, 1024 columns 415 and 299.
 #include <math.h>
 
 #include <algorithm>

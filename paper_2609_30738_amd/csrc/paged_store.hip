@@ -7,7 +7,8 @@
 //     4.2 TB/s of HBM, a copy's 4.7 (365 us with the rows' addresses per lane, 695 a row at a time); 64 single rows
 //     6.6 us: a chain of loads (slots, the row and the block's scale) and the launch.
 //   paged_compact_kernel: 96 rows of 32 layers and 8 heads 7.4 us (lengths, positions, their ranks and rows are a
-//     chain of loads); 1792 to 256 rows of 32 layers of 32768, in int8, 63 us for 207 MB, read in single rows of 256 bytes.
+//     chain of loads); 1792 to 256 rows of 32 layers of 32768, in int8, 63 us for 207 MB, read in rows of 256
+//     bytes.
 #include <limits.h>
 #include <math.h>
 

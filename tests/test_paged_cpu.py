@@ -111,6 +111,12 @@ def test_attention_checks():
     assert _attend(c, stride=4095) == _attend(c, stride=4100) == _attend(c, stride=-8) == _lib.KV_ERR_ARG
 
 
+def test_attention_scale_times_log2e():
+    """The largest scales are finite and their product with log2(e) is not."""
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        assert _attend(cache(), scale=scale) == _lib.KV_ERR_ARG
+
+
 def test_attention_workspace():
     c = _cache(n_blocks=4000, table_stride=2048, max_len=32768)
     need = _lib.lib().kv_paged_attention_workspace_bytes(ctypes.byref(c), 4, 1)
