@@ -114,7 +114,7 @@ def test_attention_checks():
 def test_attention_scale_times_log2e():
     """The largest scales are finite and their product with log2(e) is not."""
     for scale in (2.4e38, -2.4e38, 3.4e38):
-        assert _attend(cache(), scale=scale) == _lib.KV_ERR_ARG
+        assert _attend(ctypes.byref(_cache()), scale=scale) == _lib.KV_ERR_ARG
 
 
 def test_attention_workspace():
