@@ -1,6 +1,6 @@
 // Attention of the last tokens of every problem over its 8-bit paged cache (kv_paged_attention).
 //
-// paged_attn_kernel: one workgroup of four waves per (split of the rows, kv head and group of columns,
+// paged_attn_kernel: one workgroup of four waves per (kv head and group of columns, split of the rows,
 //   problem).  A column is a (token, query head) pair of the kv head; a wave takes 16 NT of them
 //   against 32 rows a step:
 //     S^T = K Q^T by v_mfma_f32_16x16x32_bf16, 16 rows a tile: the codes are exact in bf16, and the
@@ -13,15 +13,18 @@
 //   fp32 queries and weights are taken as three bf16 terms each (24 bits): the matrix products lose nothing
 //   of the operands beyond that, and accumulate in fp32.  With bf16 queries the weights are two terms for up
 //   to 16 columns, where the second one is free beside the loads, and one for more (2^-9 of each, a step of
-//   the output; five tokens of 16 requests 59 us, with two terms 64).
+//   the output; five tokens of 16 requests 59 us, with two terms 64; now 48).
 //   The reference of a column's weights is raised, and the sums rescaled, only when a logit exceeds it by
 //   more than kSlack octaves; weights are 2^(t - m - kSlack), so that none exceeds 1.
+//   The grid's fastest axis is the kv head, so that every XCD gets as many of the splits that reach past a cache's end
+//   as the others (with the splits fastest, 16 of them put each on an XCD of its own: 64 caches of up to 8000 rows
+//   151 us, now 121, 16 of up to 32768 146, now 118).
 //   The four waves are merged through LDS; with several splits the partial sums go to the workspace and
 //   paged_combine_kernel joins them.
-//   Bound by the cache's reads: one token over 32 caches of 32768 rows (e4m3, 8 heads of 128, 2.0 GB) 340 us, 5.9 TB/s
+//   Bound by the cache's reads: one token over 32 caches of 32768 rows (e4m3, 8 heads of 128, 2.0 GB) 336 us, 6.0 TB/s
 //   of the 6.9 that streaming reads reach here; 24 ragged ones of up to 24001 rows (int8, eight query heads to a
-//   kv head) 150 us, where a code's conversion costs nearly as much as its load (int8 goes through fp32); over 32
-//   caches of 100 rows 6.3 us, fp32 over four of 4097 rows 11.7 us with the join: latency.
+//   kv head, 0.66 GB) 137 us, 4.8 TB/s: the last splits of unequal caches leave CUs idle; over 32 caches of 100 rows
+//   6.0 us, fp32 over four of 4097 rows 11.7 us with the join: latency.
 #include <math.h>
 
 #include <algorithm>
@@ -95,7 +98,7 @@ template <int DT, int D, int NT> constexpr int kMinWaves = (NT == 1 ? 3 : 2) - (
 }  // namespace
 
 template <int DT, int QT, int D, int NT>
-__global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_kernel(PagedAttnArgs a, int n_groups) {
+__global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int NS = D / 32;                       // matrix steps over the head dimension
   constexpr int NI = D / 16;                       // 16-wide tiles of the output
   constexpr int KH = D / 64;                       // 16-byte loads of a key
@@ -108,8 +111,9 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
   __shared__ float sh_m[kWaves][16], sh_s[kWaves][16];
   extern __shared__ __align__(16) float sh_acc[];  // [kWaves][up to 16 columns][D]
 
-  const int split = blockIdx.x, g = blockIdx.y / n_groups, cg = blockIdx.y % n_groups, p = blockIdx.z;
-  const int G = a.pc.h_q / a.pc.h_kv;
+  const int p = blockIdx.z, g = blockIdx.x % a.pc.h_kv, cg = blockIdx.x / a.pc.h_kv, G = a.pc.h_q / a.pc.h_kv;
+  // (the problems' splits start one further each: with fewer heads than XCDs, these take long caches' ends in turn)
+  const int split = a.n_split > 1 ? (int)((blockIdx.y + (uint32_t)p) % (uint32_t)a.n_split) : 0;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, kg = lane >> 4;
   const int shift = a.pc.shift, R = 1 << shift;
   const int r0 = split * a.split_rows;
@@ -518,13 +522,14 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
     n = std::max<int64_t>(1, std::min<int64_t>(256 / units, (rows + 511) / 512));
   } else {
     // Up to 512 rows a unit stays whole (500 rows of 64 units 8.2 us whole, 9.1 split and joined; of 512 units 15.1
-    // and 22.3).  Longer ones get two rounds of the 768 workgroups that fit the chip at once, so that caches of
-    // unequal length even out, in splits of at least 512 rows; or where these are few, 512 workgroups of at least
-    // 256 rows (8 units of 2000 rows 9.4 us, in splits of 512 rows 12.0; of 32768 rows in 128 splits 25.9 us, in
-    // 64 20.2).
+    // and 22.3).  Longer ones get three rounds of the 768 workgroups that fit the chip at once, so that caches of
+    // unequal length even out (64 of up to 16384 rows and 2 heads 64 us, in two rounds 71, 32 of up to 4000 37.5 and
+    // 41.1; but 24 of 13000 rows each 126 and 120), in splits of at least 512 rows; or where these are few, 512
+    // workgroups of at least 256 rows (8 units of 2000 rows 9.4 us, in splits of 512 rows 12.0; of 32768 rows in
+    // 128 splits 25.9 us, in 64 20.2).
     units = (int64_t)pc.n_prob * pc.h_kv * column_groups(max_q, pc.group());
     auto splits = [&](int64_t wgs, int64_t least) { return std::min(wgs / units, (rows + least - 1) / least); };
-    if (rows > 512) n = std::max<int64_t>(1, std::max(splits(1536, 512), splits(512, 256)));
+    if (rows > 512) n = std::max<int64_t>(1, std::max(splits(2304, 512), splits(512, 256)));
   }
   int64_t split = ((rows + n - 1) / n + 127) / 128 * 128;
   split = std::min<int64_t>(split, plan.prompt_waves ? (int64_t)prompt_split_blocks(plan.prompt_waves) << pc.shift : kMaxSplitRows);
@@ -548,10 +553,10 @@ namespace {
 
 template <int DT, int QT, int D> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
   const int G = a.pc.group(), nt = column_tiles(a.max_q, G), groups = column_groups(a.max_q, G);
-  const dim3 grid((unsigned)a.n_split, (unsigned)(a.pc.h_kv * groups), (unsigned)a.pc.n_prob);
+  const dim3 grid((unsigned)(a.pc.h_kv * groups), (unsigned)a.n_split, (unsigned)a.pc.n_prob);
   const size_t lds = (size_t)kWaves * std::min(a.max_q * G, 16) * D * sizeof(float);
-  if (nt == 1) paged_attn_kernel<DT, QT, D, 1><<<grid, kThreads, lds, stream>>>(a, groups);
-  else paged_attn_kernel<DT, QT, D, 2><<<grid, kThreads, lds, stream>>>(a, groups);
+  if (nt == 1) paged_attn_kernel<DT, QT, D, 1><<<grid, kThreads, lds, stream>>>(a);
+  else paged_attn_kernel<DT, QT, D, 2><<<grid, kThreads, lds, stream>>>(a);
   return hipGetLastError();
 }
 
