@@ -439,12 +439,13 @@ typedef struct kv_paged_cache {
  *   slots[tok_off[p] + i] = table[p][r / R] * R + r % R, r = len_in[p] + i: where row i of the problem's
  *     new rows goes; -1 from tok_off[n_prob] on (n_slots may count a padded batch);
  *   len[p] = len_in[p] + add[p];  taken_out = blk_off[n_prob].
- * len_in: NULL is 0, and it may be len itself.  add: NULL is 1.  free_blocks [n_free]: NULL is
- * 0, 1, 2, ..  taken_in, taken_out: one value each, the entries of free_blocks used so far (NULL: 0,
- * and not written); they may be the same.  Where the free list ends, or a row lies past the table, entries and slots
+ * len_in: NULL is 0.  add: NULL is 1.  free_blocks [n_free]: NULL is 0, 1, 2, ..  taken_in, taken_out: one
+ * value each, the entries of free_blocks used so far (NULL: 0, and not written).  Where the free list ends, or a row lies past the table, entries and slots
  * are -1 and taken_out still counts the blocks asked for (rows past the table ask for none).  Rows
  * past n_slots get their blocks and no slot.  Lengths are taken as at least 0 and at most 2^24; the
- * new rows of a call must be fewer than 2^31.  len, table, tok_off, blk_off and slots must not overlap. */
+ * new rows of a call must be fewer than 2^31.  In place: len_in or add may be len itself, taken_in may be
+ * taken_out or a value of blk_off (the last call's blk_off[n_prob]), and taken_out may be blk_off + n_prob.  No
+ * output overlaps an input or another output in any other way (KV_ERR_ARG). */
 int kv_paged_tables(const kv_paged_cache* pc, const int32_t* len_in, const int32_t* add,
                     const int32_t* free_blocks, int32_t n_free, const int32_t* taken_in,
                     int32_t* taken_out, int32_t* tok_off, int32_t* blk_off, int32_t* slots,

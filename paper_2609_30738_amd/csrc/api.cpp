@@ -846,6 +846,39 @@ int check_tokens(const kv::Paged& pc, int32_t n_tok, int32_t max_q, kv::PagedPla
   return kv::paged_grid_y(pc, max_q, *plan) > kMaxGrid ? KV_ERR_SHAPE : KV_OK;
 }
 
+// kv_paged_tables' arrays.  in_place: whether an input is written as an output, in one of the ways that the header
+// allows; KV_ERR_ARG where arrays overlap in any other.
+int check_overlaps(const kv::Paged& pc, const kv::TablesArgs& a, bool* in_place) {
+  struct Words {
+    const int32_t* at;
+    int64_t n;
+  };
+  const int64_t n = pc.n_prob;
+  enum { kLen = 1, kTable = 2, kTok = 4, kBlk = 8, kSlots = 16, kTaken = 32 };
+  const Words outs[] = {{pc.len, n},         {pc.table, n * pc.table_stride}, {a.tok_off, n + 1},
+                        {a.blk_off, n + 1}, {a.slots, a.n_slots},             {a.taken_out, 1}};
+  constexpr int kOuts = sizeof(outs) / sizeof(outs[0]);
+  auto met = [&](const Words& x) {  // the outputs that x overlaps
+    int m = 0;
+    for (int i = 0; i < kOuts; ++i) {
+      const uintptr_t p = reinterpret_cast<uintptr_t>(x.at), q = reinterpret_cast<uintptr_t>(outs[i].at);
+      if (p && q && x.n > 0 && outs[i].n > 0 && p < q + outs[i].n * sizeof(int32_t) && q < p + x.n * sizeof(int32_t)) m |= 1 << i;
+    }
+    return m;
+  };
+  // (the count and the last offset are one value)
+  const int total = a.taken_out == a.blk_off + n ? kBlk | kTaken : 0;
+  for (int i = 0; i < kOuts; ++i) {
+    const int others = met(outs[i]) & ~(1 << i);
+    if (others && (others | 1 << i) != total) return KV_ERR_ARG;
+  }
+  const int len_in = a.len_in == pc.len ? 0 : met({a.len_in, n}), add = a.add == pc.len ? 0 : met({a.add, n});
+  const int taken = met({a.taken_in, 1});
+  if (len_in || add || (taken & ~(kBlk | kTaken)) || met({a.free_blocks, a.n_free})) return KV_ERR_ARG;
+  *in_place = a.len_in == pc.len || a.add == pc.len || taken;
+  return KV_OK;
+}
+
 }  // namespace
 
 int kv_paged_tables(const kv_paged_cache* c, const int32_t* len_in, const int32_t* add,
@@ -857,8 +890,10 @@ int kv_paged_tables(const kv_paged_cache* c, const int32_t* len_in, const int32_
   if (st != KV_OK) return st;
   if (!tok_off || !blk_off || (!slots && n_slots > 0)) return KV_ERR_NULL;
   if (n_free < 0 || n_slots < 0) return KV_ERR_ARG;
-  const kv::TablesArgs a{len_in, add, free_blocks, n_free, taken_in, taken_out, tok_off, blk_off, slots, n_slots,
-                         aligned16(slots)};
+  kv::TablesArgs a{len_in, add, free_blocks, n_free, taken_in, taken_out, tok_off, blk_off, slots, n_slots,
+                   aligned16(slots), false};
+  const int overlaps = check_overlaps(pc, a, &a.in_place);
+  if (overlaps != KV_OK) return overlaps;
   return launch_status(kv::launch_paged_tables(pc, a, static_cast<hipStream_t>(stream)));
 }
 

@@ -40,6 +40,7 @@ struct TablesArgs {
   int32_t* slots;           // [n_slots]
   int n_slots;
   bool slots_aligned;       // 16 bytes
+  bool in_place;            // len_in, add or taken_in is written as an output
 };
 hipError_t launch_paged_tables(const Paged& pc, const TablesArgs& a, hipStream_t stream);
 

@@ -3,9 +3,11 @@
 // tables_scan_kernel: prefix sums of the new rows and of the new blocks over the problems, 1024 at a time, in
 //   every workgroup for itself, the offsets and lengths written by the first; then each workgroup takes its
 //   share of the rows' slots and of the blocks' table entries, finding the problem by bisection in LDS.
-//   Lengths updated in place allow one workgroup (the others' sums would read what it writes): many slots are then
-//   filled by a second launch, tables_fill_kernel, from the first one's offsets, where a wave takes kWaveRows
-//   rows and finds the first one's problem by looking at 64 offsets at a time.
+//   Inputs that are outputs too (lengths in place, the count of taken blocks in blk_off or taken_out) allow one
+//   workgroup: the others' sums would read what it writes.  In the one, a value is read before the barrier that
+//   its overwriting follows, or by the thread that overwrites it.  Many slots are then filled by a second launch,
+//   tables_fill_kernel, from the first one's offsets, where a wave takes kWaveRows rows and finds the first one's
+//   problem by looking at 64 offsets at a time.
 //   Bound by latency: a step of 256 requests 5.6 us, 64 prompts of 1.1 million rows 9.3 us (as two launches 10.7;
 //   four rows a thread instead of one 7.4 and 10.0).
 #include <algorithm>
@@ -199,9 +201,8 @@ __global__ __launch_bounds__(kFillThreads) void tables_fill_kernel(Paged pc, Tab
 }
 
 hipError_t launch_paged_tables(const Paged& pc, const TablesArgs& a, hipStream_t stream) {
-  const bool in_place = a.len_in == pc.len || (a.taken_in && a.taken_in == a.taken_out);
-  if (!in_place || a.n_slots <= kFillInScan) {
-    const int wgs = in_place ? 1 : std::max(1, std::min((a.n_slots + kScanRows - 1) / kScanRows, 256));
+  if (!a.in_place || a.n_slots <= kFillInScan) {
+    const int wgs = a.in_place ? 1 : std::max(1, std::min((a.n_slots + kScanRows - 1) / kScanRows, 256));
     tables_scan_kernel<true><<<(unsigned)wgs, kThreads, 0, stream>>>(pc, a);
     return hipGetLastError();
   }

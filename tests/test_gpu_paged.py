@@ -121,6 +121,53 @@ def test_tables(n, R, most):
         assert got[5][0] == want[3][-1]
 
 
+TABLE_FORMS = ["apart", "count in blk_off", "count and total in blk_off", "added rows in len", "lengths in place"]
+
+
+@pytest.mark.parametrize("form", TABLE_FORMS)
+@pytest.mark.parametrize("n,R,most", [(1, 16, 5000), (40, 32, 300), (1024, 16, 9), (1025, 128, 300), (2300, 16, 40)])
+def test_tables_of_many_rows(n, R, most, form):
+    """More slots than one workgroup takes, requests past a scan of 1024: inputs that are apart from the outputs
+    (several workgroups), and every one that may be an output too."""
+    import torch
+    rng = _rng(n, R, most, 2)
+    empty = form == "added rows in len"
+    add = rng.integers(0, most + 1, n)
+    add[0] = most
+    len_in = np.zeros(n, int) if empty else rng.integers(0, 400, n)
+    stride = -(-(400 + most) // R) - 1 if n > 1 else -(-(400 + most) // R)  # the longest may pass the table
+    n_blocks = int((-(-(len_in + add) // R)).sum()) + 20
+    ids = rng.permutation(n_blocks).astype(np.int32)
+    table = np.full((n, stride), -3, np.int32)
+    at = 0
+    for p in range(n):
+        b = min(-(-len_in[p] // R), stride)
+        table[p, :b] = ids[at:at + b]
+        at += b
+    free, taken = ids[at - min(at, 4):], min(at, 4)
+    n_slots = int(add.sum()) + 2100
+    want = paged.tables(table, n_blocks, R, len_in, add, free, taken, n_slots)
+    t, added, lens = _dev(table), _dev(add.astype(np.int32)), _dev(len_in.astype(np.int32))
+    out_len = added if empty else lens if form == "lengths in place" else _dev(np.full(n, -5, np.int32))
+    before = None if empty else lens
+    to, bo, sl = (_dev(np.full(m, -7, np.int32)) for m in (n + 1, n + 1, n_slots))
+    tk, tk_out = _dev(np.asarray([taken], np.int32)), _dev(np.asarray([-9], np.int32))
+    if form.startswith("count"):
+        bo[n] = taken
+        tk = bo[n:]
+        if "total" in form:
+            tk_out = bo[n:]
+    pc = _lib.PagedCache.for_tables(R, n_blocks, t, out_len)
+    _say("tables", n, R, most, form)
+    _lib.paged_tables(pc, before, added, _dev(free), tk, tk_out, to, bo, sl)
+    for name, a, b in zip(("table", "len", "tok_off", "blk_off", "slots"), (t, out_len, to, bo, sl), want):
+        np.testing.assert_array_equal(a.cpu().numpy(), b, err_msg=name)
+    assert int(tk_out) == want[3][-1]
+    if form == "apart":
+        assert int(tk) == taken and torch.equal(lens, _dev(len_in.astype(np.int32)))
+        assert torch.equal(added, _dev(add.astype(np.int32)))
+
+
 def test_tables_where_the_pool_or_the_table_ends():
     """A free list too short, entries of it outside the pool, rows past the table, fewer slots than rows."""
     R, n_blocks = 16, 50

@@ -169,6 +169,39 @@ def test_tables_checks():
             assert _tables(ctypes.byref(_cache(**kw))) == code
 
 
+def test_tables_overlaps():
+    """Arrays that overlap in a way that the kernels do not take: every pair, an input that reaches into an
+    output by one value, and an output that does into another."""
+    n, n_slots, stride, n_free = 4, 10, 20, 30
+    size = dict(table=n * stride, len=n, len_in=n, add=n, free=n_free, taken_in=1, taken_out=1, tok_off=n + 1,
+                blk_off=n + 1, slots=n_slots)
+    outs = ("table", "len", "taken_out", "tok_off", "blk_off", "slots")
+    buf = np.zeros(64 * 128, np.int32)
+    base = {name: buf.ctypes.data + 4 * 128 * (2 * i + 4) for i, name in enumerate(size)}
+
+    def call(**at):
+        a = dict(base, **at)
+        c = _cache(n_prob=n, table_stride=stride, table=a["table"], len=a["len"])
+        return _lib.lib().kv_paged_tables(ctypes.byref(c), a["len_in"], a["add"], a["free"], n_free, a["taken_in"],
+                                          a["taken_out"], a["tok_off"], a["blk_off"], a["slots"], n_slots, NULL)
+
+    taken = {("taken_in", "taken_out"), ("taken_in", "blk_off")}
+    for x in size:
+        for y in outs:
+            if x == y:
+                continue
+            # x's last value on y's first one, x's first on y's last
+            ends = {base[y] - 4 * (size[x] - 1), base[y] + 4 * (size[y] - 1)}
+            if (x, y) in taken:
+                continue
+            for at in ends - ({base[y] + 4 * n} if (x, y) == ("taken_out", "blk_off") else set()):
+                if {x, y} == {"taken_out", "blk_off"} and x == "blk_off" and at == base[y] - 4 * n:
+                    continue  # the count is the last offset
+                assert call(**{x: at}) == _lib.KV_ERR_ARG, (x, y, at - base[y])
+    assert call(taken_out=base["blk_off"] + 4 * (n - 1)) == _lib.KV_ERR_ARG
+    assert call(len_in=base["len"] + 4) == call(add=base["len"] - 4) == _lib.KV_ERR_ARG
+
+
 def test_binding_checks():
     """Shapes and types that the binding itself refuses, on CPU tensors."""
     table, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
