@@ -46,9 +46,11 @@ __device__ __forceinline__ Span span_of(const PagedAttnArgs& a, int p) {
   Span s;
   s.tok0 = a.tok_off ? a.tok_off[p] : p;
   const int end = a.tok_off ? a.tok_off[p + 1] : p + 1;
-  s.n_tok = end - s.tok0;
-  if (s.tok0 < 0 || end > a.n_tok || s.n_tok > a.max_q) s.n_tok = 0;  // offsets outside the call's rows
-  s.len = a.pc.len[p];
+  // none where the offsets fall or leave the call's rows (compared before they are subtracted: a fall of more than
+  // 2^27 tokens times 16 heads would come out positive)
+  const bool ok = s.tok0 >= 0 && end >= s.tok0 && end <= a.n_tok && end - s.tok0 <= a.max_q;
+  s.n_tok = ok ? end - s.tok0 : 0;
+  s.len = max(a.pc.len[p], 0);
   s.cap = (int)min((int64_t)a.pc.table_stride << a.pc.shift, (int64_t)a.pc.max_len);
   return s;
 }

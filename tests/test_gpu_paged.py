@@ -658,6 +658,35 @@ def test_attention_strided_queries_and_wide_bounds():
     assert torch.equal(o[:5], out[:5]) and (o[5:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("max_q,max_len", [(2, 300), (2, 2000), (9, 300), (9, 2000)])
+def test_attention_of_offsets_that_are_none(dtype, max_q, max_len):
+    """Offsets that fall, by so much that the number of columns leaves 32 bits, or lie anywhere: the problems
+    between them are left out, and the ones beside them are not."""
+    import torch
+    rng = _rng(41, max_q)
+    lens = [40, 50, 60, 33, 70, 80, 90]
+    pc = _cache(rng, dtype, "e4m3", 32, 2, 64, 16, lens, max_len=max_len)
+    if max_len > 300:  # splits: a table of as many blocks
+        wide = torch.full((len(lens), 125), -1, dtype=torch.int32, device="cuda")
+        wide[:, :pc.table.shape[1]] = pc.table
+        pc = _lib.PagedCache(dtype, 32, pc.k, pc.v, pc.k_scale, pc.v_scale, wide, pc.lens, max_len)
+    q = _q(rng, 12, 32, 64, dtype)
+    big = (1 << 27) + 1
+    off = torch.tensor([0, 2, big, 0, (1 << 31) - 1, -(1 << 31), 10, 12], dtype=torch.int32, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    nb = _lib.paged_attention_workspace_bytes(pc, 12, max_q)
+    assert (nb > 0) == (max_len > 1000)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda") if nb else None
+    _say("attention offsets", dtype, max_q, max_len)
+    _lib.paged_attention(pc, q, 0.1, out, off, max_q, ws)
+    assert (out[2:10] == 7).all()
+    first = _lib.PagedCache(dtype, 32, pc.k, pc.v, pc.k_scale, pc.v_scale, pc.table[:1], pc.lens[:1], max_len)
+    last = _lib.PagedCache(dtype, 32, pc.k, pc.v, pc.k_scale, pc.v_scale, pc.table[6:], pc.lens[6:], max_len)
+    _check(first, q[:2], 0.1, [2], out[:2], "first", max_q)
+    _check(last, q[10:], 0.1, [2], out[10:], "last", max_q)
+
+
 def test_binding_refuses_overlapping_tokens_and_other_types():
     import torch
     rng = _rng(32)
