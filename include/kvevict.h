@@ -404,7 +404,9 @@ int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, 
  *     127 s (KV_INT8) over the block's finite elements (at least 2^-126), 0 for zeros; a code is x / s
  *     rounded to nearest even.  An infinity takes the largest code of its sign; a NaN stays one
  *     in KV_E4M3 and becomes 0 in KV_INT8.
- *     Attention and appending take scales of 0 and powers of two from 2^-126 on; others are undefined.
+ *     Appending takes scales of 0 and powers of two from 2^-126 on; others are undefined.  Attention takes any
+ *     finite scale with fp32 queries or max_q h_q / h_kv <= 32; with more bf16 columns a block with another
+ *     scale gives NaN to the tokens that see it.
  *   - A table entry outside [0, n_blocks) is a missing block: its rows are not written, and not seen.
  *   - Rows of a block that no problem has written may hold anything.
  * dtype: of queries, new rows and outputs.  n_blocks * block_rows and table_stride * block_rows below

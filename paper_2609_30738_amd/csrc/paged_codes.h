@@ -33,6 +33,12 @@ template <int QT> __device__ __forceinline__ float block_scale(uint32_t amax_bit
 // 1 / s (exact for a scale as block_scale gives it); 1 for 0, whose block has no finite value but 0.
 __device__ __forceinline__ float inv_scale(float s) { return s > 0.f ? 1.f / s : 1.f; }
 
+// Whether s is a scale as block_scale gives it.
+__device__ __forceinline__ bool is_scale(float s) {
+  const uint32_t u = __float_as_uint(s);
+  return (u & 0x807FFFFFu) == 0 && u != 0x7F800000u;
+}
+
 // Four values in units of the scale as codes, rounded to nearest even.  kFinite: the values are finite and
 // at most the largest code; else infinities saturate, and a NaN stays one in e4m3 and becomes 0 in int8.
 template <int QT, bool kFinite> __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {

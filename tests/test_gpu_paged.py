@@ -603,6 +603,38 @@ def test_attention_of_nan_queries_and_scales():
     _check(pc, q, 0.1, None, _attend(pc, q, 0.1), "zeros")
 
 
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("dtype,qtype,d,R,G", [("bf16", "e4m3", 128, 16, 4), ("bf16", "int8", 64, 64, 4),
+                                               ("bf16", "int8", 128, 32, 1), ("f32", "e4m3", 64, 32, 4)])
+def test_attention_of_other_scales(dtype, qtype, d, R, G, which):
+    """Scales that are no powers of two (another coder's): taken as they are for up to 32 columns and fp32; a
+    turn of more gives NaN to the tokens that see the block, and to no others."""
+    import torch
+    rng = _rng(33, d, R)
+    L, j = 333, 3
+    for n, max_len in ((2, None), (8, 2000), (L, None), (L, 4000)):
+        pc = _cache(rng, dtype, qtype, 2 * G, 2, d, R, [L, 90])
+        if max_len:
+            wide = torch.full((2, max_len // R), -1, dtype=torch.int32, device="cuda")
+            wide[:, :pc.table.shape[1]] = pc.table
+            pc = _lib.PagedCache(dtype, 2 * G, pc.k, pc.v, pc.k_scale, pc.v_scale, wide, pc.lens, max_len)
+        b = int(pc.table[0, j])
+        scale = pc.k_scale if which == "k" else pc.v_scale
+        scale[b] *= 1.37
+        n_q = [n, min(n, 90)]
+        q = _q(rng, sum(n_q), 2 * G, d, dtype)
+        _say("attention other scales", dtype, qtype, d, R, which, n, max_len)
+        out = _attend(pc, q, 0.1, n_q)
+        if dtype == "f32" or n * G <= 32:
+            _check(pc, q, 0.1, n_q, out, "as they are")
+            continue
+        sees = torch.arange(n, device="cuda") + L - n >= j * R
+        assert torch.isnan(out[:n][sees]).all() and not torch.isnan(out[:n][~sees]).any()
+        m = int((~sees).sum())  # the tokens before the block are a turn of their own
+        pc.lens[0] = m
+        _check(pc, torch.cat([q[:m], q[n:]]), 0.1, [m, n_q[1]], torch.cat([out[:m], out[n:]]), "before it", max_q=n)
+
+
 @pytest.mark.parametrize("dtype,qtype", [("bf16", "e4m3"), ("f32", "int8")])
 def test_attention_rising_logits(dtype, qtype):
     """Logits that rise by tens of octaves along the rows: the reference is raised many times."""
