@@ -455,7 +455,7 @@ int kv_paged_tables(const kv_paged_cache* pc, const int32_t* len_in, const int32
 
 /* New rows into the blocks: token t's row of head g, k_new / v_new + t * tok_stride + g * d elements
  * (tok_stride 0: h_kv * d; at least that, at most 2^26, and whole 16-byte chunks), into slot slots[t] (as
- * kv_paged_tables gives them; one outside [0, n_blocks * block_rows) is skipped).  Tokens of one block have to be
+ * kv_paged_tables gives them; one outside [0, n_blocks * block_rows) is skipped), n_tok >= 1.  Tokens of one block have to be
  * consecutive in the batch, in consecutive slots, the first behind the block's rows in use; each block
  * once in a call.  A block's first row sets its scale; where later rows need a larger scale, the codes
  * of the rows it holds are rounded to that.  Rows behind the last new one stay as they were. */
@@ -478,7 +478,7 @@ size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_to
 /* Attention of the last tokens of every problem over its cache (one generated token, a few drafted ones, or
  * a further prompt turn; their own rows are in the cache already).  Problem p has the tokens
  * tok_off[p] .. tok_off[p+1] - 1 (n_p of them, at most max_q; tok_off [n_prob + 1] on the device, NULL:
- * one token each, then n_tok = n_prob and max_q = 1).  Token j of problem p sees the rows
+ * one token each, then n_tok = n_prob and max_q = 1; 1 <= max_q <= n_tok).  Token j of problem p sees the rows
  * r <= len[p] - n_p + j:
  *   out[t,h,:] = sum_r softmax_r(scale <q[t,h], k[r]>) v[r],  kv head h / (h_q / h_kv);
  * 0 where it sees none.  q: token t at t * q_stride elements (0: h_q * d; at least that, at most 2^26, whole

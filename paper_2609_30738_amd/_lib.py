@@ -611,14 +611,15 @@ def paged_tables(pc: PagedCache, len_in, add, free_blocks, taken_in, taken_out, 
 
 def paged_append(pc: PagedCache, k_new, v_new, slots, stream=None) -> None:
     """kv_paged_append: k_new, v_new [tokens, h_kv, d], tokens of one stride (slices of a projection's
-    output, for instance); slots [tokens] int32."""
+    output, for instance); slots [tokens] int32.  No tokens: nothing to do."""
     kp, ks = pc._rows(k_new, pc.h_kv, "k_new")
     vp, vs = pc._rows(v_new, pc.h_kv, "v_new")
     n = k_new.shape[0]
     if v_new.shape[0] != n or ks != vs:
         raise ValueError("k_new and v_new must have one shape and token stride")
-    _check(lib().kv_paged_append(pc._ref, kp, vp, ks, pc._arg(slots, pc._int32, n, "slots"), n, pc._stream(stream)),
-           "kv_paged_append")
+    sp, st = pc._arg(slots, pc._int32, n, "slots"), pc._stream(stream)
+    if n:
+        _check(lib().kv_paged_append(pc._ref, kp, vp, ks, sp, n, st), "kv_paged_append")
 
 
 def paged_compact(batch: Batch, k, v, sel_idx, budget: int, keep_tail: int, pc: PagedCache,
@@ -640,15 +641,16 @@ def paged_attention_workspace_bytes(pc: PagedCache, n_tok: Optional[int] = None,
 def paged_attention(pc: PagedCache, q, scale: float, out, tok_off=None, max_q: int = 1, ws=None,
                     stream=None) -> None:
     """kv_paged_attention: q [tokens, h_q, d] (tokens of one stride), out the same shape, contiguous;
-    tok_off [n_prob + 1] int32 for several tokens to a problem, at most max_q each."""
+    tok_off [n_prob + 1] int32 for several tokens to a problem, at most max_q each.  With tok_off no tokens
+    at all are nothing to do."""
     qp, qs = pc._rows(q, pc.h_q, "q")
     if out.shape != q.shape:
         raise ValueError("out must have the shape of q")
-    _check(lib().kv_paged_attention(pc._ref, qp, qs, pc._arg(tok_off, pc._int32, pc.n_prob + 1, "tok_off"),
-                                    q.shape[0], max_q, scale, pc._arg(out, pc.rows_dtype, 0, "out"),
-                                    None if ws is None else pc._arg(ws, ws.dtype, 0, "ws"),
-                                    0 if ws is None else ws.numel() * ws.element_size(), pc._stream(stream)),
-           "kv_paged_attention")
+    n, off, op = q.shape[0], pc._arg(tok_off, pc._int32, pc.n_prob + 1, "tok_off"), pc._arg(out, pc.rows_dtype, 0, "out")
+    wp, st = None if ws is None else pc._arg(ws, ws.dtype, 0, "ws"), pc._stream(stream)
+    if n or off is None:
+        _check(lib().kv_paged_attention(pc._ref, qp, qs, off, n, max_q, scale, op, wp,
+                                        0 if ws is None else ws.numel() * ws.element_size(), st), "kv_paged_attention")
 
 
 def pyramid_budgets(budget: int, n_layers: int, beta: float) -> np.ndarray:

@@ -745,6 +745,32 @@ def test_binding_refuses_overlapping_tokens_and_other_types():
         _lib.paged_attention(far, q, 0.1, out, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
 
 
+def test_steps_without_tokens():
+    """A step in which no request gets a row: tables, appending and attention take it, and change nothing;
+    arguments of other types are refused all the same."""
+    import torch
+    rng = _rng(42)
+    pc = _cache(rng, "bf16", "e4m3", 4, 2, 64, 16, [20, 30])
+    codes, scales = _image(pc)
+    none = torch.zeros(2, dtype=torch.int32, device="cuda")
+    to, bo = (torch.empty(3, dtype=torch.int32, device="cuda") for _ in range(2))
+    slots = torch.empty(0, dtype=torch.int32, device="cuda")
+    qkv = torch.empty(0, 8, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty(0, 4, 64, dtype=torch.bfloat16, device="cuda")
+    _say("no tokens")
+    _lib.paged_tables(pc, pc.lens, none, None, None, None, to, bo, slots)
+    _lib.paged_append(pc, qkv[:, 4:6], qkv[:, 6:], slots)
+    _lib.paged_attention(pc, qkv[:, :4], 0.1, out, to, 1)
+    assert pc.lens.tolist() == [20, 30] and to.tolist() == bo.tolist() == [0, 0, 0]
+    _same_image(pc, codes, scales, "no tokens")
+    with pytest.raises(ValueError):
+        _lib.paged_append(pc, qkv[:, 4:6].float(), qkv[:, 6:], slots)
+    with pytest.raises(ValueError):
+        _lib.paged_attention(pc, qkv[:, :4], 0.1, out.float(), to, 1)
+    with pytest.raises(_lib.KvError):  # one token each, and there are none
+        _lib.paged_attention(pc, qkv[:, :4], 0.1, out)
+
+
 def test_attention_past_32_bit_offsets():
     """Blocks whose codes lie past 4 GiB of the pool, written and read."""
     import torch
