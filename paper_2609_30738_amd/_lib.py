@@ -531,7 +531,10 @@ class PagedCache:
         if table.dim() != 2 or lens.numel() != table.shape[0]:
             raise ValueError("table must be [n_prob, table_stride] and lens [n_prob]")
         self.table, self.lens, self.device = table, lens, table.device
-        self._int32, self._torch_c = torch.int32, torch._C
+        self._int32, self._current_device = torch.int32, torch.cuda.current_device
+        # (torch.cuda.current_stream() makes an object of the stream: 3 us of a call of 9)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                                   lambda index: torch.cuda.current_stream(index).cuda_stream)
         self.n_prob = table.shape[0]
         self.struct = KvPagedCache(n_prob=self.n_prob, block_rows=int(block_rows), n_blocks=int(n_blocks),
                                    table_stride=table.shape[1], table=self._arg(table, torch.int32, 0, "table"),
@@ -585,10 +588,9 @@ class PagedCache:
     def _stream(self, stream):
         """The stream to launch on: kernels go to the current device, which has to be the cache's."""
         index = self.device.index
-        if index != self._torch_c._cuda_getDevice():
+        if index != self._current_device():
             raise ValueError(f"the cache is on {self.device}, which is not the current device")
-        # (torch.cuda.current_stream() makes an object of it: 3 us of a call of 9)
-        return self._torch_c._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+        return self._raw_stream(index) if stream is None else stream.cuda_stream
 
 
 def paged_tables(pc: PagedCache, len_in, add, free_blocks, taken_in, taken_out, tok_off, blk_off, slots,

@@ -745,6 +745,18 @@ def test_binding_refuses_overlapping_tokens_and_other_types():
         _lib.paged_attention(far, q, 0.1, out, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
 
 
+def test_streams(monkeypatch):
+    """The current stream and one that is given, with torch's raw stream query and without it."""
+    import torch
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(2):
+        pc = _lib.PagedCache.for_tables(16, 4, _dev(np.zeros((2, 2), np.int32)), _dev(np.zeros(2, np.int32)))
+        with torch.cuda.stream(side):
+            assert pc._stream(None) == side.cuda_stream and pc._stream(other) == other.cuda_stream
+        assert pc._stream(None) == torch.cuda.current_stream().cuda_stream
+        monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+
+
 def test_steps_without_tokens():
     """A step in which no request gets a row: tables, appending and attention take it, and change nothing;
     arguments of other types are refused all the same."""
