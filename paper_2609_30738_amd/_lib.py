@@ -531,8 +531,10 @@ class PagedCache:
         if table.dim() != 2 or lens.numel() != table.shape[0]:
             raise ValueError("table must be [n_prob, table_stride] and lens [n_prob]")
         self.table, self.lens, self.device = table, lens, table.device
-        self._int32, self._current_device = torch.int32, torch.cuda.current_device
-        # (torch.cuda.current_stream() makes an object of the stream: 3 us of a call of 9)
+        self._int32 = torch.int32
+        # the queries under torch.cuda's where this torch has them (torch.cuda.current_stream() makes an object of
+        # the stream: 3 us of a call of 9)
+        self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                                    lambda index: torch.cuda.current_stream(index).cuda_stream)
         self.n_prob = table.shape[0]
