@@ -486,7 +486,9 @@ size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_to
  * the product with V with 24 significant bits (fp32 queries), 16 (bf16 and max_q h_q / h_kv <= 16) or as
  * bf16 (more).  The outputs of
  * tokens outside every problem (a padded batch) stay as they were, and so do a problem's whose tok_off reaches outside
- * [0, n_tok], falls or spans more than max_q.  Calls that overlap on one workspace race. */
+ * [0, n_tok], falls or spans more than max_q.  Turns that a launch does not take are refused (KV_ERR_SHAPE): with fp32
+ * queries h_kv ceil(max_q (h_q / h_kv) / 32) > 65535 (8 kv heads of 4: 65,528 tokens go), with bf16 ones
+ * ceil(max_q (h_q / h_kv) / 256) ceil(max_len / (4096 block_rows)) > 65535, and max_q > 2^24.  Calls that overlap on one workspace race. */
 int kv_paged_attention(const kv_paged_cache* pc, const void* q, int64_t q_stride, const int32_t* tok_off,
                        int32_t n_tok, int32_t max_q, float scale, void* out, void* ws, size_t ws_bytes,
                        void* stream);

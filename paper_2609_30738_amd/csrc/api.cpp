@@ -843,7 +843,7 @@ int check_tokens(const kv::Paged& pc, int32_t n_tok, int32_t max_q, kv::PagedPla
   if (n_tok < 1 || max_q < 1 || max_q > n_tok) return KV_ERR_ARG;
   if (max_q > kMaxLen) return KV_ERR_SHAPE;
   *plan = kv::paged_plan(pc, max_q);
-  return kv::paged_grid_y(pc, max_q, *plan) > kMaxGrid ? KV_ERR_SHAPE : KV_OK;
+  return kv::paged_grid_groups(pc, max_q, *plan) > kMaxGrid ? KV_ERR_SHAPE : KV_OK;
 }
 
 // kv_paged_tables' arrays.  in_place: whether an input is written as an output, in one of the ways that the header

@@ -68,8 +68,10 @@ struct PagedPlan {
   int split_rows, n_split, prompt_waves;
 };
 PagedPlan paged_plan(const Paged& pc, int max_q);
-// Workgroups along the grid's second axis (at most 65535).
-int64_t paged_grid_y(const Paged& pc, int max_q, const PagedPlan& plan);
+// Workgroups along the grid axis that the columns are on: the second one of paged_prompt.hip's kernel, with its splits,
+// the first one of paged_attention.hip's, with the kv heads.  At most 65535: the limit of a second axis, and on the
+// first what keeps the join's launch (256 threads a column) far below 2^32 threads.
+int64_t paged_grid_groups(const Paged& pc, int max_q, const PagedPlan& plan);
 size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t stream);
 // Blocks of a split that the prompt kernel of so many waves holds in LDS beside its tiles

@@ -538,7 +538,7 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
   return plan;
 }
 
-int64_t paged_grid_y(const Paged& pc, int max_q, const PagedPlan& plan) {
+int64_t paged_grid_groups(const Paged& pc, int max_q, const PagedPlan& plan) {
   const int64_t cols = (int64_t)max_q * pc.group();
   if (plan.prompt_waves) return (cols + 32 * plan.prompt_waves - 1) / (32 * plan.prompt_waves) * plan.n_split;
   return (int64_t)pc.h_kv * column_groups(max_q, pc.group());

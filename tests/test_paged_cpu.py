@@ -111,6 +111,23 @@ def test_attention_checks():
     assert _attend(c, stride=4095) == _attend(c, stride=4100) == _attend(c, stride=-8) == _lib.KV_ERR_ARG
 
 
+def test_attention_of_the_longest_turns():
+    """The largest turns that the launches take, by the workspace that they ask for, and one token more."""
+    f = lambda c, n: _lib.lib().kv_paged_attention_workspace_bytes(ctypes.byref(c), n, n)  # noqa: E731
+    # a unit's 4 columns a token, 8 heads: 8191 groups of 32 columns
+    c = _cache(dtype=_lib.KV_F32, n_blocks=1000, table_stride=1000, max_len=16000)
+    most = 8191 * 32 // 4
+    assert f(c, most) == -(-most * 32 * 8 * 130 * 4 // 256) * 256 and f(c, most + 1) == 0
+    assert _attend(ctypes.byref(c), n_tok=most + 1, max_q=most + 1) == _lib.KV_ERR_SHAPE
+    assert _attend(ctypes.byref(c), n_tok=most, max_q=most, ws_bytes=0) == _lib.KV_ERR_WORKSPACE
+    # two splits of 65536 rows: 32767 groups of 256 columns
+    c = _cache(n_blocks=8192, table_stride=8192, max_len=131072)
+    most = 32767 * 256 // 4
+    assert f(c, most) == -(-most * 32 * 2 * 130 * 4 // 256) * 256 and f(c, most + 1) == 0
+    assert _attend(ctypes.byref(c), n_tok=most + 1, max_q=most + 1) == _lib.KV_ERR_SHAPE
+    assert _attend(ctypes.byref(c), n_tok=most, max_q=most, ws_bytes=0) == _lib.KV_ERR_WORKSPACE
+
+
 def test_attention_scale_times_log2e():
     """The largest scales are finite and their product with log2(e) is not."""
     for scale in (2.4e38, -2.4e38, 3.4e38):
