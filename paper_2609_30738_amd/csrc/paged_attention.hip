@@ -21,7 +21,7 @@
 //   151 us, now 121, 16 of up to 32768 146, now 118).
 //   The four waves are merged through LDS; with several splits the partial sums go to the workspace and
 //   paged_combine_kernel joins them.
-//   Bound by the cache's reads: one token over 32 caches of 32768 rows (e4m3, 8 heads of 128, 2.0 GB) 336 us, 6.0 TB/s
+//   Bound by the cache's reads: one token over 32 caches of 32768 rows (e4m3, 8 heads of 128, 2.0 GB) 335 us, 6.0 TB/s
 //   of the 6.9 that streaming reads reach here; 24 ragged ones of up to 24001 rows (int8, eight query heads to a
 //   kv head, 0.66 GB) 137 us, 4.8 TB/s: the last splits of unequal caches leave CUs idle; over 32 caches of 100 rows
 //   6.0 us, fp32 over four of 4097 rows 11.7 us with the join: latency.
@@ -87,7 +87,7 @@ __device__ __forceinline__ float column_sum(float v) {
 }
 
 // A load with the non-temporal bit where one workgroup alone reads a row (up to 16 columns, one group of them):
-// 32 caches of 32768 rows 346 us, 370 without it.
+// 32 caches of 32768 rows 335 us, 363 without it.
 template <bool kOnce, typename T> __device__ __forceinline__ T load_code(const T* p) {
   return kOnce ? __builtin_nontemporal_load(p) : *p;
 }
@@ -522,10 +522,13 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
     n = std::max<int64_t>(1, std::min<int64_t>(256 / units, (rows + 511) / 512));
   } else {
     // Up to 512 rows a unit stays whole (500 rows of 64 units 8.2 us whole, 9.1 split and joined; of 512 units 15.1
-    // and 22.3).  Longer ones get three rounds of the 768 workgroups that fit the chip at once, so that caches of
-    // unequal length even out (64 of up to 16384 rows and 2 heads 64 us, in two rounds 71, 32 of up to 4000 37.5 and
-    // 41.1; but 24 of 13000 rows each 126 and 120), in splits of at least 512 rows; or where these are few, 512
-    // workgroups of at least 256 rows (8 units of 2000 rows 9.4 us, in splits of 512 rows 12.0; of 32768 rows in
+    // and 22.3).  Longer ones get 2304 workgroups in splits of at least 512 rows.  That is three rounds of the 768 that
+    // fit the chip with one column tile (bf16, d = 128), so that caches of unequal length even out: 24 of up to 16001
+    // rows 91 us, with 1536 104, 64 of up to 16384 and 2 heads 64 and 71, 32 of up to 4000 37.5 and 41.1; caches of one
+    // length pay for it, 24 of 13000 rows 109 and 105.  Two column tiles let 512 fit, fp32 512 and 256, d = 64 more.  The
+    // number is the same for all: five tokens over 16 caches of up to 6001 rows 42 us, as with 768 to 3456 (fp32 80, with
+    // 768 74), over 24 of up to 24001 168 and with 1536 167, over 24 of 13000 150 and 137, one fp32 token over 24 of up
+    // to 16001 100 and 104.  Where the splits are few, 512 workgroups of at least 256 rows (8 units of 2000 rows 9.4 us, in splits of 512 rows 12.0; of 32768 rows in
     // 128 splits 25.9 us, in 64 20.2).
     units = (int64_t)pc.n_prob * pc.h_kv * column_groups(max_q, pc.group());
     auto splits = [&](int64_t wgs, int64_t least) { return std::min(wgs / units, (rows + least - 1) / least); };
