@@ -603,6 +603,70 @@ def test_attention_of_nan_queries_and_scales():
     _check(pc, q, 0.1, None, _attend(pc, q, 0.1), "zeros")
 
 
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 6, 40, 200])
+def test_attention_of_queries_that_are_no_numbers(dtype, n, split):
+    """NaN and infinite queries, over whole rows and over splits, for every kernel: NaN in their tokens and heads
+    alone."""
+    import torch
+    rng = _rng(43, n)
+    lens = [210, 700 if split else 450]
+    pc = _cache(rng, dtype, "e4m3", 4, 2, 128, 16, lens)
+    n_q = [n, max(1, n - 1)]
+    q = _q(rng, sum(n_q), 4, 128, dtype)
+    assert (_lib.paged_attention_workspace_bytes(pc, len(q), n) > 0) == split
+    bad = torch.zeros(len(q), 4, dtype=torch.bool, device="cuda")
+    for t, h, x in ((0, 2, np.nan), (n // 2, 1, np.inf), (len(q) - 1, 3, -np.inf), (len(q) - 1, 0, np.nan)):
+        q[t, h, (7 * t + h) % 128] = x
+        bad[t, h] = True
+    _say("attention NaN queries", dtype, n, split)
+    out = _attend(pc, q, 0.1, n_q)
+    assert torch.equal(torch.isnan(out).all(-1), bad) and torch.equal(torch.isnan(out).any(-1), bad)
+    q[bad] = 0.5
+    same = _attend(pc, q, 0.1, n_q)
+    _check(pc, q, 0.1, n_q, torch.where(bad[..., None], same, out), "the others")
+
+
+@pytest.mark.parametrize("profile", ["rising", "alternating", "late"])
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("dtype,qtype,d", [("bf16", "e4m3", 64), ("bf16", "int8", 128), ("bf16", "e4m3", 128),
+                                           ("f32", "e4m3", 64)])
+def test_attention_of_moving_logits(dtype, qtype, d, split, profile):
+    """Logits that move by tens of octaves from one 32 rows to the next, up for some columns of a wave and
+    down or hardly at all for others: the reference moves again and again, between tiles and between the
+    halves of one.  Few tokens, and turns that four and eight waves take."""
+    import torch
+    rng = _rng(44, d)
+    L = 900 if split else 470
+    pc = _cache(rng, dtype, qtype, 4, 1, d, 32, [L, L - 45])
+    u = np.where(rng.random(d) < 0.5, -1.0, 1.0)
+    codes, _ = _image(pc)
+    pc.k_scale.fill_(0.5)
+    for p, rows in enumerate(pc.lens.tolist()):
+        half = np.arange(rows) // 32
+        if profile == "rising":
+            level = -60 + 120.0 * half / half.max()
+        elif profile == "alternating":
+            level = np.where(half % 2 == 0, 60.0, -60.0) * (0.5 + 0.5 * half / half.max())
+        else:
+            level = np.where(np.arange(rows) < rows - 30, -60.0, 60.0)
+        for r in range(rows):
+            t = int(pc.table[p, r // 32])
+            codes[0][t, 0, r % 32] = paged.encode(u * (level[r] + rng.integers(-2, 3, d)), 1.0, qtype)
+    pc.k.view(torch.uint8).copy_(_dev(codes[0]))
+    for n in (1, 9, 30, 90):
+        n_q = [n, max(1, n - 4)]
+        amp = rng.choice([1.0, -1.0, 0.5, 0.125, -0.03125], (sum(n_q), 4, 1))
+        q = _dev((u * amp).astype(np.float32), _dt(dtype))
+        assert (_lib.paged_attention_workspace_bytes(pc, len(q), n) > 0) == split
+        scale = 16.0 / d
+        _say("attention moving", dtype, qtype, d, split, profile, n)
+        out = _attend(pc, q, scale, n_q)
+        _check(pc, q, scale, n_q, out, f"{profile} n={n}")
+        assert torch.equal(out, _attend(pc, q, scale, n_q))  # the same bits again
+
+
 @pytest.mark.parametrize("which", ["k", "v"])
 @pytest.mark.parametrize("dtype,qtype,d,R,G", [("bf16", "e4m3", 128, 16, 4), ("bf16", "int8", 64, 64, 4),
                                                ("bf16", "int8", 128, 32, 1), ("f32", "e4m3", 64, 32, 4)])
