@@ -2,10 +2,10 @@
 //
 // A scale is a power of two (or 0: a block of zeros), the least one with max|x| <= 448 s for e4m3
 // and 127 s for int8 over the block's finite values.  A value is code * s: exact in bf16, whatever the
-// code.  A power of two costs e4m3 nothing (its precision does not depend on the scale) and
-// int8 up to one bit of its range; in return a block whose scale grows with a later row moves its codes
-// by whole binades, so that e4m3's normal numbers stay as they were, and the codes of given rows are the
-// same on every path.
+// code, while it is a normal number (e4m3's smallest code at scales below 2^-117 is not: it may become 0).
+// A power of two costs e4m3 nothing (its precision does not depend on the scale) and int8 up to one bit of
+// its range; in return a block whose scale grows with a later row moves its codes by whole binades, so that
+// e4m3's normal numbers stay as they were, and the codes of given rows are the same on every path.
 #pragma once
 
 #include <hip/hip_runtime.h>

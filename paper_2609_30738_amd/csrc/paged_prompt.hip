@@ -15,10 +15,11 @@
 //   The grid's fastest axis is the kv head: workgroups go to the 8 XCDs in turn, so that with 8 heads one L2
 //   holds one head's rows.  The last columns, which see the most rows, come first.
 //
-//   Bound by the matrix units, 43 % busy, and by the LDS beside them, whose operands a wave reads for itself.  Three
-//   prompts of up to 4096 tokens over caches of up to 16384 rows (32 heads over 8, d = 128): 1842 us, 1.05 PFLOP/s of
-//   the 1.58 that a large product reaches; 1144 us at d = 64, 1921 from int8.  At an earlier step (1900 us) the same
-//   without staging took 1612, without the operands' reads 1685, without both 1303, the products alone 785.
+//   Bound by the matrix units, 43 % busy, by the weights that they do not hide, and by the LDS beside them, whose
+//   operands a wave reads for itself.  Three prompts of up to 4096 tokens over caches of up to 16384 rows (32 heads
+//   over 8, d = 128): 1838 us, 1.06 PFLOP/s of the 1.58 that a large product reaches; 1135 us at d = 64, 1926 from
+//   int8.  At an earlier step (1900 us) the same without staging took 1612, without the operands' reads 1685, without
+//   both 1303, the products alone 785.
 //   Measured and left: V transposed as it is staged 2020 (then 1900), both halves' logits before the weights 1890
 //   (then 1842), masked and unmasked tiles as two copies of the code 2905 (then 2372), raised wave priority around the
 //   products 2005 (then 1900), the staging spread over the second product 1908, 64 columns a wave (half the operand
