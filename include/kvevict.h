@@ -406,7 +406,8 @@ int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, 
  *     in KV_E4M3 and becomes 0 in KV_INT8.
  *     Appending takes scales of 0 and powers of two from 2^-126 on; others are undefined.  Attention takes any
  *     finite scale with fp32 queries or max_q h_q / h_kv <= 32; with more bf16 columns a block with another
- *     scale gives NaN to the tokens that see it.
+ *     scale, or one above 2^119 (KV_E4M3: elements above 2.9e38) or 2^121 (KV_INT8: 3.3e38), gives NaN to the
+ *     tokens that see it.
  *   - A table entry outside [0, n_blocks) is a missing block: its rows are not written, and not seen.
  *   - Rows of a block that no problem has written may hold anything.
  * dtype: of queries, new rows and outputs.  n_blocks * block_rows and table_stride * block_rows below

@@ -33,10 +33,11 @@ template <int QT> __device__ __forceinline__ float block_scale(uint32_t amax_bit
 // 1 / s (exact for a scale as block_scale gives it); 1 for 0, whose block has no finite value but 0.
 __device__ __forceinline__ float inv_scale(float s) { return s > 0.f ? 1.f / s : 1.f; }
 
-// Whether s is a scale as block_scale gives it.
-__device__ __forceinline__ bool is_scale(float s) {
+// Whether s is a scale as block_scale gives it, and every code times it is finite in bf16: 448 2^119, 127 2^121 (blocks of
+// values near fp32's largest have a larger one, and 256 2^120 and 64 2^122 are 2^128).
+template <int QT> __device__ __forceinline__ bool is_bf16_scale(float s) {
   const uint32_t u = __float_as_uint(s);
-  return (u & 0x807FFFFFu) == 0 && u != 0x7F800000u;
+  return (u & 0x807FFFFFu) == 0 && s <= (QT == kQtE4m3 ? 0x1p119f : 0x1p121f);
 }
 
 // Four values in units of the scale as codes, rounded to nearest even.  kFinite: the values are finite and

@@ -145,10 +145,11 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
     int block = a.pc.table[(int64_t)p * a.pc.table_stride + (r0 >> shift) + i];
     if ((uint32_t)block >= (uint32_t)a.pc.n_blocks) block = -1;
     const int64_t unit = (int64_t)max(block, 0) * a.pc.h_kv + g;
-    // The conversion takes a scale's exponent alone: a block with another scale than block_scale's gives NaN
-    // logits, which reach the columns that see it, instead of other values without a word.
+    // The conversion takes a scale's exponent alone, and an infinity in V would reach columns that do not see it (as
+    // 0 times it): a block with another scale than block_scale's, or of values that leave bf16, gives NaN logits,
+    // which reach the columns that see it.
     const float ks = a.pc.k_scale[unit], vs = a.pc.v_scale[unit];
-    const bool ok = is_scale(ks) && is_scale(vs);
+    const bool ok = is_bf16_scale<QT>(ks) && is_bf16_scale<QT>(vs);
     blocks.id[i] = block;
     blocks.k_scale[i] = ok ? ks : NAN;
     blocks.v_scale[i] = ok && block >= 0 ? vs : 1.f;

@@ -699,6 +699,32 @@ def test_attention_of_other_scales(dtype, qtype, d, R, G, which):
         _check(pc, torch.cat([q[:m], q[n:]]), 0.1, [m, n_q[1]], torch.cat([out[:m], out[n:]]), "before it", max_q=n)
 
 
+@pytest.mark.parametrize("qtype,d", [("e4m3", 128), ("int8", 64)])
+@pytest.mark.parametrize("n", [200, 30])
+def test_attention_beside_the_largest_values(qtype, d, n):
+    """A block of values that round to 2^128, an infinity in bf16 and fp32 (rows of the type's lowest value, say):
+    NaN to the tokens of a turn that see it, nothing to the ones before it in the same tile."""
+    import torch
+    rng = _rng(45, d)
+    L, R = 200, 16
+    pc = _cache(rng, "bf16", qtype, 8, 2, d, R, [L, 90])
+    low = torch.full((L, 2, d), torch.finfo(torch.bfloat16).min, dtype=torch.bfloat16, device="cuda")
+    row = torch.randn(L, 2, d, device="cuda").to(torch.bfloat16)
+    j = 11
+    slots = int(pc.table[0, j]) * R + torch.arange(R, dtype=torch.int32, device="cuda")
+    _lib.paged_append(pc, row[:R], low[:R], slots)
+    n_q = [n, min(n, 90)]
+    q = _q(rng, sum(n_q), 8, d, "bf16")
+    _say("attention largest values", qtype, d, n)
+    out = _attend(pc, q, 0.1, n_q)
+    sees = torch.arange(n, device="cuda") + L - n >= j * R
+    assert sees.any() and not sees.all()
+    assert torch.isnan(out[:n][sees]).all() and torch.isfinite(out[:n][~sees]).all()
+    m = int((~sees).sum())
+    pc.lens[0] = L - n + m
+    _check(pc, torch.cat([q[:m], q[n:]]), 0.1, [m, n_q[1]], torch.cat([out[:m], out[n:]]), "before it", max_q=n)
+
+
 @pytest.mark.parametrize("dtype,qtype", [("bf16", "e4m3"), ("f32", "int8")])
 def test_attention_rising_logits(dtype, qtype):
     """Logits that rise by tens of octaves along the rows: the reference is raised many times."""
