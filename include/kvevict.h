@@ -72,6 +72,18 @@ extern "C" {
 #define KV_E4M3 0 /* OCP 8-bit floating point: 4 exponent bits, 3 mantissa bits, no infinities       */
 #define KV_INT8 1 /* -127 .. 127                                                                     */
 
+/* ---- 4-bit code type (kv_paged_cache) --------------------------------------------------------- */
+#define KV_E2M1 4 /* OCP 4-bit floating point: 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign; two to a byte  */
+
+/* ---- rotary positions (kv_rotary) ------------------------------------------------------------- */
+#define KV_ROTARY_HALF 0        /* pairs (i, i + rot_dim / 2)                                        */
+#define KV_ROTARY_INTERLEAVED 1 /* pairs (2 i, 2 i + 1)                                              */
+#define KV_ROTARY_PLAIN 0       /* frequencies f = base^(-2 i / rot_dim)                (no parameters) */
+#define KV_ROTARY_LINEAR 1      /* f / F                                                (F)          */
+#define KV_ROTARY_NTK 2         /* base F^(rot_dim / (rot_dim - 2)) instead of base     (F)          */
+#define KV_ROTARY_YARN 3        /* see kv_rotary_frequencies                            (F, L0, beta_fast, beta_slow) */
+#define KV_ROTARY_BANDS 4       /* see kv_rotary_frequencies                            (F, L0, low, high)            */
+
 /* ---- depth-profile families (section 3.3) ----------------------------------------------------- */
 #define KV_PROFILE_GLOBAL 0   /* a(l) = a0                                   (1 parameter)      */
 #define KV_PROFILE_SEGMENTS 1 /* a(l) = a[floor(n_seg * l / n_layers)]       (n_seg parameters) */
@@ -392,10 +404,10 @@ int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, 
                         const void* k_new, const void* v_new, float scale, float* out, void* ws,
                         size_t ws_bytes, void* stream);
 
-/* A batch of caches held in 8 bits, in blocks that the problems share (section 4.3's generation over
+/* A batch of caches held in 8 or 4 bits, in blocks that the problems share (section 4.3's generation over
  * the kept rows, for caches of unequal and growing length).  A block holds block_rows rows (16, 32, 64 or
  * 128) of every kv head: pools k, v [n_blocks][h_kv][block_rows][d] of 8-bit codes (KV_E4M3 or
- * KV_INT8) and scales k_scale, v_scale [n_blocks][h_kv] fp32; an element is code * scale.  Row r of
+ * KV_INT8) and scales k_scale, v_scale [n_blocks][h_kv] fp32; an element is code * scale (KV_E2M1: below).  Row r of
  * problem p is row r % block_rows of block table[p][r / block_rows] (table [n_prob][table_stride],
  * len [n_prob]: the rows in use).  Every pointer is a device pointer, and table and len are read on
  * the device alone: they may change between the replays of a captured graph.  max_len bounds
@@ -408,11 +420,16 @@ int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, 
  *     finite scale with fp32 queries or max_q h_q / h_kv <= 32; with more bf16 columns a block with another
  *     scale, or one above 2^119 (KV_E4M3: elements above 2.9e38) or 2^121 (KV_INT8: 3.3e38), gives NaN to the
  *     tokens that see it.
+ *   - KV_E2M1: pools [n_blocks][h_kv][block_rows][d / 2] bytes, element 2 i in the low half of byte i, and scales
+ *     [n_blocks][h_kv][d / 32][block_rows] bytes b, one for 32 elements of a row: an element is code * 2^(b - 127).  A written
+ *     byte is the least with max|x| <= 6 2^(b - 127) over the 32 elements' finite ones, at least 2 and at most 252 (larger
+ *     elements, above 2.5e38, become 6 2^125); a code is nearest, ties to the even one.  An infinity takes the largest code of its
+ *     sign, a NaN becomes 0.  Reading takes any byte (above 252 as 252).  No row's codes depend on another row.
  *   - A table entry outside [0, n_blocks) is a missing block: its rows are not written, and not seen.
  *   - Rows of a block that no problem has written may hold anything.
  * dtype: of queries, new rows and outputs.  n_blocks * block_rows and table_stride * block_rows below
  * 2^31, h_q / h_kv <= 16, h_kv <= 4096, d in {64, 128}, max_len <= 2^24, else KV_ERR_SHAPE; pools
- * 16-byte aligned.  kv_paged_tables uses n_prob, block_rows, n_blocks, table_stride, table and len
+ * 16-byte aligned, and so are KV_E2M1's scales.  kv_paged_tables uses n_prob, block_rows, n_blocks, table_stride, table and len
  * alone. */
 typedef struct kv_paged_cache {
   int32_t dtype;
@@ -427,8 +444,8 @@ typedef struct kv_paged_cache {
   int32_t max_len;
   void* k;
   void* v;
-  float* k_scale;
-  float* v_scale;
+  void* k_scale; /* float (KV_E4M3, KV_INT8) or uint8_t (KV_E2M1) */
+  void* v_scale;
   int32_t* table;
   int32_t* len;
 } kv_paged_cache;
@@ -459,9 +476,57 @@ int kv_paged_tables(const kv_paged_cache* pc, const int32_t* len_in, const int32
  * kv_paged_tables gives them; one outside [0, n_blocks * block_rows) is skipped), n_tok >= 1.  Tokens of one block have to be
  * consecutive in the batch, in consecutive slots, the first behind the block's rows in use; each block
  * once in a call.  A block's first row sets its scale; where later rows need a larger scale, the codes
- * of the rows it holds are rounded to that.  Rows behind the last new one stay as they were. */
+ * of the rows it holds are rounded to that.  Rows behind the last new one stay as they were.  KV_E2M1: the tokens may come in any
+ * order, each slot once. */
 int kv_paged_append(const kv_paged_cache* pc, const void* k_new, const void* v_new, int64_t tok_stride,
                     const int32_t* slots, int32_t n_tok, void* stream);
+
+/* A rotation of rows by their positions: of a head's first rot_dim elements (a multiple of 16, at most d, KV_ERR_SHAPE),
+ * the pair i < rot_dim / 2 (a, b), by `layout`, at position p becomes
+ *   (a c - b s, b c + a s),  c = factor cos(p freq[i]),  s = factor sin(p freq[i]);
+ * elements from rot_dim on stay as they are.  inverse other than 0: by the angle -p freq[i], which is also the
+ * gradient of the rotation: of out's gradient it makes x's.  freq: rot_dim / 2 values in radians a position, doubles on the
+ * device; angles are formed in 64 bits, so that far positions (and negative ones) lose nothing; |p freq[i]| < 2^31.
+ * layout other than KV_ROTARY_HALF and KV_ROTARY_INTERLEAVED, or a factor that is not finite: KV_ERR_ARG. */
+typedef struct kv_rotary {
+  int32_t layout;
+  int32_t rot_dim;
+  int32_t inverse;
+  float factor;
+  const double* freq;
+} kv_rotary;
+
+/* Frequencies of a rotation, host-only: freq_host [rot_dim / 2] and factor_host [1] of a family, i < rot_dim / 2,
+ * f_i = base^(-2 i / rot_dim):
+ *   KV_ROTARY_PLAIN, _LINEAR, _NTK   as beside their names, factor 1;
+ *   KV_ROTARY_YARN    f_i ((1 - g) / F + g), g = 1 - clamp((i - lo) / max(hi - lo, 0.001), 0, 1), lo = max(floor(at(beta_fast)), 0),
+ *                     hi = min(ceil(at(beta_slow)), rot_dim - 1), at(b) = rot_dim ln(L0 / (2 pi b)) / (2 ln base);
+ *                     factor 0.1 ln F + 1;
+ *   KV_ROTARY_BANDS   f_i ((1 - t) / F + t), t = clamp((L0 f_i / (2 pi) - low) / (high - low), 0, 1), factor 1.
+ * rot_dim even and at least 2 (NTK: 4), base > 1, F >= 1, L0 > 0, beta_fast > beta_slow > 0, high > low > 0, all
+ * finite, and the family's number of parameters, else KV_ERR_ARG. */
+int kv_rotary_frequencies(int32_t family, double base, const double* params_host, int32_t n_params,
+                          int32_t rot_dim, double* freq_host, float* factor_host);
+
+/* Rows rotated by their positions: token t's heads x + t * x_stride + h * d elements, h < heads, to
+ * out + t * out_stride + h * d, at position pos[t] (pos [n_tok] on the device).  dtype of x and out; the products in fp32, rounded
+ * once.  Strides as in kv_paged_append (0: heads * d).  out may be x with x's stride; any other overlap of their rows is
+ * KV_ERR_ARG.  d in {64, 128}, heads >= 1, 1 <= n_tok <= 2^25. */
+int kv_rotate(const kv_rotary* rot, int32_t dtype, int32_t heads, int32_t d, const void* x, int64_t x_stride,
+              const int32_t* pos, int32_t n_tok, void* out, int64_t out_stride, void* stream);
+
+/* kv_paged_append of rotated keys, at positions pos [n_tok] (a row's place in a cache that was evicted is not its position):
+ * k_new is rotated in fp32 and coded from there, as kv_rotate of fp32 rows and kv_paged_append would, v_new as it is.  q
+ * (nullable): every token's queries are rotated too, as kv_rotate does from q to q_out, whatever the token's slot.  n_tok <= 2^25. */
+int kv_paged_append_rotated(const kv_paged_cache* pc, const kv_rotary* rot, const int32_t* pos, const void* q, int64_t q_stride,
+                            void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new, int64_t tok_stride,
+                            const int32_t* slots, int32_t n_tok, void* stream);
+
+/* The caches' rows as contiguous keys and values, in kv_problem's layout, so that an eviction can run over them again:
+ * problem p's L_p = row_off[p + 1] - row_off[p] rows to k_out, v_out + row_off[p] * h_kv * d elements, [h_kv][L_p][d] of the cache's
+ * dtype (row_off [n_prob + 1] on the device).  Rows from len[p] on, and rows of missing blocks, are zeros.  A problem whose row_off reaches
+ * outside [0, n_rows], falls or spans more than max_len is left out.  k_out or v_out may be NULL, not both. */
+int kv_paged_rows(const kv_paged_cache* pc, const int64_t* row_off, int64_t n_rows, void* k_out, void* v_out, void* stream);
 
 /* kv_compact_cache_ex into the blocks (sections 1 and 3.1): rows 0 .. B_p - 1 of problem p and head g are
  * the rows of the selected positions in ascending order, then the last keep_tail positions, each block

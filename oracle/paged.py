@@ -1,10 +1,11 @@
-"""The 8-bit paged cache in plain numpy: codes and scales, block tables, appending, compaction and
-attention, from the definitions in include/kvevict.h, in float64.
+"""The 8- and 4-bit paged caches in plain numpy: codes and scales, block tables, appending, compaction, reading back
+and attention, from the definitions in include/kvevict.h, in float64.
 
 TEST INFRASTRUCTURE ONLY (see the package docstring).
 
 Codes are uint8 arrays of bit patterns (e4m3: sign, 4 exponent bits with bias 7, 3 mantissa bits, 0x7F
-and 0xFF not numbers; int8: two's complement).
+and 0xFF not numbers; int8: two's complement).  4-bit ones (e2m1: sign, 2 exponent bits with bias 1, 1 mantissa bit) lie
+two to a byte, their scales are the exponent bytes of powers of two.
 """
 from __future__ import annotations
 
@@ -132,6 +133,78 @@ def cache_rows(codes: np.ndarray, scale: np.ndarray, table: np.ndarray, n: int, 
     at = np.where(ok, ids, 0)
     x = values(codes[at], qtype) * scale[at].astype(np.float64)[..., None, None]
     x = x.transpose(1, 0, 2, 3).reshape(h_kv, -1, d)[:, :n]
+    return x, np.repeat(ok, R)[:n]
+
+
+# ---- 4 bits: codes [n_blocks, h_kv, R, d / 2], scale bytes [n_blocks, h_kv, d / 32, R]
+
+GROUP4 = 32
+
+
+def values4(codes: np.ndarray) -> np.ndarray:
+    """What packed codes [.., n] stand for, in units of their scales: [.., 2 n]."""
+    u = np.arange(16)
+    e, f = (u >> 1) & 3, (u & 1) / 2.0
+    table = np.where(e > 0, (1 + f) * 2.0 ** (e - 1), f) * np.where(u >= 8, -1.0, 1.0)
+    codes = np.asarray(codes, dtype=np.uint8)
+    return table[np.stack([codes & 15, codes >> 4], -1)].reshape(*codes.shape[:-1], 2 * codes.shape[-1])
+
+
+def scale_byte4(amax: float) -> int:
+    """The least b with amax <= 6 2^(b - 127), 2 <= b <= 252."""
+    b = 2
+    while b < 252 and amax > 6 * 2.0 ** (b - 127):
+        b += 1
+    return b
+
+
+def encode4(x: np.ndarray):
+    """Rows [.., d] -> packed codes [.., d / 2] and scale bytes [.., d / 32]: nearest, ties to the even code."""
+    x = np.asarray(x, dtype=np.float64)
+    parts = x.reshape(*x.shape[:-1], -1, GROUP4)
+    flat = parts.reshape(-1, GROUP4)
+    b = np.array([scale_byte4(finite_max(row)) for row in flat], np.uint8).reshape(parts.shape[:-1])
+    nan = np.isnan(parts)
+    y = np.where(nan, 0.0, np.clip(parts / 2.0 ** (b[..., None].astype(np.float64) - 127), -6.0, 6.0))
+    grid = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6.0])
+    a = np.abs(y)
+    hi = np.minimum(np.searchsorted(grid, a), 7)
+    lo = np.maximum(hi - 1, 0)
+    up = (a - grid[lo] > grid[hi] - a) | ((a - grid[lo] == grid[hi] - a) & (hi % 2 == 0))
+    code = (np.where(up, hi, lo) | np.where(np.signbit(y), 8, 0)).astype(np.uint8).reshape(x.shape)
+    return code[..., 0::2] | code[..., 1::2] << 4, b
+
+
+def append4(codes: np.ndarray, scale: np.ndarray, new: np.ndarray, slots: np.ndarray) -> None:
+    """append for 4 bits: every row by itself."""
+    n_blocks, _, R, _ = codes.shape
+    for t, s in enumerate(np.asarray(slots)):
+        if 0 <= s < n_blocks * R:
+            codes[s // R, :, s % R], scale[s // R, :, :, s % R] = encode4(new[t])
+
+
+def compact4(codes: np.ndarray, scale: np.ndarray, table: np.ndarray, x: np.ndarray, sel: np.ndarray, tail: int) -> None:
+    """compact for 4 bits."""
+    n_blocks, h_kv, R, _ = codes.shape
+    L = x.shape[1]
+    for g in range(h_kv):
+        pos = np.concatenate([np.sort(sel[g]), np.arange(L - tail, L)])
+        rows = np.where(((pos >= 0) & (pos < L))[:, None], x[g, np.clip(pos, 0, L - 1)], 0.0)
+        for r, row in enumerate(rows):
+            b = int(table[r // R])
+            if 0 <= b < n_blocks:
+                codes[b, g, r % R], scale[b, g, :, r % R] = encode4(row)
+
+
+def cache_rows4(codes: np.ndarray, scale: np.ndarray, table: np.ndarray, n: int):
+    """cache_rows for 4 bits."""
+    n_blocks, h_kv, R, half = codes.shape
+    ids = np.asarray(table[:-(-n // R)] if n else [], dtype=np.int64)
+    ok = (ids >= 0) & (ids < n_blocks)
+    at = np.where(ok, ids, 0)
+    s = 2.0 ** (np.minimum(scale[at], 252).astype(np.float64) - 127)  # [blocks, h_kv, d / 32, R]
+    x = values4(codes[at]) * np.repeat(s.swapaxes(2, 3), GROUP4, -1)
+    x = x.transpose(1, 0, 2, 3).reshape(h_kv, -1, 2 * half)[:, :n]
     return x, np.repeat(ok, R)[:n]
 
 

@@ -33,6 +33,12 @@ KV_BF16 = 1
 
 KV_E4M3 = 0
 KV_INT8 = 1
+KV_E2M1 = 4
+
+KV_ROTARY_HALF = 0
+KV_ROTARY_INTERLEAVED = 1
+ROTARY_LAYOUTS = {"half": KV_ROTARY_HALF, "interleaved": KV_ROTARY_INTERLEAVED}
+ROTARY_FAMILIES = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 
 KV_PROFILE_GLOBAL = 0
 KV_PROFILE_SEGMENTS = 1
@@ -52,7 +58,8 @@ SYMBOLS = ("kv_strerror", "kv_version", "kv_workspace_bytes", "kv_candidate_stri
            "kv_candidates_workspace_bytes", "kv_mmr_select_candidates", "kv_evict_pass",
            "kv_compact_cache", "kv_compact_cache_ex", "kv_decode_workspace_bytes",
            "kv_decode_attention", "kv_paged_tables", "kv_paged_append", "kv_paged_compact",
-           "kv_paged_attention", "kv_paged_attention_workspace_bytes", "kv_pyramid_budgets",
+           "kv_paged_attention", "kv_paged_attention_workspace_bytes", "kv_paged_append_rotated",
+           "kv_paged_rows", "kv_rotate", "kv_rotary_frequencies", "kv_pyramid_budgets",
            "kv_depth_profile")
 
 
@@ -79,6 +86,11 @@ class KvPagedCache(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "qtype", "n_prob", "h_q", "h_kv", "d", "block_rows",
                                               "n_blocks", "table_stride", "max_len")] + \
                [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "len")]
+
+
+class KvRotary(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("factor", ctypes.c_float), ("freq", ctypes.c_void_p)]
 
 
 class KvSelectOpts(ctypes.Structure):
@@ -150,6 +162,12 @@ def lib() -> ctypes.CDLL:
         h.kv_paged_attention_workspace_bytes.argtypes = [pc, i32, i32]
         h.kv_paged_attention_workspace_bytes.restype = sz
         h.kv_paged_attention.argtypes = [pc, vp, i64, vp, i32, i32, ctypes.c_float, vp, vp, sz, vp]
+        ro = ctypes.POINTER(KvRotary)
+        h.kv_rotate.argtypes = [ro, i32, i32, i32, vp, i64, vp, i32, vp, i64, vp]
+        h.kv_paged_append_rotated.argtypes = [pc, ro, vp, vp, i64, vp, i64, vp, vp, i64, vp, i32, vp]
+        h.kv_paged_rows.argtypes = [pc, vp, i64, vp, vp, vp]
+        h.kv_rotary_frequencies.argtypes = [i32, ctypes.c_double, ctypes.POINTER(ctypes.c_double), i32, i32,
+                                            ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)]
         h.kv_pyramid_budgets.argtypes = [i32, i32, ctypes.c_double, ctypes.POINTER(ctypes.c_int32)]
         h.kv_depth_profile.argtypes = [i32, ctypes.POINTER(ctypes.c_double), i32, i32,
                                        ctypes.POINTER(ctypes.c_float)]
@@ -159,6 +177,7 @@ def lib() -> ctypes.CDLL:
                      "kv_mmr_select_scored", "kv_window_candidates", "kv_mmr_select_candidates",
                      "kv_evict_pass", "kv_compact_cache", "kv_compact_cache_ex", "kv_decode_attention",
                      "kv_paged_tables", "kv_paged_append", "kv_paged_compact", "kv_paged_attention",
+                     "kv_rotate", "kv_paged_append_rotated", "kv_paged_rows", "kv_rotary_frequencies",
                      "kv_pyramid_budgets", "kv_depth_profile"):
             getattr(h, name).restype = ctypes.c_int
         _LIB = h
@@ -498,19 +517,60 @@ def decode_attention(cb: CacheBatch, q, k_cache, v_cache, k_new, v_new, scale: f
                                      _stream(stream)), "kv_decode_attention")
 
 
-class PagedCache:
-    """A batch of 8-bit caches in shared blocks (kv_paged_cache), around the caller's device tensors:
+def _token_rows(t, dtype, device, heads: int, d: int, name: str):
+    """Address and token stride of [tokens, heads, d] rows; tokens may lie apart (slices of a projection)."""
+    shape = t.shape
+    if t.dtype is not dtype or t.device != device or len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} must be a {dtype} tensor [tokens, {heads}, {d}] on {device}")
+    st = t.stride()
+    if st[2] != 1 or (st[1] != d and heads > 1):
+        raise ValueError(f"the heads of a token must be contiguous in {name}")
+    if shape[0] > 1 and st[0] < heads * d:
+        raise ValueError(f"the tokens overlap in {name}")
+    return t.data_ptr(), (st[0] if shape[0] > 1 else heads * d)
+
+
+class _OnDevice:
+    """What launches on a device of its own."""
+
+    def _on(self, device):
+        import torch
+        self.device = device
+        # the queries under torch.cuda's where this torch has them (torch.cuda.current_stream() makes an object of
+        # the stream: 3 us of a call of 9)
+        self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                                   lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+    def _stream(self, stream):
+        """The stream to launch on: kernels go to the current device, which has to be the tensors'."""
+        index = self.device.index
+        if index != self._current_device():
+            raise ValueError(f"the {self._what} is on {self.device}, which is not the current device")
+        return self._raw_stream(index) if stream is None else stream.cuda_stream
+
+
+class PagedCache(_OnDevice):
+    """A batch of 8- or 4-bit caches in shared blocks (kv_paged_cache), around the caller's device tensors:
     k, v [n_blocks, h_kv, block_rows, d] (torch.float8_e4m3fn or int8), k_scale, v_scale
-    [n_blocks, h_kv] fp32, table [n_prob, table_stride] int32 and lens [n_prob] int32.  dtype ("bf16" or
-    "f32") is that of queries, new rows and outputs; max_len bounds the lengths (default: what the
-    table holds)."""
+    [n_blocks, h_kv] fp32, table [n_prob, table_stride] int32 and lens [n_prob] int32.  4 bits: k, v
+    [n_blocks, h_kv, block_rows, d / 2] torch.float4_e2m1fn_x2, scales [n_blocks, h_kv, d / 32, block_rows]
+    torch.float8_e8m0fnu.  dtype ("bf16" or "f32") is that of queries, new rows and outputs; max_len bounds the
+    lengths (default: what the table holds)."""
+
+    _what = "cache"
 
     def __init__(self, dtype: str, h_q: int, k, v, k_scale, v_scale, table, lens,
                  max_len: Optional[int] = None):
         import torch
         n_blocks, h_kv, block_rows, d = k.shape
-        if k.dtype not in (torch.float8_e4m3fn, torch.int8) or v.dtype != k.dtype or v.shape != k.shape:
-            raise ValueError("k and v must be float8_e4m3fn or int8 tensors of one shape")
+        qtype = {torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8, torch.float4_e2m1fn_x2: KV_E2M1}.get(k.dtype)
+        if qtype is None or v.dtype != k.dtype or v.shape != k.shape:
+            raise ValueError("k and v must be float8_e4m3fn, int8 or float4_e2m1fn_x2 tensors of one shape")
+        n_scales, scales = n_blocks * h_kv, torch.float32
+        if qtype == KV_E2M1:
+            d *= 2
+            n_scales, scales = n_scales * (d // 32) * block_rows, torch.float8_e8m0fnu
         if dtype not in ("bf16", "f32"):
             raise ValueError("dtype must be bf16 or f32")
         self._tables(table, lens, n_blocks, block_rows)
@@ -519,24 +579,20 @@ class PagedCache:
         self.rows_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         s = self.struct
         s.dtype = KV_BF16 if dtype == "bf16" else KV_F32
-        s.qtype = KV_E4M3 if k.dtype == torch.float8_e4m3fn else KV_INT8
+        s.qtype = qtype
         s.h_q, s.h_kv, s.d = self.h_q, self.h_kv, self.d = int(h_q), h_kv, d
         s.max_len = min(table.shape[1] * block_rows, 1 << 24) if max_len is None else int(max_len)
         s.k, s.v = self._arg(k, k.dtype, 0, "k"), self._arg(v, k.dtype, 0, "v")
-        s.k_scale = self._arg(k_scale, torch.float32, n_blocks * h_kv, "k_scale")
-        s.v_scale = self._arg(v_scale, torch.float32, n_blocks * h_kv, "v_scale")
+        s.k_scale = self._arg(k_scale, scales, n_scales, "k_scale")
+        s.v_scale = self._arg(v_scale, scales, n_scales, "v_scale")
 
     def _tables(self, table, lens, n_blocks, block_rows):
         import torch
         if table.dim() != 2 or lens.numel() != table.shape[0]:
             raise ValueError("table must be [n_prob, table_stride] and lens [n_prob]")
-        self.table, self.lens, self.device = table, lens, table.device
+        self.table, self.lens = table, lens
         self._int32 = torch.int32
-        # the queries under torch.cuda's where this torch has them (torch.cuda.current_stream() makes an object of
-        # the stream: 3 us of a call of 9)
-        self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
-                                   lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self._on(table.device)
         self.n_prob = table.shape[0]
         self.struct = KvPagedCache(n_prob=self.n_prob, block_rows=int(block_rows), n_blocks=int(n_blocks),
                                    table_stride=table.shape[1], table=self._arg(table, torch.int32, 0, "table"),
@@ -553,12 +609,16 @@ class PagedCache:
     @classmethod
     def allocate(cls, dtype: str, qtype: str, h_q: int, h_kv: int, d: int, block_rows: int, n_blocks: int,
                  n_prob: int, table_stride: int, max_len: Optional[int] = None, device=None) -> "PagedCache":
-        """Empty pools (their contents are undefined), a table of missing blocks and lengths of 0."""
+        """Empty pools (their contents are undefined) of qtype "e4m3", "int8" or "e2m1", a table of missing blocks and
+        lengths of 0."""
         import torch
         dev = torch.device("cuda") if device is None else torch.device(device)
-        qt = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}[qtype]
-        pool = lambda: torch.empty(n_blocks, h_kv, block_rows, d, dtype=torch.uint8, device=dev).view(qt)
-        scales = lambda: torch.empty(n_blocks, h_kv, dtype=torch.float32, device=dev)
+        qt = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8, "e2m1": torch.float4_e2m1fn_x2}[qtype]
+        four = qtype == "e2m1"
+        pool = lambda: torch.empty(n_blocks, h_kv, block_rows, d // 2 if four else d, dtype=torch.uint8, device=dev).view(qt)
+        scales = lambda: (torch.empty(n_blocks, h_kv, d // 32, block_rows, dtype=torch.uint8, device=dev)
+                          .view(torch.float8_e8m0fnu) if four else
+                          torch.empty(n_blocks, h_kv, dtype=torch.float32, device=dev))
         return cls(dtype, h_q, pool(), pool(), scales(), scales(),
                    torch.full((n_prob, table_stride), -1, dtype=torch.int32, device=dev),
                    torch.zeros(n_prob, dtype=torch.int32, device=dev), max_len)
@@ -575,24 +635,7 @@ class PagedCache:
         return t.data_ptr()
 
     def _rows(self, t, heads: int, name: str):
-        """Address and token stride of [tokens, heads, d] rows; tokens may lie apart (slices of a projection)."""
-        d = self.d
-        shape = t.shape
-        if t.dtype is not self.rows_dtype or t.device != self.device or len(shape) != 3 or shape[1] != heads or shape[2] != d:
-            raise ValueError(f"{name} must be a {self.rows_dtype} tensor [tokens, {heads}, {d}] on {self.device}")
-        st = t.stride()
-        if st[2] != 1 or (st[1] != d and heads > 1):
-            raise ValueError(f"the heads of a token must be contiguous in {name}")
-        if shape[0] > 1 and st[0] < heads * d:
-            raise ValueError(f"the tokens overlap in {name}")
-        return t.data_ptr(), (st[0] if shape[0] > 1 else heads * d)
-
-    def _stream(self, stream):
-        """The stream to launch on: kernels go to the current device, which has to be the cache's."""
-        index = self.device.index
-        if index != self._current_device():
-            raise ValueError(f"the cache is on {self.device}, which is not the current device")
-        return self._raw_stream(index) if stream is None else stream.cuda_stream
+        return _token_rows(t, self.rows_dtype, self.device, heads, self.d, name)
 
 
 def paged_tables(pc: PagedCache, len_in, add, free_blocks, taken_in, taken_out, tok_off, blk_off, slots,
@@ -624,6 +667,104 @@ def paged_append(pc: PagedCache, k_new, v_new, slots, stream=None) -> None:
     sp, st = pc._arg(slots, pc._int32, n, "slots"), pc._stream(stream)
     if n:
         _check(lib().kv_paged_append(pc._ref, kp, vp, ks, sp, n, st), "kv_paged_append")
+
+
+class Rotary(_OnDevice):
+    """A rotation by positions (kv_rotary): layout "half" or "interleaved", freq [rot_dim / 2] float64 on the device (radians a
+    position; rotary_frequencies gives them), the factor of the rotated elements, and whether it turns back."""
+
+    _what = "rotation"
+
+    def __init__(self, layout: str, freq, factor: float = 1.0, inverse: bool = False):
+        import torch
+        if layout not in ROTARY_LAYOUTS:
+            raise ValueError("layout must be half or interleaved")
+        if freq.dtype is not torch.float64 or not freq.is_cuda or not freq.is_contiguous() or freq.dim() != 1:
+            raise ValueError("freq must be a contiguous float64 device tensor [rot_dim / 2]")
+        self.freq = freq
+        self._on(freq.device)
+        self.struct = KvRotary(ROTARY_LAYOUTS[layout], 2 * freq.numel(), int(bool(inverse)), float(factor), freq.data_ptr())
+        self._ref = ctypes.byref(self.struct)
+
+    def ref(self):
+        return self._ref
+
+
+def rotary_frequencies(family: str, rot_dim: int, base: float = 10000.0, params: Sequence[float] = ()):
+    """-> (frequencies [rot_dim / 2] float64, factor) of a family "plain", "linear" (F), "ntk" (F), "yarn" (F, L0,
+    beta_fast, beta_slow) or "bands" (F, L0, low, high)."""
+    fam = ROTARY_FAMILIES[family] if isinstance(family, str) else int(family)
+    p = (ctypes.c_double * len(params))(*[float(x) for x in params])
+    out, factor = (ctypes.c_double * max(1, int(rot_dim) // 2))(), ctypes.c_float()
+    _check(lib().kv_rotary_frequencies(fam, float(base), p, len(params), int(rot_dim), out, ctypes.byref(factor)),
+           "kv_rotary_frequencies")
+    return np.frombuffer(out, dtype=np.float64).copy(), float(factor.value)
+
+
+def _positions(pos, device, n: int):
+    import torch
+    if pos.dtype is not torch.int32 or pos.device != device or not pos.is_contiguous() or pos.numel() < n:
+        raise ValueError(f"pos must be a contiguous int32 tensor of at least {n} positions on {device}")
+    return pos.data_ptr()
+
+
+def rotate(rot: Rotary, x, pos, out, stream=None) -> None:
+    """kv_rotate: x [tokens, heads, d] bf16 or fp32 (tokens of one stride) at positions pos [tokens] int32, to out of the
+    same shape and type, which may be x.  No tokens: nothing to do."""
+    import torch
+    if x.dtype not in (torch.bfloat16, torch.float32) or x.dim() != 3:
+        raise ValueError("x must be a bfloat16 or float32 tensor [tokens, heads, d]")
+    n, heads, d = x.shape
+    if out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    xp, xs = _token_rows(x, x.dtype, rot.device, heads, d, "x")
+    op, os_ = _token_rows(out, x.dtype, rot.device, heads, d, "out")
+    pp = _positions(pos, rot.device, n)
+    st = rot._stream(stream)
+    if n:
+        _check(lib().kv_rotate(rot._ref, KV_BF16 if x.dtype is torch.bfloat16 else KV_F32, heads, d, xp, xs, pp, n, op, os_, st),
+               "kv_rotate")
+
+
+def paged_append_rotated(pc: PagedCache, rot: Rotary, pos, k_new, v_new, slots, q=None, q_out=None, stream=None) -> None:
+    """kv_paged_append_rotated: paged_append with k_new rotated to positions pos [tokens] int32 on the way, and with q
+    [tokens, h_q, d] its rotation in q_out (which may be q).  No tokens: nothing to do."""
+    kp, ks = pc._rows(k_new, pc.h_kv, "k_new")
+    vp, vs = pc._rows(v_new, pc.h_kv, "v_new")
+    n = k_new.shape[0]
+    if v_new.shape[0] != n or ks != vs:
+        raise ValueError("k_new and v_new must have one shape and token stride")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    qp, qs, op, os_ = None, 0, None, 0
+    if q is not None:
+        qp, qs = pc._rows(q, pc.h_q, "q")
+        op, os_ = pc._rows(q_out, pc.h_q, "q_out")
+        if q.shape[0] != n or q_out.shape[0] != n:
+            raise ValueError("q and q_out must have as many tokens as k_new")
+    if rot.device != pc.device:
+        raise ValueError(f"the rotation is on {rot.device}, the cache on {pc.device}")
+    pp, sp, st = pc._arg(pos, pc._int32, n, "pos"), pc._arg(slots, pc._int32, n, "slots"), pc._stream(stream)
+    if n:
+        _check(lib().kv_paged_append_rotated(pc._ref, rot._ref, pp, qp, qs, op, os_, kp, vp, ks, sp, n, st),
+               "kv_paged_append_rotated")
+
+
+def paged_rows(pc: PagedCache, row_off, k_out, v_out, n_rows: Optional[int] = None, stream=None) -> None:
+    """kv_paged_rows: the rows of every problem p into k_out and v_out (either may be None) at row_off[p] h_kv d elements,
+    [h_kv][row_off[p + 1] - row_off[p]][d]; row_off [n_prob + 1] int64.  n_rows: the rows that the outputs hold (default:
+    all)."""
+    import torch
+    unit = pc.h_kv * pc.d
+    held = [t.numel() // unit for t in (k_out, v_out) if t is not None]
+    if not held:
+        raise ValueError("one of k_out and v_out is needed")
+    n_rows = min(held) if n_rows is None else int(n_rows)
+    kp = pc._arg(k_out, pc.rows_dtype, n_rows * unit, "k_out")
+    vp = pc._arg(v_out, pc.rows_dtype, n_rows * unit, "v_out")
+    op, st = pc._arg(row_off, torch.int64, pc.n_prob + 1, "row_off"), pc._stream(stream)
+    if n_rows:
+        _check(lib().kv_paged_rows(pc._ref, op, n_rows, kp, vp, st), "kv_paged_rows")
 
 
 def paged_compact(batch: Batch, k, v, sel_idx, budget: int, keep_tail: int, pc: PagedCache,

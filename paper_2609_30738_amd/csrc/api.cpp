@@ -22,6 +22,7 @@ constexpr float kLog2eF = 1.4426950408889634f;  // log2(e): kernels take logits 
 constexpr int kMaxPool = 63;  // widest max-pool window of kv_mmr_select_ex
 constexpr size_t kWsAlign = 256;
 constexpr int64_t kMaxTokenStride = (int64_t)1 << 26;
+constexpr int kMaxRotated = 1 << 25;  // tokens of a rotation: its launch stays below 2^32 threads
 
 size_t align_up(size_t x) { return (x + kWsAlign - 1) & ~(kWsAlign - 1); }
 
@@ -802,16 +803,17 @@ int check_paged(const kv_paged_cache* c, kv::Paged* pc, bool tables = false) {
   if (c->table_stride < 1 || (int64_t)c->table_stride * c->block_rows > INT32_MAX) return KV_ERR_SHAPE;
   if (!tables) {
     if (c->dtype != KV_F32 && c->dtype != KV_BF16) return KV_ERR_DTYPE;
-    if (c->qtype != KV_E4M3 && c->qtype != KV_INT8) return KV_ERR_DTYPE;
+    if (c->qtype != KV_E4M3 && c->qtype != KV_INT8 && c->qtype != KV_E2M1) return KV_ERR_DTYPE;
     if (!c->k || !c->v || !c->k_scale || !c->v_scale) return KV_ERR_NULL;
     if (!aligned16(c->k) || !aligned16(c->v)) return KV_ERR_ARG;
+    if (c->qtype == KV_E2M1 && (!aligned16(c->k_scale) || !aligned16(c->v_scale))) return KV_ERR_ARG;
     if (c->h_kv < 1 || c->h_kv > 4096 || c->h_q < c->h_kv || c->h_q % c->h_kv != 0 || c->h_q / c->h_kv > 16)
       return KV_ERR_SHAPE;
     if (c->d != 64 && c->d != 128) return KV_ERR_SHAPE;
     if (c->max_len < 0 || c->max_len > kMaxLen) return KV_ERR_SHAPE;
   }
   pc->dtype = c->dtype == KV_BF16 ? kv::kDtBf16 : kv::kDtF32;
-  pc->qtype = c->qtype == KV_E4M3 ? kv::kQtE4m3 : kv::kQtInt8;
+  pc->qtype = c->qtype == KV_E4M3 ? kv::kQtE4m3 : c->qtype == KV_INT8 ? kv::kQtInt8 : kv::kQtE2m1;
   pc->n_prob = c->n_prob;
   pc->h_q = c->h_q;
   pc->h_kv = c->h_kv;
@@ -835,6 +837,45 @@ int check_stride(const kv::Paged& pc, int heads, int64_t* stride) {
   const int64_t packed = (int64_t)heads * pc.d;
   if (*stride == 0) *stride = packed;
   if (*stride < packed || *stride > kMaxTokenStride || *stride % (pc.dtype == kv::kDtBf16 ? 8 : 4) != 0) return KV_ERR_ARG;
+  return KV_OK;
+}
+
+// A rotation of heads of d elements; fills the kernels' description.
+int check_rotary(const kv_rotary* r, int d, kv::Rotary* rot) {
+  if (!r || !r->freq) return KV_ERR_NULL;
+  if (r->layout != KV_ROTARY_HALF && r->layout != KV_ROTARY_INTERLEAVED) return KV_ERR_ARG;
+  if (!std::isfinite(r->factor) || (reinterpret_cast<uintptr_t>(r->freq) & 7)) return KV_ERR_ARG;
+  if (r->rot_dim < 16 || r->rot_dim > d || r->rot_dim % 16 != 0) return KV_ERR_SHAPE;
+  *rot = {r->layout == KV_ROTARY_INTERLEAVED, r->rot_dim, r->inverse ? -1.f : 1.f, r->factor, r->freq};
+  return KV_OK;
+}
+
+// Whether rows of `bytes` bytes, n of them x_step (out_step) bytes apart, meet in any other way than row for row.
+bool rows_overlap(const void* x, int64_t x_step, const void* out, int64_t out_step, int64_t bytes, int64_t n) {
+  const intptr_t p = reinterpret_cast<intptr_t>(x), q = reinterpret_cast<intptr_t>(out);
+  if (x_step == out_step && (p == q || n == 1)) return p != q && p < q + bytes && q < p + bytes;
+  if (p >= q + (n - 1) * out_step + bytes || q >= p + (n - 1) * x_step + bytes) return false;
+  if (x_step != out_step) return n > 1 || (p != q && p < q + bytes && q < p + bytes);
+  // slices of the same wide rows
+  const int64_t apart = ((q - p) % x_step + x_step) % x_step;
+  return apart < bytes || x_step - apart < bytes;
+}
+
+// The rows of a rotation from x to out.
+int check_rotate(const kv::Rotary& rot, int dtype, int heads, int d, const void* x, int64_t x_stride, const int32_t* pos, int n_tok,
+                 void* out, int64_t out_stride, kv::RotateArgs* a) {
+  if (!x || !out || !pos) return KV_ERR_NULL;
+  if (!aligned16(x) || !aligned16(out) || n_tok < 1) return KV_ERR_ARG;
+  if (n_tok > kMaxRotated) return KV_ERR_SHAPE;
+  kv::Paged pc{};
+  pc.dtype = dtype;
+  pc.d = d;
+  int st = check_stride(pc, heads, &x_stride);
+  if (st == KV_OK) st = check_stride(pc, heads, &out_stride);
+  if (st != KV_OK) return st;
+  const int64_t e = dtype == kv::kDtBf16 ? 2 : 4;
+  if (rows_overlap(x, x_stride * e, out, out_stride * e, heads * d * e, n_tok)) return KV_ERR_ARG;
+  *a = {rot, x, out, x_stride, out_stride, pos, n_tok, heads, 1};
   return KV_OK;
 }
 
@@ -908,6 +949,82 @@ int kv_paged_append(const kv_paged_cache* c, const void* k_new, const void* v_ne
   if (st != KV_OK) return st;
   return launch_status(kv::launch_paged_append(pc, k_new, v_new, tok_stride, slots, n_tok,
                                                static_cast<hipStream_t>(stream)));
+}
+
+int kv_rotate(const kv_rotary* r, int32_t dtype, int32_t heads, int32_t d, const void* x, int64_t x_stride,
+              const int32_t* pos, int32_t n_tok, void* out, int64_t out_stride, void* stream) {
+  if (dtype != KV_F32 && dtype != KV_BF16) return KV_ERR_DTYPE;
+  if ((d != 64 && d != 128) || heads < 1 || heads > kMaxTokenStride / d) return KV_ERR_SHAPE;
+  kv::Rotary rot;
+  int st = check_rotary(r, d, &rot);
+  if (st != KV_OK) return st;
+  kv::RotateArgs a;
+  const int dt = dtype == KV_BF16 ? kv::kDtBf16 : kv::kDtF32;
+  st = check_rotate(rot, dt, heads, d, x, x_stride, pos, n_tok, out, out_stride, &a);
+  if (st != KV_OK) return st;
+  return launch_status(kv::launch_rotate(dt, d, a, static_cast<hipStream_t>(stream)));
+}
+
+int kv_paged_append_rotated(const kv_paged_cache* c, const kv_rotary* r, const int32_t* pos, const void* q, int64_t q_stride,
+                            void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new, int64_t tok_stride,
+                            const int32_t* slots, int32_t n_tok, void* stream) {
+  kv::Paged pc{};
+  int st = check_paged(c, &pc);
+  if (st != KV_OK) return st;
+  kv::Rotary rot;
+  st = check_rotary(r, pc.d, &rot);
+  if (st != KV_OK) return st;
+  if (!pos || !k_new || !v_new || !slots || (q != nullptr) != (q_out != nullptr)) return KV_ERR_NULL;
+  if (!aligned16(k_new) || !aligned16(v_new) || n_tok < 1) return KV_ERR_ARG;
+  if (n_tok > kMaxRotated) return KV_ERR_SHAPE;
+  st = check_stride(pc, pc.h_kv, &tok_stride);
+  if (st != KV_OK) return st;
+  kv::RotateArgs rq{rot, nullptr, nullptr, 0, 0, pos, n_tok, 0, 1};
+  if (q) st = check_rotate(rot, pc.dtype, pc.h_q, pc.d, q, q_stride, pos, n_tok, q_out, q_out_stride, &rq);
+  if (st != KV_OK) return st;
+  return launch_status(kv::launch_paged_append_rotated(pc, rq, k_new, v_new, tok_stride, slots, static_cast<hipStream_t>(stream)));
+}
+
+int kv_paged_rows(const kv_paged_cache* c, const int64_t* row_off, int64_t n_rows, void* k_out, void* v_out, void* stream) {
+  kv::Paged pc{};
+  const int st = check_paged(c, &pc);
+  if (st != KV_OK) return st;
+  if (!row_off || (!k_out && !v_out)) return KV_ERR_NULL;
+  if (!aligned16(k_out) || !aligned16(v_out) || n_rows < 1) return KV_ERR_ARG;
+  return launch_status(kv::launch_paged_rows(pc, row_off, n_rows, k_out, v_out, static_cast<hipStream_t>(stream)));
+}
+
+int kv_rotary_frequencies(int32_t family, double base, const double* params_host, int32_t n_params, int32_t rot_dim,
+                          double* freq_host, float* factor_host) {
+  if (!freq_host || !factor_host) return KV_ERR_NULL;
+  const int wanted[] = {0, 1, 1, 4, 4};
+  if (family < KV_ROTARY_PLAIN || family > KV_ROTARY_BANDS || n_params != wanted[family]) return KV_ERR_ARG;
+  if (n_params > 0 && !params_host) return KV_ERR_NULL;
+  if (rot_dim < (family == KV_ROTARY_NTK ? 4 : 2) || rot_dim % 2 != 0 || !(base > 1) || !std::isfinite(base)) return KV_ERR_ARG;
+  for (int i = 0; i < n_params; ++i)
+    if (!(params_host[i] > 0) || !std::isfinite(params_host[i])) return KV_ERR_ARG;
+  const double F = n_params > 0 ? params_host[0] : 1.0, r = rot_dim, kTwoPi = 6.283185307179586;
+  if (F < 1) return KV_ERR_ARG;
+  if (family == KV_ROTARY_YARN && !(params_host[2] > params_host[3])) return KV_ERR_ARG;
+  if (family == KV_ROTARY_BANDS && !(params_host[3] > params_host[2])) return KV_ERR_ARG;
+  if (family == KV_ROTARY_NTK) base *= std::pow(F, r / (r - 2));
+  double lo = 0, hi = 0;
+  if (family == KV_ROTARY_YARN) {
+    auto at = [&](double turns) { return r * std::log(params_host[1] / (kTwoPi * turns)) / (2 * std::log(base)); };
+    lo = std::max(std::floor(at(params_host[2])), 0.0);
+    hi = std::min(std::ceil(at(params_host[3])), r - 1);
+  }
+  *factor_host = family == KV_ROTARY_YARN ? (float)(0.1 * std::log(F) + 1) : 1.f;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / r);
+    double keep = 1;  // the share of the unscaled frequency
+    if (family == KV_ROTARY_LINEAR) keep = 0;
+    else if (family == KV_ROTARY_YARN) keep = 1 - std::min(std::max((i - lo) / std::max(hi - lo, 1e-3), 0.0), 1.0);
+    else if (family == KV_ROTARY_BANDS)
+      keep = std::min(std::max((params_host[1] * f / kTwoPi - params_host[2]) / (params_host[3] - params_host[2]), 0.0), 1.0);
+    freq_host[i] = keep == 1 ? f : f * ((1 - keep) / F + keep);
+  }
+  return KV_OK;
 }
 
 int kv_paged_compact(const kv_problem* pr, const void* k, const void* v, const int32_t* sel_idx,

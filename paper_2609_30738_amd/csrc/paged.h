@@ -1,4 +1,4 @@
-// The 8-bit paged cache on the host's side: its description as the kernels take it, and the
+// The paged cache of 8- or 4-bit codes on the host's side: its description as the kernels take it, and the
 // launchers.  Arguments are validated by the C ABI layer before any of these is called.
 #pragma once
 
@@ -10,9 +10,11 @@ namespace kv {
 
 constexpr int kQtE4m3 = 0;
 constexpr int kQtInt8 = 1;
+constexpr int kQtE2m1 = 4;  // 4 bits, two to a byte
 
-// Pools [n_blocks][h_kv][1 << shift][d] of codes and [n_blocks][h_kv] of scales; row r of problem p is
-// row r % R of block table[p][r / R], R = 1 << shift.
+// Pools [n_blocks][h_kv][1 << shift][d] of codes and [n_blocks][h_kv] of scales (e2m1: d / 2 bytes to a row, and
+// scale bytes [n_blocks][h_kv][d / 32][1 << shift]); row r of problem p is row r % R of block table[p][r / R],
+// R = 1 << shift.
 struct Paged {
   int dtype, qtype;
   int n_prob, h_q, h_kv, d;
@@ -20,8 +22,8 @@ struct Paged {
   int n_blocks, table_stride, max_len;
   uint8_t* k;
   uint8_t* v;
-  float* k_scale;
-  float* v_scale;
+  void* k_scale;
+  void* v_scale;
   int32_t* table;
   int32_t* len;
   int group() const { return h_q / h_kv; }
@@ -51,6 +53,32 @@ hipError_t launch_paged_compact(const Paged& pc, const int32_t* lens, int max_le
                                 const void* k, const void* v, const int32_t* sel_idx, int budget,
                                 const int32_t* budgets, int keep_tail, hipStream_t stream);
 
+// A rotation by positions (kv_rotary): freq [rot / 2] radians a position.
+struct Rotary {
+  bool interleaved;
+  int rot;       // rotated elements of a head
+  float sign;    // -1: by the opposite angle
+  float factor;  // of the rotated elements
+  const double* freq;
+};
+// Rows of `heads` heads of d elements, out (nullable) and their rotation; strides in elements between two tokens.
+struct RotateArgs {
+  Rotary rot;
+  const void* x;
+  void* out;
+  int64_t x_stride, out_stride;
+  const int32_t* pos;  // [n_tok]
+  int n_tok, heads;
+  int parts;  // workgroups that share the heads of a group of tokens
+};
+hipError_t launch_rotate(int dtype, int d, const RotateArgs& a, hipStream_t stream);
+// Rows into the blocks with K rotated, and the rotated rows of q (rq.x null: none) in the same launch (paged_rotated.hip).
+hipError_t launch_paged_append_rotated(const Paged& pc, const RotateArgs& rq, const void* k_new, const void* v_new,
+                                       int64_t tok_stride, const int32_t* slots, hipStream_t stream);
+// The caches' rows, contiguous (paged_read.hip).
+hipError_t launch_paged_rows(const Paged& pc, const int64_t* row_off, int64_t n_rows, void* k_out, void* v_out,
+                             hipStream_t stream);
+
 // Attention over the blocks (paged_attention.hip).
 struct PagedAttnArgs {
   Paged pc;
@@ -74,6 +102,8 @@ PagedPlan paged_plan(const Paged& pc, int max_q);
 int64_t paged_grid_groups(const Paged& pc, int max_q, const PagedPlan& plan);
 size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t stream);
+// The same without the join, over 4-bit blocks (paged_attention4.hip).  nt: 16-wide column tiles of a wave.
+hipError_t launch_paged_attention4(const PagedAttnArgs& a, int nt, hipStream_t stream);
 // Blocks of a split that the prompt kernel of so many waves holds in LDS beside its tiles
 // (two workgroups of four waves share a CU's 160 KB, one of eight has it alone).
 constexpr int prompt_split_blocks(int waves) { return waves == 4 ? 256 : 4096; }

@@ -1,4 +1,5 @@
-// Attention of the last tokens of every problem over its 8-bit paged cache (kv_paged_attention).
+// Attention of the last tokens of every problem over its 8-bit paged cache (kv_paged_attention), and the join of the
+// splits of every paged cache.
 //
 // paged_attn_kernel: one workgroup of four waves per (kv head and group of columns, split of the rows,
 //   problem).  A column is a (token, query head) pair of the kv head; a wave takes 16 NT of them
@@ -39,58 +40,9 @@ namespace kv {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kThreads = kAttnThreads;
+constexpr int kWaves = kAttnWaves;
 constexpr int kStep = 32;               // rows of a wave's step
-constexpr int kMaxSplitRows = 2048;     // the blocks and scales of a split are held in LDS
-constexpr int kMaxSplitBlocks = kMaxSplitRows / 16;
-
-typedef float __attribute__((ext_vector_type(4))) f32x4v;
-
-__device__ __forceinline__ f32x4v mfma16(const u32x4_t& a, const u32x4_t& b, const f32x4v& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, a), __builtin_bit_cast(bf16x8v, b), c,
-                                                 0, 0, 0);
-}
-
-__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
-
-// Eight floats as N bf16 terms that add up to them (8 bits of each per term).
-template <int N> __device__ __forceinline__ void split_terms(const float (&x)[8], u32x4_t (&t)[N]) {
-  float r[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) r[i] = x[i];
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      t[n][i] = pack_bf16(r[2 * i], r[2 * i + 1]);
-      if (n + 1 < N) {
-        r[2 * i] -= bf16_lo(t[n][i]);
-        r[2 * i + 1] -= bf16_hi(t[n][i]);
-      }
-    }
-}
-
-// Largest value and sum over the four lanes of a column (l, l ^ 16, l ^ 32, l ^ 48).
-__device__ __forceinline__ float column_max(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float column_sum(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// A load with the non-temporal bit where one workgroup alone reads a row (up to 16 columns, one group of them):
-// 32 caches of 32768 rows 335 us, 363 without it.
-template <bool kOnce, typename T> __device__ __forceinline__ T load_code(const T* p) {
-  return kOnce ? __builtin_nontemporal_load(p) : *p;
-}
 
 // Waves per SIMD that the registers are held to: as many as run without spills.
 template <int DT, int D, int NT> constexpr int kMinWaves = (NT == 1 ? 3 : 2) - (DT == kDtF32 && D == 128 ? 1 : 0);
@@ -135,7 +87,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves<DT, D, NT>)) void paged_attn_k
   if (tid < kMaxSplitBlocks) sh_block[tid] = has ? id : -1;
   __syncthreads();
   const int64_t scale_at = (int64_t)(has ? id : 0) * a.pc.h_kv + g;
-  const float my_ks = has ? a.pc.k_scale[scale_at] * a.c : 0.f, my_vs = has ? a.pc.v_scale[scale_at] : 0.f;
+  const float my_ks = has ? static_cast<const float*>(a.pc.k_scale)[scale_at] * a.c : 0.f, my_vs = has ? static_cast<const float*>(a.pc.v_scale)[scale_at] : 0.f;
 
   // the codes of 32 rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n
   u32x4_t xk[2][KH];
@@ -580,8 +532,9 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan,
     return a.pc.qtype == kQtE4m3 ? d(dt, std::integral_constant<int, kQtE4m3>{})
                                  : d(dt, std::integral_constant<int, kQtInt8>{});
   };
-  const hipError_t e = plan.prompt_waves ? launch_paged_prompt(a, plan.prompt_waves, stream)
-                       : bf16            ? q(std::integral_constant<int, kDtBf16>{})
+  const hipError_t e = plan.prompt_waves              ? launch_paged_prompt(a, plan.prompt_waves, stream)
+                       : a.pc.qtype == kQtE2m1        ? launch_paged_attention4(a, column_tiles(a.max_q, a.pc.group()), stream)
+                       : bf16                         ? q(std::integral_constant<int, kDtBf16>{})
                                          : q(std::integral_constant<int, kDtF32>{});
   if (e != hipSuccess || a.n_split == 1) return e;
   if (bf16) return a.pc.d == 64 ? combine<kDtBf16, 64>(a, stream) : combine<kDtBf16, 128>(a, stream);

@@ -1,0 +1,338 @@
+// Attention of the last tokens of every problem over its 4-bit paged cache (kv_paged_attention on a cache of e2m1
+// codes, up to 32 columns at a time; a column is a (token, query head) pair of the kv head).
+//
+// paged_attn4_kernel: workgroups, columns, splits, references and weights as in paged_attention.hip's kernel; what
+//   differs is how the codes come in.
+//     S^T = K Q^T,  O^T = V^T P^T  by v_mfma_f32_16x16x32_bf16.
+//   The scales belong to a row and 32 of its elements, so they go into the operands, where the conversion from four bits
+//   applies them at no cost (a code times its scale is exact in bf16).  A lane's operand of K is a quarter of a row: at
+//   d = 128 one 16-byte load and one scale.  For V a lane takes D / 16 elements of each of its rows, a word at d = 128, and
+//   the scales of 16 rows in one load; pairs of rows are put together by byte permutations once converted.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "paged.h"
+#include "paged_codes.h"
+#include "paged_span.h"
+
+namespace kv {
+
+namespace {
+
+constexpr int kThreads = kAttnThreads;
+constexpr int kWaves = kAttnWaves;
+
+// Tiles of 16 rows in a wave's step, and the waves per SIMD that the registers are held to.
+template <int NT> constexpr int kTiles4 = NT == 1 ? 2 : 2;
+template <int DT, int D, int NT> constexpr int kMinWaves4 = (NT == 1 ? 3 : 2) - (DT == kDtF32 && D == 128 ? 1 : 0);
+
+}  // namespace
+
+template <int DT, int D, int NT>
+__global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4_kernel(PagedAttnArgs a) {
+  constexpr int NS = D / 32;                       // matrix steps over the head dimension
+  constexpr int NI = D / 16;                       // 16-wide tiles of the output, elements of V that a lane takes
+  constexpr int KW = D / 32;                       // words of a key that a lane takes
+  constexpr int RB = D / 2, NG = D / kGroup4;      // bytes and scales of a row
+  constexpr int TS = kTiles4<NT>, STEP = 16 * TS;
+  constexpr int QN = DT == kDtBf16 ? 1 : 3;        // bf16 terms of a query
+  constexpr int PN = DT == kDtF32 ? 3 : (NT == 1 ? 2 : 1);  // and of a weight
+  constexpr int COLS = 16 * NT;
+  __shared__ int32_t sh_block[kMaxSplitBlocks];
+  __shared__ float sh_m[kWaves][16], sh_s[kWaves][16];
+  extern __shared__ __align__(16) float sh_acc[];  // [kWaves][up to 16 columns][D]
+
+  const int p = blockIdx.z, g = blockIdx.x % a.pc.h_kv, cg = blockIdx.x / a.pc.h_kv, G = a.pc.h_q / a.pc.h_kv;
+  // (the problems' splits start one further each: with fewer heads than XCDs, these take long caches' ends in turn)
+  const int split = a.n_split > 1 ? (int)((blockIdx.y + (uint32_t)p) % (uint32_t)a.n_split) : 0;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, kg = lane >> 4;
+  const int shift = a.pc.shift, R = 1 << shift;
+  const int r0 = split * a.split_rows;
+  // the split's table entries load beside the lengths
+  const int entry = (r0 >> shift) + tid;
+  const int id = tid << shift < a.split_rows && entry < a.pc.table_stride
+                     ? a.pc.table[(int64_t)p * a.pc.table_stride + entry] : -1;
+  const Span sp = span_of(a, p);
+  const int col0 = cg * COLS;
+  const int n_cols = min(sp.n_tok * G - col0, COLS);
+  if (n_cols <= 0) return;
+  const int vis_max = sp.visible((col0 + n_cols - 1) / G);
+  const int vis_min = sp.visible(col0 / G);
+  const int r1 = min(vis_max, r0 + a.split_rows);
+  if (r0 >= r1 && a.n_split > 1) return;  // the join reads the splits below a column's last row
+
+  const bool has = tid << shift < r1 - r0 && id >= 0 && id < a.pc.n_blocks;
+  if (tid < kMaxSplitBlocks) sh_block[tid] = has ? id : -1;
+  __syncthreads();
+
+  // The codes and scales of a step's rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n.
+  uint32_t xk[TS][KW], xv[TS][4], ksb[TS];
+  u32x4_t vsb[TS];  // of 16 rows
+  const int k_row = 4 * (n & 3) + (n >> 2);
+  // a wave-uniform address and a lane's 32-bit offset
+  const uint32_t k_lane = k_row * RB + kg * (4 * KW), v_lane = kg * RB + n * (NI / 2);
+  const uint32_t ks_lane = (kg * (D / 4) / kGroup4) * R + k_row, vs_lane = (n * NI / kGroup4) * R;
+  auto tile_at = [&](int rb, int t, int64_t& codes, int64_t& scales) {
+    const int r = min(rb + 16 * t, (r1 - 1) & ~15) - r0;
+    const int64_t id = max(__builtin_amdgcn_readfirstlane(sh_block[r >> shift]), 0);
+    const int64_t unit = id * a.pc.h_kv + g;
+    codes = (unit << shift) * RB + (r & (R - 1)) * RB;
+    scales = (unit << shift) * NG + (r & (R - 1));
+  };
+  auto load_k = [&](int rb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TS; ++t) {
+      int64_t codes, scales;
+      tile_at(rb, t, codes, scales);
+      const uint8_t* ks = a.pc.k + codes + k_lane;
+      if constexpr (KW == 4) {
+        const u32x4_t u = load_code<NT == 1>(reinterpret_cast<const u32x4_t*>(ks));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xk[t][i] = u[i];
+      } else {
+        const u32x2_t u = load_code<NT == 1>(reinterpret_cast<const u32x2_t*>(ks));
+        xk[t][0] = u[0];
+        xk[t][1] = u[1];
+      }
+      ksb[t] = *(static_cast<const uint8_t*>(a.pc.k_scale) + scales + ks_lane);
+    }
+  };
+  auto load_v = [&](int rb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TS; ++t) {
+      int64_t codes, scales;
+      tile_at(rb, t, codes, scales);
+      const uint8_t* vs = a.pc.v + codes;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (NI == 8) xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint32_t*>(vs + (v_lane + 4 * j * RB)));
+        else xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint16_t*>(vs + (v_lane + 4 * j * RB)));
+      }
+      vsb[t] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.pc.v_scale) + scales + vs_lane);
+    }
+  };
+
+  constexpr int kRound = kWaves * STEP;
+  const int rb0 = r0 + wave * STEP;
+  if (rb0 < r1) {
+    load_k(rb0);
+    load_v(rb0);
+  }
+  // the queries' operand: column n, elements D / 4 kg + 8 s .. + 7
+  u32x4_t qf[NT][NS][QN];
+  int vis[NT];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    const int col = col0 + 16 * ct + n;
+    const bool live = 16 * ct + n < n_cols;
+    const int j = live ? col / G : 0, h = live ? col % G : 0;
+    vis[ct] = live ? sp.visible(j) : 0;
+    const int64_t at = (int64_t)(sp.tok0 + j) * a.q_stride + (int64_t)(g * G + h) * D;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int e = D / 4 * kg + 8 * s;
+      if constexpr (DT == kDtBf16) {
+        qf[ct][s][0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at + e);
+      } else {
+        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + e);
+        const float4 x = src[0], y = src[1];
+        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        split_terms<QN>(f, qf[ct][s]);
+      }
+    }
+  }
+
+  float m[NT], mu[NT], sum[NT];  // mu: m, or 0 before the first finite logit
+  f32x4v acc[NT][NI];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    m[ct] = -INFINITY;
+    mu[ct] = 0.f;
+    sum[ct] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) acc[ct][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // A step's rows; the codes of the step at `next` (if any) load as this one's are used up.
+  auto step = [&](int rb, int next) __attribute__((always_inline)) {
+    int blk[TS], any = 0;
+#pragma unroll
+    for (int t = 0; t < TS; ++t) {
+      blk[t] = __builtin_amdgcn_readfirstlane(sh_block[(min(rb + 16 * t, (r1 - 1) & ~15) - r0) >> shift]);
+      any |= blk[t];
+    }
+    // its rows are not all visible to every column, or a block is missing
+    const bool masked = rb + STEP > vis_min || any < 0;
+    float lg[NT][4 * TS];
+    // (codes are converted here, not where they were loaded a step before: registers)
+#pragma unroll
+    for (int t = 0; t < TS; ++t)
+#pragma unroll
+      for (int i = 0; i < KW; ++i) asm volatile("" : "+v"(xk[t][i]));
+#pragma unroll
+    for (int t = 0; t < TS; ++t) {
+      f32x4v s4[NT];
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) s4[ct] = f32x4v{0.f, 0.f, 0.f, 0.f};
+      const float ksc = scale4(ksb[t]);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const u32x4_t kf = decode8_e2m1(xk[t][s], ksc);
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+          for (int q = QN - 1; q >= 0; --q) s4[ct] = mfma16(kf, qf[ct][s][q], s4[ct]);
+      }
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float l = s4[ct][j] * a.c;
+          if (masked && (blk[t] < 0 || rb + 16 * t + 4 * j + kg >= vis[ct])) l = -INFINITY;
+          lg[ct][4 * t + j] = l;
+        }
+    }
+    if (next < r1) load_k(next);
+    bool over = false;
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) {
+      float tm = lg[ct][0];
+#pragma unroll
+      for (int e = 1; e < 4 * TS; ++e) tm = fmaxf(tm, lg[ct][e]);
+      over = over || tm > m[ct] + kSlack;
+    }
+    if (__ballot(over)) {
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        float tm = lg[ct][0];
+#pragma unroll
+        for (int e = 1; e < 4 * TS; ++e) tm = fmaxf(tm, lg[ct][e]);
+        const float mn = fmaxf(m[ct], column_max(tm));
+        const float f = m[ct] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+        m[ct] = mn;
+        mu[ct] = mn == -INFINITY ? 0.f : mn;
+        sum[ct] *= f;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[ct][i][j] *= f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < TS / 2; ++u) {  // two tiles at a time
+      u32x4_t pf[NT][PN];
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[e] = __builtin_amdgcn_exp2f(lg[ct][8 * u + e] - mu[ct]) * kSlackScale;
+          sum[ct] += w[e];
+        }
+        split_terms<PN>(w, pf[ct]);
+      }
+      float vsc[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        asm volatile("" : "+v"(xv[2 * u + (e >> 2)][e & 3]));
+        vsc[e] = scale4(vsb[2 * u + (e >> 2)][e & 3] >> (8 * kg) & 255u);
+      }
+      // V^T: pairs of elements of eight rows, put together as pairs of rows
+      auto pair = [&](auto b) __attribute__((always_inline)) {
+        constexpr int B = decltype(b)::value;
+        uint32_t x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = decode2_e2m1<B>(xv[2 * u + (e >> 2)][e & 3], vsc[e]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          u32x4_t vf;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vf[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], i ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+            for (int q = PN - 1; q >= 0; --q) acc[ct][2 * B + i] = mfma16(vf, pf[ct][q], acc[ct][2 * B + i]);
+        }
+      };
+      pair(std::integral_constant<int, 0>{});
+      pair(std::integral_constant<int, 1>{});
+      if constexpr (NI == 8) {
+        pair(std::integral_constant<int, 2>{});
+        pair(std::integral_constant<int, 3>{});
+      }
+    }
+    if (next < r1) load_v(next);
+  };
+
+  for (int rb = rb0; rb < r1; rb += kRound) step(rb, rb + kRound);  // the waves' steps in turn
+
+  // merge of the waves, 16 columns at a time: element NI (4 kg + j) + i of column n
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    const int cols = min(n_cols - 16 * ct, 16);
+    if (cols <= 0) break;
+    const float s = column_sum(sum[ct]);
+    if (kg == 0) {
+      sh_m[wave][n] = m[ct];
+      sh_s[wave][n] = s;
+    }
+    if (n < cols) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < NI; i += 4)
+          *reinterpret_cast<float4*>(&sh_acc[(wave * cols + n) * D + (4 * kg + j) * NI + i]) =
+              make_float4(acc[ct][i][j], acc[ct][i + 1][j], acc[ct][i + 2][j], acc[ct][i + 3][j]);
+    }
+    __syncthreads();
+    for (int idx = tid; idx < cols * D; idx += kThreads) {
+      const int cc = idx / D, e = idx % D;
+      float M = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) M = fmaxf(M, sh_m[i][cc]);
+      float S = 0.f, A = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const float f = part_weight(sh_m[i][cc], M);
+        S = fmaf(sh_s[i][cc], f, S);
+        A = fmaf(sh_acc[(i * cols + cc) * D + e], f, A);
+      }
+      const int col = col0 + 16 * ct + cc;
+      const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
+      if (a.n_split == 1) {
+        store_out<DT>(a.out, row * D + e, A, S);
+      } else {
+        float* pt = a.part + (row * a.n_split + split) * (D + 2);
+        if (e == 0) {
+          pt[0] = M;
+          pt[1] = S;
+        }
+        pt[2 + e] = A;
+      }
+    }
+    if (ct + 1 < NT) __syncthreads();
+  }
+}
+
+namespace {
+
+template <int DT, int D> hipError_t attend(const PagedAttnArgs& a, int nt, hipStream_t stream) {
+  const int64_t cols = (int64_t)a.max_q * a.pc.group();
+  const dim3 grid((unsigned)(a.pc.h_kv * ((cols + 16 * nt - 1) / (16 * nt))), (unsigned)a.n_split, (unsigned)a.pc.n_prob);
+  const size_t lds = (size_t)kWaves * std::min<int64_t>(cols, 16) * D * sizeof(float);
+  if (nt == 1) paged_attn4_kernel<DT, D, 1><<<grid, kThreads, lds, stream>>>(a);
+  else paged_attn4_kernel<DT, D, 2><<<grid, kThreads, lds, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention4(const PagedAttnArgs& a, int nt, hipStream_t stream) {
+  if (a.pc.dtype == kDtBf16) return a.pc.d == 64 ? attend<kDtBf16, 64>(a, nt, stream) : attend<kDtBf16, 128>(a, nt, stream);
+  return a.pc.d == 64 ? attend<kDtF32, 64>(a, nt, stream) : attend<kDtF32, 128>(a, nt, stream);
+}
+
+}  // namespace kv

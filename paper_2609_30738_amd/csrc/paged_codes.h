@@ -1,11 +1,17 @@
-// Device side of the 8-bit paged cache: codes and scales.
+// Device side of the paged cache: codes and scales.
 //
-// A scale is a power of two (or 0: a block of zeros), the least one with max|x| <= 448 s for e4m3
+// 8 bits.  // A scale is a power of two (or 0: a block of zeros), the least one with max|x| <= 448 s for e4m3
 // and 127 s for int8 over the block's finite values.  A value is code * s: exact in bf16, whatever the
 // code, while it is a normal number (e4m3's smallest code at scales below 2^-117 is not: it may become 0).
 // A power of two costs e4m3 nothing (its precision does not depend on the scale) and int8 up to one bit of
 // its range; in return a block whose scale grows with a later row moves its codes by whole binades, so that
 // e4m3's normal numbers stay as they were, and the codes of given rows are the same on every path.
+//
+// 4 bits.  e2m1 codes, +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}, element 2 i in a byte's low half, and for 32 elements of a row
+// a byte b: the least scale 2^(b - 127) with max|x| <= 6 2^(b - 127), 2 <= b <= 252.  With a scale for each row and
+// 32 elements no code depends on other rows, so that rows can be written in any order.  The bounds keep every code but 0
+// times its scale a normal finite number, in bf16 as in fp32: a row that a mask leaves out can hold any byte and adds
+// 0 times it, 0.  The conversions from and to four bits take a scale's exponent alone.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -19,6 +25,14 @@ namespace kv {
 typedef __bf16 __attribute__((ext_vector_type(2))) bf16x2_t;
 typedef uint32_t __attribute__((ext_vector_type(2))) u32x2_t;
 typedef uint32_t __attribute__((ext_vector_type(4))) u32x4_t;
+
+// Two floats as a bf16 pair, rounded to nearest even.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  bf16x2_t r;
+  r[0] = (__bf16)a;
+  r[1] = (__bf16)b;
+  return __builtin_bit_cast(uint32_t, r);
+}
 
 // The scale of a block whose largest finite |x| has these bits.
 template <int QT> __device__ __forceinline__ float block_scale(uint32_t amax_bits) {
@@ -92,6 +106,38 @@ template <int QT, int H> __device__ __forceinline__ uint32_t decode2_bf16(uint32
     return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
   }
 }
+
+// ---- 4 bits
+
+constexpr int kGroup4 = 32;      // elements that share a scale
+constexpr uint32_t kTop4 = 252;  // the largest scale byte
+
+// The scale byte of elements whose largest finite |x| has these bits: 6 = 1.5 2^2.
+__device__ __forceinline__ uint32_t scale_byte4(uint32_t amax_bits) {
+  const int e = (int)(amax_bits >> 23) - 2 + ((amax_bits & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+  return (uint32_t)min(max(e, 2), (int)kTop4);
+}
+__device__ __forceinline__ float scale4(uint32_t byte) { return __uint_as_float(min(byte, kTop4) << 23); }
+
+// Two bf16 values (no NaN) as codes in units of the scale, rounded to nearest even, past 6, 6, in the byte SEL of u.
+template <int SEL> __device__ __forceinline__ uint32_t encode2_bf16(uint32_t u, uint32_t pair, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(u, __builtin_bit_cast(bf16x2_t, pair), scale, SEL);
+}
+__device__ __forceinline__ uint32_t encode8_bf16(const u32x4_t& x, float scale) {
+  return encode2_bf16<3>(encode2_bf16<2>(encode2_bf16<1>(encode2_bf16<0>(0u, x[0], scale), x[1], scale), x[2], scale), x[3], scale);
+}
+// The same of two fp32 values.
+template <int SEL> __device__ __forceinline__ uint32_t encode2_f32(uint32_t u, float a, float b, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, a, b, scale, SEL);
+}
+// The two codes of byte SEL times the scale as a bf16 pair, and as fp32.
+template <int SEL> __device__ __forceinline__ uint32_t decode2_e2m1(uint32_t u, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, scale, SEL));
+}
+__device__ __forceinline__ u32x4_t decode8_e2m1(uint32_t u, float scale) {
+  return u32x4_t{decode2_e2m1<0>(u, scale), decode2_e2m1<1>(u, scale), decode2_e2m1<2>(u, scale), decode2_e2m1<3>(u, scale)};
+}
+
 template <int QT> __device__ __forceinline__ u32x2_t decode4_bf16(uint32_t u, float scale = 1.f) {
   return u32x2_t{decode2_bf16<QT, 0>(u, scale), decode2_bf16<QT, 1>(u, scale)};
 }

@@ -133,22 +133,30 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
   // Staging: a wave takes the rows of 1 KB of K and of V, 16 bytes a lane.  They lie in one 16-row group, so
   // block, scale and address are the wave's.  Blocks and scales come from LDS: scalar loads return out of order
   // with the reads of the products' operands, which then have to be waited for all at once (177 us of 1900).
+  // (e2m1: 8 bytes a lane, and the byte of their scale)
+  constexpr bool kFour = QT == kQtE2m1;
   constexpr int ROWS = 1024 / D, NTASK = kTile / (ROWS * W) > 0 ? kTile / (ROWS * W) : 1;
+  using Codes = std::conditional_t<kFour, u32x2_t, u32x4_t>;
   static_assert(ROWS <= 16, "a task lies in one block");
   const int wv = __builtin_amdgcn_readfirstlane(wave), lane_row = lane / (D / 16), lane_e = lane % (D / 16) * 16;
   int32_t id[NTASK];  // the block of the tile after the codes', and its scales
   float next_ks[NTASK], next_vs[NTASK];
-  u32x4_t kc[NTASK], vc[NTASK];
+  Codes kc[NTASK], vc[NTASK];
   float ksc[NTASK], vsc[NTASK];
+  uint32_t ksb[NTASK], vsb[NTASK];
   bool has[NTASK];
   for (int i = tid; i << shift < r1 - r0; i += 64 * W) {
     int block = a.pc.table[(int64_t)p * a.pc.table_stride + (r0 >> shift) + i];
     if ((uint32_t)block >= (uint32_t)a.pc.n_blocks) block = -1;
+    if constexpr (kFour) {
+      blocks.id[i] = block;
+      continue;
+    }
     const int64_t unit = (int64_t)max(block, 0) * a.pc.h_kv + g;
     // The conversion takes a scale's exponent alone, and an infinity in V would reach columns that do not see it (as
     // 0 times it): a block with another scale than block_scale's, or of values that leave bf16, gives NaN logits,
     // which reach the columns that see it.
-    const float ks = a.pc.k_scale[unit], vs = a.pc.v_scale[unit];
+    const float ks = static_cast<const float*>(a.pc.k_scale)[unit], vs = static_cast<const float*>(a.pc.v_scale)[unit];
     const bool ok = is_bf16_scale<QT>(ks) && is_bf16_scale<QT>(vs);
     blocks.id[i] = block;
     blocks.k_scale[i] = ok ? ks : NAN;
@@ -163,8 +171,10 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       const int r = t * kTile + task_row(i);
       const int at = min(r, r1 - r0 - 1) >> shift;
       id[i] = blocks.id[at];
-      next_ks[i] = blocks.k_scale[at];
-      next_vs[i] = blocks.v_scale[at];
+      if constexpr (!kFour) {
+        next_ks[i] = blocks.k_scale[at];
+        next_vs[i] = blocks.v_scale[at];
+      }
       if (r0 + r >= r1) id[i] = -1;
     }
   };
@@ -175,14 +185,30 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
       const int block = __builtin_amdgcn_readfirstlane(id[i]);
       has[i] = block >= 0;
       const int64_t unit = (int64_t)max(block, 0) * a.pc.h_kv + g;
-      const int64_t at = ((unit << shift) + ((r0 + t * kTile + task_row(i)) & (R - 1))) * D;
+      const int in = (r0 + t * kTile + task_row(i)) & (R - 1);
+      if constexpr (kFour) {
+        const int64_t at = ((unit << shift) + in) * (D / 2), sat = (unit << shift) * (D / kGroup4) + in;
+        const uint32_t mine = (uint32_t)(lane_e / kGroup4 * R + lane_row);
+        kc[i] = *reinterpret_cast<const u32x2_t*>(a.pc.k + at + 8 * (uint32_t)lane);
+        vc[i] = *reinterpret_cast<const u32x2_t*>(a.pc.v + at + 8 * (uint32_t)lane);
+        ksb[i] = (static_cast<const uint8_t*>(a.pc.k_scale) + sat)[mine];
+        vsb[i] = (static_cast<const uint8_t*>(a.pc.v_scale) + sat)[mine];
+        continue;
+      } else {
+      const int64_t at = ((unit << shift) + in) * D;
       kc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.k + at + 16 * (uint32_t)lane);
       vc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.v + at + 16 * (uint32_t)lane);
       ksc[i] = next_ks[i];
       vsc[i] = next_vs[i];
+      }
     }
   };
-  auto put = [&](uint16_t* to, const u32x4_t& c, float scale) __attribute__((always_inline)) {
+  auto put = [&](uint16_t* to, const Codes& c, float scale) __attribute__((always_inline)) {
+    if constexpr (kFour) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w) *reinterpret_cast<u32x4_t*>(to + 8 * w) = decode8_e2m1(c[w], scale);
+      return;
+    } else
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       const u32x2_t y = decode4_bf16<QT>(c[2 * w], scale), z = decode4_bf16<QT>(c[2 * w + 1], scale);
@@ -202,11 +228,15 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
         asm volatile("" : "+v"(kc[i][0]), "+v"(kc[i][1]), "+v"(kc[i][2]), "+v"(kc[i][3]));
         asm volatile("" : "+v"(vc[i][0]), "+v"(vc[i][1]), "+v"(vc[i][2]), "+v"(vc[i][3]));
       }
+      if constexpr (kFour) {
+        ksc[i] = scale4(ksb[i]);
+        vsc[i] = scale4(vsb[i]);
+      }
       // (a missing block's or a later row's K may be anything: its logits are masked)
       put(&x.k[r * T::KS + lane_e], kc[i], ksc[i]);
-      if (!has[i] || rb + task_row(i) + ROWS > r1) {
+      if (!kFour && (!has[i] || rb + task_row(i) + ROWS > r1)) {
         // a row that no column sees holds anything: zero its values, so that 0 times them is 0
-        if (!has[i] || rb + r >= r1) vc[i] = u32x4_t{0u, 0u, 0u, 0u};
+        if (!has[i] || rb + r >= r1) vc[i] = Codes{};
       }
       if (QT == kQtE4m3 && rb + kTile > vis_min) {
 #pragma unroll
@@ -423,6 +453,7 @@ hipError_t launch_paged_prompt(const PagedAttnArgs& a, int waves, hipStream_t st
   auto d = [&](auto qt) {
     return a.pc.d == 64 ? w(qt, std::integral_constant<int, 64>{}) : w(qt, std::integral_constant<int, 128>{});
   };
+  if (a.pc.qtype == kQtE2m1) return d(std::integral_constant<int, kQtE2m1>{});
   return a.pc.qtype == kQtE4m3 ? d(std::integral_constant<int, kQtE4m3>{}) : d(std::integral_constant<int, kQtInt8>{});
 }
 

@@ -1,4 +1,4 @@
-// Rows into the 8-bit blocks of a paged cache: new tokens (kv_paged_append) and the rows that an
+// Rows into the blocks of a paged cache: new tokens (kv_paged_append) and the rows that an
 // eviction keeps (kv_paged_compact).
 //
 // A wave takes the rows of one (block, kv head) of K or of V, 16 bytes a lane and load, and holds them in
@@ -17,153 +17,14 @@
 
 #include "compact_rows.h"
 #include "paged.h"
-#include "paged_codes.h"
+#include "paged_rows.h"
 
 namespace kv {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kStoreThreads;
 constexpr int kWaves = kThreads / 64;
-
-typedef uint16_t __attribute__((ext_vector_type(2))) u16x2_t;
-
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
-}
-
-// The values of a 16-byte chunk.
-template <int DT> __device__ __forceinline__ void chunk_values(const u32x4_t& u, float (&f)[16 / sizeof(typename Elem<DT>::T)]) {
-  if constexpr (DT == kDtBf16) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(u[i] << 16);
-      f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(u[i]);
-  }
-}
-
-template <int QT, bool kFinite, int EPT> __device__ __forceinline__ void store_chunk(uint8_t* dst, const float (&f)[EPT], float inv) {
-  if constexpr (EPT == 8) {
-    u32x2_t u;
-    u[0] = encode4<QT, kFinite>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-    u[1] = encode4<QT, kFinite>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
-    *reinterpret_cast<u32x2_t*>(dst) = u;
-  } else {
-    *reinterpret_cast<uint32_t*>(dst) = encode4<QT, kFinite>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-  }
-}
-
-// Chunks of a lane in a block of 1 << SHIFT rows.
-template <int DT, int D, int SHIFT> constexpr int kChunks = ((D * (int)sizeof(typename Elem<DT>::T)) << SHIFT) / 1024;
-// Chunks that a lane holds in registers; blocks of more (fp32, 128 rows of 128) are read twice: 89,000 fp32 rows (910 MB)
-// 335 us, in blocks of 64 rows 279.
-constexpr int kHeldChunks = 32;
-
-// The scale of a block that holds row0 rows at scale `old` and gets rows whose own scale is s: the held codes move
-// by whole binades where s is larger.  Every lane of the wave calls it.
-template <int QT, int D> __device__ __forceinline__ float grown_scale(uint8_t* codes, int row0, float old, float s) {
-  if (row0 == 0) return s;
-  if (old >= s && old < INFINITY) return old;
-  const float f = old > 0.f && old < s ? old * inv_scale(s) : 0.f;
-  u32x4_t* at = reinterpret_cast<u32x4_t*>(codes);
-  for (int i = threadIdx.x & 63; i < row0 * D / 16; i += 64) {
-    u32x4_t u = at[i];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      float y[4];
-      decode4<QT>(u[w], y);
-      u[w] = encode4<QT, false>(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
-    }
-    at[i] = u;
-  }
-  return s;
-}
-
-// store_rows for any values: read twice, infinities and NaNs apart.
-template <int DT, int QT, int D, typename Load>
-__device__ __forceinline__ void store_rows_any(uint8_t* codes, float* scale, int row0, int n, Load load) {
-  constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH;
-  const int lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
-  const float old = row0 > 0 ? *scale : 0.f;
-  uint32_t amax = 0;
-#pragma unroll 4
-  for (int i = 0; i * RPP < n; ++i) {
-    float f[EPT];
-    chunk_values<DT>(load(i), f);
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const uint32_t u = __float_as_uint(f[e]) & 0x7FFFFFFFu;
-      amax = max(amax, u < 0x7F800000u ? u : 0u);
-    }
-  }
-  const float s = grown_scale<QT, D>(codes, row0, old, block_scale<QT>(wave_max_u32(amax))), inv = inv_scale(s);
-#pragma unroll 4
-  for (int i = 0; i * RPP < n; ++i) {
-    float f[EPT];
-    chunk_values<DT>(load(i), f);
-    if (i * RPP + rr < n) store_chunk<QT, false>(codes + (row0 + i * RPP + rr) * D + c * EPT, f, inv);
-  }
-  if (lane == 0) *scale = s;
-}
-
-// Rows row0 .. row0 + n - 1 of one block and head; the block holds row0 rows already.  load(i): the lane's 16-byte
-// chunk, number lane % CH of row i RPP + lane / CH of the new ones (zeros past the last).  Every lane of the wave
-// calls it.
-template <int DT, int QT, int D, int SHIFT, typename Load>
-__device__ __forceinline__ void store_rows(uint8_t* codes, float* scale, int row0, int n, Load load) {
-  constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH;
-  constexpr int NC = kChunks<DT, D, SHIFT>;
-  if constexpr (NC > kHeldChunks) {
-    store_rows_any<DT, QT, D>(codes, scale, row0, n, load);
-    return;
-  } else {
-    const int lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
-    const float old = row0 > 0 ? *scale : 0.f;
-    u32x4_t x[NC];
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      x[i] = u32x4_t{0u, 0u, 0u, 0u};
-      if (i * RPP < n) x[i] = load(i);
-    }
-    uint32_t amax = 0;  // without the signs; two bf16 at a time
-#pragma unroll
-    for (int i = 0; i < NC; ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        if constexpr (DT == kDtBf16) {
-          const u16x2_t u = __builtin_bit_cast(u16x2_t, x[i][w] & 0x7FFF7FFFu);
-          amax = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, amax), u));
-        } else {
-          amax = max(amax, x[i][w] & 0x7FFFFFFFu);
-        }
-      }
-    if constexpr (DT == kDtBf16) amax = max(amax << 16, amax & 0xFFFF0000u);
-    amax = wave_max_u32(amax);
-    if (amax >= 0x7F800000u) {  // an infinity or a NaN among them
-      store_rows_any<DT, QT, D>(codes, scale, row0, n, load);
-      return;
-    }
-    const float s = grown_scale<QT, D>(codes, row0, old, block_scale<QT>(amax)), inv = inv_scale(s);
-    uint8_t* to = codes + row0 * D + rr * D + c * EPT;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      // (a value's conversion is not kept from the first pass over the chunks: registers)
-      asm volatile("" : "+v"(x[i][0]), "+v"(x[i][1]), "+v"(x[i][2]), "+v"(x[i][3]));
-      if (i * RPP + rr < n) {
-        float f[EPT];
-        chunk_values<DT>(x[i], f);
-        store_chunk<QT, true>(to + i * RPP * D, f, inv);
-      }
-    }
-    if (lane == 0) *scale = s;
-  }
-}
 
 }  // namespace
 
@@ -217,8 +78,8 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
     // a wave-uniform address and a lane's 32-bit offset
     const uint8_t* src = static_cast<const uint8_t*>(kv ? a.v_new : a.k_new) + (int64_t)t0 * a.tok_bytes + g * (CH * 16);
     const uint32_t mine = lane / CH * a.tok_bytes + lane % CH * 16;
-    store_rows<DT, QT, D, SHIFT>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit,
-                                 row0, n, [&](int i) {
+    store_rows<DT, QT, D, SHIFT>(unit_codes<QT, D, SHIFT>(kv ? a.pc.v : a.pc.k, unit),
+                                 unit_scale<QT, D, SHIFT>(kv ? a.pc.v_scale : a.pc.k_scale, unit), row0, n, [&](int i) {
                                    u32x4_t x = {0u, 0u, 0u, 0u};
                                    if (i * RPP + lane / CH < n)
                                      x = *reinterpret_cast<const u32x4_t*>(src + (int64_t)i * RPP * a.tok_bytes + mine);
@@ -355,8 +216,9 @@ __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArg
     const u32x4_t* src = static_cast<const u32x4_t*>(kv ? a.v : a.k) + base;
     const int64_t unit = (int64_t)block * a.pc.h_kv + g;
     const int r0 = j << SHIFT;
-    store_rows<DT, QT, D, SHIFT>((kv ? a.pc.v : a.pc.k) + unit * R * D, (kv ? a.pc.v_scale : a.pc.k_scale) + unit, 0,
-                                 min(R, rows - r0), [&](int i) {
+    store_rows<DT, QT, D, SHIFT>(unit_codes<QT, D, SHIFT>(kv ? a.pc.v : a.pc.k, unit),
+                                 unit_scale<QT, D, SHIFT>(kv ? a.pc.v_scale : a.pc.k_scale, unit), 0, min(R, rows - r0),
+                                 [&](int i) {
                                    // without a branch, so that the rows' loads are in flight together
                                    const int r = min(r0 + i * RPP + lane / CH, rows - 1);
                                    const int kept = n > 0 ? lds[min(r - first, n - 1)] : 0;
@@ -367,27 +229,6 @@ __global__ __launch_bounds__(kThreads) void paged_compact_kernel(PagedCompactArg
                                  });
   }
 }
-
-namespace {
-
-template <int V> using Int = std::integral_constant<int, V>;
-
-// f(dtype, qtype, d, shift) of integral constants.
-template <typename F> hipError_t dispatch(const Paged& pc, F f) {
-  auto shift = [&](auto dt, auto qt, auto d) {
-    switch (pc.shift) {
-      case 4: return f(dt, qt, d, Int<4>{});
-      case 5: return f(dt, qt, d, Int<5>{});
-      case 6: return f(dt, qt, d, Int<6>{});
-      default: return f(dt, qt, d, Int<7>{});
-    }
-  };
-  auto d = [&](auto dt, auto qt) { return pc.d == 64 ? shift(dt, qt, Int<64>{}) : shift(dt, qt, Int<128>{}); };
-  auto q = [&](auto dt) { return pc.qtype == kQtE4m3 ? d(dt, Int<kQtE4m3>{}) : d(dt, Int<kQtInt8>{}); };
-  return pc.dtype == kDtBf16 ? q(Int<kDtBf16>{}) : q(Int<kDtF32>{});
-}
-
-}  // namespace
 
 hipError_t launch_paged_append(const Paged& pc, const void* k_new, const void* v_new, int64_t tok_stride,
                                const int32_t* slots, int n_tok, hipStream_t stream) {
