@@ -424,7 +424,8 @@ int kv_decode_attention(const kv_cache_batch* cb, const void* q, void* k_cache, 
  *     [n_blocks][h_kv][d / 32][block_rows] bytes b, one for 32 elements of a row: an element is code * 2^(b - 127).  A written
  *     byte is the least with max|x| <= 6 2^(b - 127) over the 32 elements' finite ones, at least 2 and at most 252 (larger
  *     elements, above 2.5e38, become 6 2^125); a code is nearest, ties to the even one.  An infinity takes the largest code of its
- *     sign, a NaN becomes 0.  Reading takes any byte (above 252 as 252).  No row's codes depend on another row.
+ *     sign, a NaN becomes 0.  A row with a byte above 252 (never
+ *     written) may give the tokens that see it infinities or NaN, and no others.  No row's codes depend on another row.
  *   - A table entry outside [0, n_blocks) is a missing block: its rows are not written, and not seen.
  *   - Rows of a block that no problem has written may hold anything.
  * dtype: of queries, new rows and outputs.  n_blocks * block_rows and table_stride * block_rows below

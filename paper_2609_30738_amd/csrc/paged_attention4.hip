@@ -26,7 +26,7 @@ constexpr int kThreads = kAttnThreads;
 constexpr int kWaves = kAttnWaves;
 
 // Tiles of 16 rows in a wave's step, and the waves per SIMD that the registers are held to.
-template <int NT> constexpr int kTiles4 = NT == 1 ? 2 : 2;
+constexpr int kTiles4 = 2;
 template <int DT, int D, int NT> constexpr int kMinWaves4 = (NT == 1 ? 3 : 2) - (DT == kDtF32 && D == 128 ? 1 : 0);
 
 }  // namespace
@@ -37,9 +37,9 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   constexpr int NI = D / 16;                       // 16-wide tiles of the output, elements of V that a lane takes
   constexpr int KW = D / 32;                       // words of a key that a lane takes
   constexpr int RB = D / 2, NG = D / kGroup4;      // bytes and scales of a row
-  constexpr int TS = kTiles4<NT>, STEP = 16 * TS;
+  constexpr int TS = kTiles4, STEP = 16 * TS;
   constexpr int QN = DT == kDtBf16 ? 1 : 3;        // bf16 terms of a query
-  constexpr int PN = DT == kDtF32 ? 3 : (NT == 1 ? 2 : 1);  // and of a weight
+  constexpr int PN = DT == kDtF32 ? 3 : (NT == 1 ? 2 : 1);  // bf16 terms of a weight
   constexpr int COLS = 16 * NT;
   __shared__ int32_t sh_block[kMaxSplitBlocks];
   __shared__ float sh_m[kWaves][16], sh_s[kWaves][16];
@@ -48,7 +48,8 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   const int p = blockIdx.z, g = blockIdx.x % a.pc.h_kv, cg = blockIdx.x / a.pc.h_kv, G = a.pc.h_q / a.pc.h_kv;
   // (the problems' splits start one further each: with fewer heads than XCDs, these take long caches' ends in turn)
   const int split = a.n_split > 1 ? (int)((blockIdx.y + (uint32_t)p) % (uint32_t)a.n_split) : 0;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, kg = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int shift = a.pc.shift, R = 1 << shift;
   const int r0 = split * a.split_rows;
   // the split's table entries load beside the lengths
@@ -68,59 +69,64 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   if (tid < kMaxSplitBlocks) sh_block[tid] = has ? id : -1;
   __syncthreads();
 
-  // The codes and scales of a step's rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n.
+  // The codes and scales of a step's rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n;
+  // their blocks, and where these lie.
   uint32_t xk[TS][KW], xv[TS][4], ksb[TS];
   u32x4_t vsb[TS];  // of 16 rows
+  int blk[TS], next_blk[TS];
+  int64_t codes_at[TS], scales_at[TS];
   const int k_row = 4 * (n & 3) + (n >> 2);
   // a wave-uniform address and a lane's 32-bit offset
   const uint32_t k_lane = k_row * RB + kg * (4 * KW), v_lane = kg * RB + n * (NI / 2);
-  const uint32_t ks_lane = (kg * (D / 4) / kGroup4) * R + k_row, vs_lane = (n * NI / kGroup4) * R;
-  auto tile_at = [&](int rb, int t, int64_t& codes, int64_t& scales) {
-    const int r = min(rb + 16 * t, (r1 - 1) & ~15) - r0;
-    const int64_t id = max(__builtin_amdgcn_readfirstlane(sh_block[r >> shift]), 0);
-    const int64_t unit = id * a.pc.h_kv + g;
-    codes = (unit << shift) * RB + (r & (R - 1)) * RB;
-    scales = (unit << shift) * NG + (r & (R - 1));
-  };
-  auto load_k = [&](int rb) __attribute__((always_inline)) {
+  const uint32_t ks_lane = (kg * (8 * KW) / kGroup4) * R + k_row, vs_lane = (n * NI / kGroup4) * R;
+  auto locate = [&](int rb) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < TS; ++t) {
-      int64_t codes, scales;
-      tile_at(rb, t, codes, scales);
-      const uint8_t* ks = a.pc.k + codes + k_lane;
+      const int r = min(rb + 16 * t, (r1 - 1) & ~15) - r0;
+      next_blk[t] = __builtin_amdgcn_readfirstlane(sh_block[r >> shift]);
+      const int64_t unit = (int64_t)max(next_blk[t], 0) * a.pc.h_kv + g;
+      codes_at[t] = (unit << shift) * RB + (r & (R - 1)) * RB;
+      scales_at[t] = (unit << shift) * NG + (r & (R - 1));
+    }
+  };
+  auto load_k = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TS; ++t) {
+      const uint8_t* ks = a.pc.k + codes_at[t];
       if constexpr (KW == 4) {
-        const u32x4_t u = load_code<NT == 1>(reinterpret_cast<const u32x4_t*>(ks));
+        const u32x4_t u = load_code<NT == 1>(reinterpret_cast<const u32x4_t*>(ks + k_lane));
 #pragma unroll
         for (int i = 0; i < 4; ++i) xk[t][i] = u[i];
       } else {
-        const u32x2_t u = load_code<NT == 1>(reinterpret_cast<const u32x2_t*>(ks));
+        const u32x2_t u = load_code<NT == 1>(reinterpret_cast<const u32x2_t*>(ks + k_lane));
         xk[t][0] = u[0];
         xk[t][1] = u[1];
       }
-      ksb[t] = *(static_cast<const uint8_t*>(a.pc.k_scale) + scales + ks_lane);
+      ksb[t] = (static_cast<const uint8_t*>(a.pc.k_scale) + scales_at[t])[ks_lane];
     }
   };
-  auto load_v = [&](int rb) __attribute__((always_inline)) {
+  auto load_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < TS; ++t) {
-      int64_t codes, scales;
-      tile_at(rb, t, codes, scales);
-      const uint8_t* vs = a.pc.v + codes;
+      const uint8_t* vs = a.pc.v + codes_at[t];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (NI == 8) xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint32_t*>(vs + (v_lane + 4 * j * RB)));
         else xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint16_t*>(vs + (v_lane + 4 * j * RB)));
       }
-      vsb[t] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.pc.v_scale) + scales + vs_lane);
+      vsb[t] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.pc.v_scale) + scales_at[t] + vs_lane);
     }
   };
 
   constexpr int kRound = kWaves * STEP;
   const int rb0 = r0 + wave * STEP;
   if (rb0 < r1) {
-    load_k(rb0);
-    load_v(rb0);
+    locate(rb0);
+    load_k();
+    load_v();
   }
+  // a negative scale turns the queries' signs; a scale of 0 gives equal weights, as the least number does
+  const float c = fmaxf(fabsf(a.c), 0x1p-126f);
   // the queries' operand: column n, elements D / 4 kg + 8 s .. + 7
   u32x4_t qf[NT][NS][QN];
   int vis[NT];
@@ -136,37 +142,43 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
       const int e = D / 4 * kg + 8 * s;
       if constexpr (DT == kDtBf16) {
         qf[ct][s][0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at + e);
+        if (a.c < 0.f) qf[ct][s][0] ^= 0x80008000u;
       } else {
         const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + e);
         const float4 x = src[0], y = src[1];
-        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        if (a.c < 0.f) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = -f[i];
+        }
         split_terms<QN>(f, qf[ct][s]);
       }
     }
   }
 
-  float m[NT], mu[NT], sum[NT];  // mu: m, or 0 before the first finite logit
-  f32x4v acc[NT][NI];
+  float m[NT], mu[NT];  // mu: m (0 before the first finite logit) and kSlack octaves
+  f32x4v acc[NT][NI], sum[NT];
 #pragma unroll
   for (int ct = 0; ct < NT; ++ct) {
     m[ct] = -INFINITY;
-    mu[ct] = 0.f;
-    sum[ct] = 0.f;
+    mu[ct] = kSlack;
+    sum[ct] = f32x4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NI; ++i) acc[ct][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
   }
+  const uint32_t v_turn = (8 * kg + 9) & 31;  // turns byte kg of a word to a float's exponent
 
   // A step's rows; the codes of the step at `next` (if any) load as this one's are used up.
   auto step = [&](int rb, int next) __attribute__((always_inline)) {
-    int blk[TS], any = 0;
+    int any = 0;
 #pragma unroll
     for (int t = 0; t < TS; ++t) {
-      blk[t] = __builtin_amdgcn_readfirstlane(sh_block[(min(rb + 16 * t, (r1 - 1) & ~15) - r0) >> shift]);
+      blk[t] = next_blk[t];
       any |= blk[t];
     }
     // its rows are not all visible to every column, or a block is missing
     const bool masked = rb + STEP > vis_min || any < 0;
-    float lg[NT][4 * TS];
+    f32x4v lg[NT][TS];
     // (codes are converted here, not where they were loaded a step before: registers)
 #pragma unroll
     for (int t = 0; t < TS; ++t)
@@ -174,51 +186,48 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
       for (int i = 0; i < KW; ++i) asm volatile("" : "+v"(xk[t][i]));
 #pragma unroll
     for (int t = 0; t < TS; ++t) {
-      f32x4v s4[NT];
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) s4[ct] = f32x4v{0.f, 0.f, 0.f, 0.f};
-      const float ksc = scale4(ksb[t]);
+      for (int ct = 0; ct < NT; ++ct) lg[ct][t] = f32x4v{0.f, 0.f, 0.f, 0.f};
+      const float ksc = __uint_as_float(ksb[t] << 23);
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const u32x4_t kf = decode8_e2m1(xk[t][s], ksc);
 #pragma unroll
+        for (int q = QN - 1; q >= 0; --q)
+#pragma unroll
+          for (int ct = 0; ct < NT; ++ct) lg[ct][t] = mfma16(kf, qf[ct][s][q], lg[ct][t]);
+      }
+      if (masked) {
+#pragma unroll
         for (int ct = 0; ct < NT; ++ct)
 #pragma unroll
-          for (int q = QN - 1; q >= 0; --q) s4[ct] = mfma16(kf, qf[ct][s][q], s4[ct]);
+          for (int j = 0; j < 4; ++j)
+            if (blk[t] < 0 || rb + 16 * t + 4 * j + kg >= vis[ct]) lg[ct][t][j] = -INFINITY;
       }
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float l = s4[ct][j] * a.c;
-          if (masked && (blk[t] < 0 || rb + 16 * t + 4 * j + kg >= vis[ct])) l = -INFINITY;
-          lg[ct][4 * t + j] = l;
-        }
     }
-    if (next < r1) load_k(next);
+    if (next < r1) {
+      locate(next);
+      load_k();
+    }
+    float top[NT];
     bool over = false;
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) {
-      float tm = lg[ct][0];
+      top[ct] = lg[ct][0][0];
 #pragma unroll
-      for (int e = 1; e < 4 * TS; ++e) tm = fmaxf(tm, lg[ct][e]);
-      over = over || tm > m[ct] + kSlack;
+      for (int e = 1; e < 4 * TS; ++e) top[ct] = fmaxf(top[ct], lg[ct][e >> 2][e & 3]);
+      over = over || fmaf(top[ct], c, -m[ct]) > kSlack;
     }
     if (__ballot(over)) {
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
-        float tm = lg[ct][0];
-#pragma unroll
-        for (int e = 1; e < 4 * TS; ++e) tm = fmaxf(tm, lg[ct][e]);
-        const float mn = fmaxf(m[ct], column_max(tm));
+        const float mn = fmaxf(m[ct], column_max(top[ct]) * c);
         const float f = m[ct] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[ct] - mn);
         m[ct] = mn;
-        mu[ct] = mn == -INFINITY ? 0.f : mn;
+        mu[ct] = mn == -INFINITY ? kSlack : mn + kSlack;
         sum[ct] *= f;
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[ct][i][j] *= f;
+        for (int i = 0; i < NI; ++i) acc[ct][i] *= f;
       }
     }
 #pragma unroll
@@ -228,17 +237,24 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
       for (int ct = 0; ct < NT; ++ct) {
         float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] = __builtin_amdgcn_exp2f(lg[ct][8 * u + e] - mu[ct]) * kSlackScale;
-          sum[ct] += w[e];
-        }
+        for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(lg[ct][2 * u + (e >> 2)][e & 3], c, -mu[ct]));
         split_terms<PN>(w, pf[ct]);
+        // their sum: as the products take them, with a row of ones
+        const u32x4_t one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+        for (int q = PN - 1; q >= 0; --q) sum[ct] = mfma16(one, pf[ct][q], sum[ct]);
       }
       float vsc[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         asm volatile("" : "+v"(xv[2 * u + (e >> 2)][e & 3]));
-        vsc[e] = scale4(vsb[2 * u + (e >> 2)][e & 3] >> (8 * kg) & 255u);
+        const uint32_t s = vsb[2 * u + (e >> 2)][e & 3];
+        vsc[e] = __uint_as_float(__builtin_amdgcn_alignbit(s, s, v_turn));
+      }
+      if (masked) {
+        // a row that a column does not see adds 0 times its values: these have to be finite
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vsc[e] = fminf(fabsf(vsc[e]), 0x1p125f);
       }
       // V^T: pairs of elements of eight rows, put together as pairs of rows
       auto pair = [&](auto b) __attribute__((always_inline)) {
@@ -264,7 +280,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
         pair(std::integral_constant<int, 3>{});
       }
     }
-    if (next < r1) load_v(next);
+    if (next < r1) load_v();
   };
 
   for (int rb = rb0; rb < r1; rb += kRound) step(rb, rb + kRound);  // the waves' steps in turn
@@ -274,10 +290,9 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   for (int ct = 0; ct < NT; ++ct) {
     const int cols = min(n_cols - 16 * ct, 16);
     if (cols <= 0) break;
-    const float s = column_sum(sum[ct]);
     if (kg == 0) {
       sh_m[wave][n] = m[ct];
-      sh_s[wave][n] = s;
+      sh_s[wave][n] = sum[ct][0];
     }
     if (n < cols) {
 #pragma unroll
