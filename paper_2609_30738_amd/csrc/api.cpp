@@ -884,6 +884,8 @@ int check_tokens(const kv::Paged& pc, int32_t n_tok, int32_t max_q, kv::PagedPla
   if (n_tok < 1 || max_q < 1 || max_q > n_tok) return KV_ERR_ARG;
   if (max_q > kMaxLen) return KV_ERR_SHAPE;
   *plan = kv::paged_plan(pc, max_q);
+  // the rounds of all problems are counted in 32 bits
+  if (plan->shares && ((int64_t)pc.max_len / 128 + 1) * pc.n_prob > INT32_MAX) return KV_ERR_SHAPE;
   return kv::paged_grid_groups(pc, max_q, *plan) > kMaxGrid ? KV_ERR_SHAPE : KV_OK;
 }
 
@@ -1058,7 +1060,7 @@ size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* c, int32_t n_tok
   kv::Paged pc{};
   kv::PagedPlan plan;
   if (check_paged(c, &pc) != KV_OK || check_tokens(pc, n_tok, max_q, &plan) != KV_OK) return 0;
-  return align_up(kv::paged_ws_bytes(pc, n_tok, plan));
+  return align_up(kv::paged_ws_bytes(pc, n_tok, max_q, plan));
 }
 
 int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride, const int32_t* tok_off,
@@ -1076,7 +1078,7 @@ int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride,
   if (!tok_off && (n_tok != a.pc.n_prob || max_q != 1)) return KV_ERR_ARG;
   st = check_stride(a.pc, a.pc.h_q, &q_stride);
   if (st != KV_OK) return st;
-  const size_t need = align_up(kv::paged_ws_bytes(a.pc, n_tok, plan));
+  const size_t need = align_up(kv::paged_ws_bytes(a.pc, n_tok, max_q, plan));
   if (need > 0 && (ws_bytes < need || !ws || (reinterpret_cast<uintptr_t>(ws) & (kWsAlign - 1))))
     return KV_ERR_WORKSPACE;
   a.q = q;
@@ -1089,6 +1091,11 @@ int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride,
   a.split_rows = plan.split_rows;
   a.n_split = plan.n_split;
   a.part = static_cast<float*>(ws);
+  a.shares = plan.shares;
+  if (plan.shares) {
+    a.prefix = static_cast<int32_t*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kv::paged4_prefix_bytes(a.pc, max_q));
+  }
   return launch_status(kv::launch_paged_attention(a, plan, static_cast<hipStream_t>(stream)));
 }
 

@@ -90,20 +90,27 @@ struct PagedAttnArgs {
   void* out;  // [n_tok][h_q][d], the queries' type
   int split_rows, n_split;
   float* part;  // [n_tok][h_q][n_split][d + 2] when n_split > 1
+  // up to 32 columns over 4-bit blocks: workgroups that share a unit's rounds (0: one for each problem), and their prefix sums
+  int shares;
+  int32_t* prefix;
 };
 // prompt_waves: 0 for paged_attention.hip's kernel, else the waves of paged_prompt.hip's (32 columns each).
 struct PagedPlan {
   int split_rows, n_split, prompt_waves;
+  int shares;  // of paged_attention4.hip's kernel, 0: whole problems
 };
 PagedPlan paged_plan(const Paged& pc, int max_q);
 // Workgroups along the grid axis that the columns are on: the second one of paged_prompt.hip's kernel, with its splits,
 // the first one of paged_attention.hip's, with the kv heads.  At most 65535: the limit of a second axis, and on the
 // first what keeps the join's launch (256 threads a column) far below 2^32 threads.
 int64_t paged_grid_groups(const Paged& pc, int max_q, const PagedPlan& plan);
-size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan);
+size_t paged_ws_bytes(const Paged& pc, int n_tok, int max_q, const PagedPlan& plan);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t stream);
-// The same without the join, over 4-bit blocks (paged_attention4.hip).  nt: 16-wide column tiles of a wave.
-hipError_t launch_paged_attention4(const PagedAttnArgs& a, int nt, hipStream_t stream);
+// Up to 32 columns at a time over 4-bit blocks (paged_attention4.hip).
+int paged4_shares(const Paged& pc, int max_q);
+size_t paged4_prefix_bytes(const Paged& pc, int max_q);
+size_t paged4_ws_bytes(const Paged& pc, int max_q, int shares);
+hipError_t launch_paged_attention4(const PagedAttnArgs& a, hipStream_t stream);
 // Blocks of a split that the prompt kernel of so many waves holds in LDS beside its tiles
 // (two workgroups of four waves share a CU's 160 KB, one of eight has it alone).
 constexpr int prompt_split_blocks(int waves) { return waves == 4 ? 256 : 4096; }

@@ -463,7 +463,7 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
   const int64_t rows = std::max<int64_t>(1, std::min<int64_t>(pc.max_len, (int64_t)pc.table_stride << pc.shift));
   const int64_t cols = (int64_t)max_q * pc.group();
   PagedPlan plan;
-  plan.prompt_waves = 0;
+  plan.prompt_waves = plan.shares = 0;
   int64_t n = 1, units;
   if (pc.dtype == kDtBf16 && cols > 32) {  // (20 columns 51 us in paged_attn_kernel, 85 in the other)
     plan.prompt_waves = cols <= 128 ? 4 : 8;
@@ -490,6 +490,7 @@ PagedPlan paged_plan(const Paged& pc, int max_q) {
   split = std::min<int64_t>(split, plan.prompt_waves ? (int64_t)prompt_split_blocks(plan.prompt_waves) << pc.shift : kMaxSplitRows);
   plan.split_rows = (int)split;
   plan.n_split = (int)((rows + split - 1) / split);
+  if (pc.qtype == kQtE2m1 && !plan.prompt_waves && plan.n_split > 1) plan.shares = paged4_shares(pc, max_q);
   return plan;
 }
 
@@ -499,7 +500,8 @@ int64_t paged_grid_groups(const Paged& pc, int max_q, const PagedPlan& plan) {
   return (int64_t)pc.h_kv * column_groups(max_q, pc.group());
 }
 
-size_t paged_ws_bytes(const Paged& pc, int n_tok, const PagedPlan& plan) {
+size_t paged_ws_bytes(const Paged& pc, int n_tok, int max_q, const PagedPlan& plan) {
+  if (plan.shares) return paged4_ws_bytes(pc, max_q, plan.shares);
   if (plan.n_split == 1) return 0;
   return (size_t)n_tok * pc.h_q * plan.n_split * (pc.d + 2) * sizeof(float);
 }
@@ -532,9 +534,9 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan,
     return a.pc.qtype == kQtE4m3 ? d(dt, std::integral_constant<int, kQtE4m3>{})
                                  : d(dt, std::integral_constant<int, kQtInt8>{});
   };
-  const hipError_t e = plan.prompt_waves              ? launch_paged_prompt(a, plan.prompt_waves, stream)
-                       : a.pc.qtype == kQtE2m1        ? launch_paged_attention4(a, column_tiles(a.max_q, a.pc.group()), stream)
-                       : bf16                         ? q(std::integral_constant<int, kDtBf16>{})
+  if (a.pc.qtype == kQtE2m1 && !plan.prompt_waves) return launch_paged_attention4(a, stream);
+  const hipError_t e = plan.prompt_waves ? launch_paged_prompt(a, plan.prompt_waves, stream)
+                       : bf16            ? q(std::integral_constant<int, kDtBf16>{})
                                          : q(std::integral_constant<int, kDtF32>{});
   if (e != hipSuccess || a.n_split == 1) return e;
   if (bf16) return a.pc.d == 64 ? combine<kDtBf16, 64>(a, stream) : combine<kDtBf16, 128>(a, stream);

@@ -29,9 +29,50 @@ constexpr int kWaves = kAttnWaves;
 constexpr int kTiles4 = 2;
 template <int DT, int D, int NT> constexpr int kMinWaves4 = (NT == 1 ? 3 : 2) - (DT == kDtF32 && D == 128 ? 1 : 0);
 
+constexpr int kLeastRounds4 = 2;  // of a share
+constexpr int kRound4 = kWaves * 16 * kTiles4;  // rows of a workgroup's round
+
+typedef const __attribute__((address_space(4))) int32_t* uniform_ints;  // read by scalar loads
+
+// Rounds of problem p's rows for the columns from col0 on (at least one if it has such columns).
+__device__ __forceinline__ int rounds_of(const PagedAttnArgs& a, int p, int col0, int cols, int G) {
+  const Span sp = span_of(a, p);
+  const int n = min(sp.n_tok * G - col0, cols);
+  return n <= 0 ? 0 : max(1, (sp.visible((col0 + n - 1) / G) + kRound4 - 1) / kRound4);
+}
+
+// Rounds to a share, of T in n shares.
+__device__ __forceinline__ int share_of(int T, int n) { return max((int)(((int64_t)T + n - 1) / n), kLeastRounds4); }
+
+// Place of a share's part of a unit's column: slot 0 of a problem that begins before the share, 1 of one that ends behind it.
+__device__ __forceinline__ int64_t part4_at(int unit, int share, int slot, int col, int cols, int shares) {
+  return (((int64_t)unit * shares + share) * 2 + slot) * cols + col;
+}
+
+// Inclusive sum over a workgroup; total: of all.  Starts and ends synchronised.
+__device__ __forceinline__ int scan_sum(int v, int& total) {
+  __shared__ int sums[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  if (lane == 63) sums[wave] = v;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) v += sums[w];
+    total += sums[w];
+  }
+  __syncthreads();
+  return v;
+}
+
 }  // namespace
 
-template <int DT, int D, int NT>
+template <int DT, int D, int NT, bool SHARES>
 __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4_kernel(PagedAttnArgs a) {
   constexpr int NS = D / 32;                       // matrix steps over the head dimension
   constexpr int NI = D / 16;                       // 16-wide tiles of the output, elements of V that a lane takes
@@ -41,34 +82,70 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   constexpr int QN = DT == kDtBf16 ? 1 : 3;        // bf16 terms of a query
   constexpr int PN = DT == kDtF32 ? 3 : (NT == 1 ? 2 : 1);  // bf16 terms of a weight
   constexpr int COLS = 16 * NT;
-  __shared__ int32_t sh_block[kMaxSplitBlocks];
   __shared__ float sh_m[kWaves][16], sh_s[kWaves][16];
   extern __shared__ __align__(16) float sh_acc[];  // [kWaves][up to 16 columns][D]
 
-  const int p = blockIdx.z, g = blockIdx.x % a.pc.h_kv, cg = blockIdx.x / a.pc.h_kv, G = a.pc.h_q / a.pc.h_kv;
-  // (the problems' splits start one further each: with fewer heads than XCDs, these take long caches' ends in turn)
-  const int split = a.n_split > 1 ? (int)((blockIdx.y + (uint32_t)p) % (uint32_t)a.n_split) : 0;
+  const int g = blockIdx.x % a.pc.h_kv, G = a.pc.h_q / a.pc.h_kv;
+  const int groups = (a.max_q * G + COLS - 1) / COLS, cg = blockIdx.x / a.pc.h_kv % groups, col0 = cg * COLS;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int shift = a.pc.shift, R = 1 << shift;
-  const int r0 = split * a.split_rows;
-  // the split's table entries load beside the lengths
-  const int entry = (r0 >> shift) + tid;
-  const int id = tid << shift < a.split_rows && entry < a.pc.table_stride
-                     ? a.pc.table[(int64_t)p * a.pc.table_stride + entry] : -1;
-  const Span sp = span_of(a, p);
-  const int col0 = cg * COLS;
-  const int n_cols = min(sp.n_tok * G - col0, COLS);
-  if (n_cols <= 0) return;
-  const int vis_max = sp.visible((col0 + n_cols - 1) / G);
-  const int vis_min = sp.visible(col0 / G);
-  const int r1 = min(vis_max, r0 + a.split_rows);
-  if (r0 >= r1 && a.n_split > 1) return;  // the join reads the splits below a column's last row
 
-  const bool has = tid << shift < r1 - r0 && id >= 0 && id < a.pc.n_blocks;
-  if (tid < kMaxSplitBlocks) sh_block[tid] = has ? id : -1;
-  __syncthreads();
+  // the share: rounds `at` to `end` of all problems' one after the other, from problem p on, whose first one is `base`
+  const int share = SHARES ? (int)(blockIdx.x / a.pc.h_kv / groups) : 0;
+  int p = SHARES ? 0 : (int)blockIdx.z, base = 0, at = 0, end = 1;
+  if constexpr (SHARES) {
+    __shared__ int first[2];
+    int rounds = tid < a.pc.n_prob ? rounds_of(a, tid, col0, COLS, G) : 0, total;
+    int sum = scan_sum(rounds, total), T = total;
+    for (int q = kThreads; q < a.pc.n_prob; q += kThreads) {
+      scan_sum(q + tid < a.pc.n_prob ? rounds_of(a, q + tid, col0, COLS, G) : 0, total);
+      T += total;
+    }
+    const int S = share_of(T, a.shares);
+    at = (int)min((int64_t)share * S, (int64_t)T);
+    end = min(at + S, T);
+    const bool writes = share == 0 && g == 0;
+    if (at >= end && !writes) return;
+    int32_t* prefix = a.prefix + (int64_t)cg * (a.pc.n_prob + 1);  // for the join
+    for (int q = 0, before = 0; q < a.pc.n_prob; q += kThreads) {
+      if (q > 0) {
+        rounds = q + tid < a.pc.n_prob ? rounds_of(a, q + tid, col0, COLS, G) : 0;
+        sum = scan_sum(rounds, total);
+      } else if (a.pc.n_prob > kThreads) {
+        sum = scan_sum(rounds, total);
+      }
+      const int mine = before + sum - rounds;
+      if (at >= mine && at < mine + rounds) {
+        first[0] = q + tid;
+        first[1] = mine;
+      }
+      if (writes && q + tid < a.pc.n_prob) prefix[q + tid] = mine;
+      before += total;
+      if (!writes && before > at) break;
+    }
+    if (writes && tid == 0) prefix[a.pc.n_prob] = T;
+    if (at >= end) return;
+    __syncthreads();
+    p = __builtin_amdgcn_readfirstlane(first[0]);
+    base = __builtin_amdgcn_readfirstlane(first[1]);
+  }
 
+  for (; at < end; ++p) {
+    const Span sp = span_of(a, p);
+    const int n_cols = __builtin_amdgcn_readfirstlane(min(sp.n_tok * G - col0, COLS));
+    if (n_cols <= 0) {
+      if constexpr (SHARES) continue;
+      return;
+    }
+    const int vis_max = __builtin_amdgcn_readfirstlane(sp.visible((col0 + n_cols - 1) / G));
+    const int vis_min = __builtin_amdgcn_readfirstlane(sp.visible(col0 / G));
+    const int all = max(1, (vis_max + kRound4 - 1) / kRound4);  // the problem's rounds, and those of the share
+    const int from = at - base, to = SHARES ? min(end - base, all) : all;
+    const int r0 = from * kRound4, r1 = min(vis_max, to * kRound4);
+    const bool whole = !SHARES || (from == 0 && to == all);
+    at = base + to;
+    base += all;
   // The codes and scales of a step's rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n;
   // their blocks, and where these lie.
   uint32_t xk[TS][KW], xv[TS][4], ksb[TS];
@@ -79,11 +156,18 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   // a wave-uniform address and a lane's 32-bit offset
   const uint32_t k_lane = k_row * RB + kg * (4 * KW), v_lane = kg * RB + n * (NI / 2);
   const uint32_t ks_lane = (kg * (8 * KW) / kGroup4) * R + k_row, vs_lane = (n * NI / kGroup4) * R;
+  // the table entries of a step's rows are read a step before their codes
+  int ahead[TS];
+  const uniform_ints table = (uniform_ints)(uintptr_t)(a.pc.table + (int64_t)p * a.pc.table_stride);
+  auto look = [&](int rb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TS; ++t) ahead[t] = table[min(rb + 16 * t, (r1 - 1) & ~15) >> shift];
+  };
   auto locate = [&](int rb) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < TS; ++t) {
-      const int r = min(rb + 16 * t, (r1 - 1) & ~15) - r0;
-      next_blk[t] = __builtin_amdgcn_readfirstlane(sh_block[r >> shift]);
+      const int r = min(rb + 16 * t, (r1 - 1) & ~15);
+      next_blk[t] = (uint32_t)ahead[t] < (uint32_t)a.pc.n_blocks ? ahead[t] : -1;
       const int64_t unit = (int64_t)max(next_blk[t], 0) * a.pc.h_kv + g;
       codes_at[t] = (unit << shift) * RB + (r & (R - 1)) * RB;
       scales_at[t] = (unit << shift) * NG + (r & (R - 1));
@@ -118,12 +202,13 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
     }
   };
 
-  constexpr int kRound = kWaves * STEP;
   const int rb0 = r0 + wave * STEP;
   if (rb0 < r1) {
+    look(rb0);
     locate(rb0);
     load_k();
     load_v();
+    if (rb0 + kRound4 < r1) look(rb0 + kRound4);
   }
   // a negative scale turns the queries' signs; a scale of 0 gives equal weights, as the least number does
   const float c = fmaxf(fabsf(a.c), 0x1p-126f);
@@ -208,6 +293,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
     if (next < r1) {
       locate(next);
       load_k();
+      if (next + kRound4 < r1) look(next + kRound4);
     }
     float top[NT];
     bool over = false;
@@ -283,7 +369,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
     if (next < r1) load_v();
   };
 
-  for (int rb = rb0; rb < r1; rb += kRound) step(rb, rb + kRound);  // the waves' steps in turn
+  for (int rb = rb0; rb < r1; rb += kRound4) step(rb, rb + kRound4);  // the waves' steps in turn
 
   // merge of the waves, 16 columns at a time: element NI (4 kg + j) + i of column n
 #pragma unroll
@@ -317,10 +403,10 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
       }
       const int col = col0 + 16 * ct + cc;
       const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
-      if (a.n_split == 1) {
+      if (whole) {
         store_out<DT>(a.out, row * D + e, A, S);
       } else {
-        float* pt = a.part + (row * a.n_split + split) * (D + 2);
+        float* pt = a.part + part4_at(cg * a.pc.h_kv + g, share, from > 0 ? 0 : 1, 16 * ct + cc, min(a.max_q * G, COLS), a.shares) * (D + 2);
         if (e == 0) {
           pt[0] = M;
           pt[1] = S;
@@ -328,26 +414,123 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
         pt[2 + e] = A;
       }
     }
-    if (ct + 1 < NT) __syncthreads();
+    if (ct + 1 < NT || SHARES) __syncthreads();
   }
+  }
+}
+
+// One workgroup per (column, kv head, problem): the parts of the shares that the problem's rounds fall to, the waves' in
+// turn, kJoin at a time in flight.
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void paged_join4_kernel(PagedAttnArgs a, int COLS) {
+  constexpr int E = D / 64, kJoin = 4;
+  __shared__ float sh_a[kWaves][D], sh_m[kWaves], sh_s[kWaves];
+  const int col = blockIdx.x, g = blockIdx.y, p = blockIdx.z, G = a.pc.h_q / a.pc.h_kv, cg = col / COLS;
+  const int32_t* prefix = a.prefix + (int64_t)cg * (a.pc.n_prob + 1);
+  const int lo = prefix[p], hi = prefix[p + 1], T = prefix[a.pc.n_prob];
+  const Span sp = span_of(a, p);
+  if (col >= sp.n_tok * G) return;
+  const int S = share_of(T, a.shares), s0 = lo / S, n = (hi - 1) / S - s0 + 1;
+  if (n == 1) return;  // one share had them all
+  const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, cols = min(a.max_q * G, COLS);
+  float m = -INFINITY, sum = 0.f, A[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) A[e] = 0.f;
+  for (int i = wave; i < n; i += kJoin * kWaves) {
+    float xm[kJoin], xs[kJoin], xa[kJoin][E];
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j) {
+      const bool in = i + j * kWaves < n;
+      const int s = s0 + (in ? i + j * kWaves : i);
+      const float* x = a.part + part4_at(cg * a.pc.h_kv + g, s, (int64_t)s * S > lo ? 0 : 1, col % COLS, cols, a.shares) * (D + 2);
+      xm[j] = in ? x[0] : -INFINITY;
+      xs[j] = in ? x[1] : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) xa[j][e] = in ? x[2 + E * lane + e] : 0.f;
+    }
+    float mn = m;
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j) mn = fmaxf(mn, xm[j]);
+    const float f = part_weight(m, mn);
+    sum *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) A[e] *= f;
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j) {
+      const float w = part_weight(xm[j], mn);
+      sum = fmaf(xs[j], w, sum);
+#pragma unroll
+      for (int e = 0; e < E; ++e) A[e] = fmaf(xa[j][e], w, A[e]);
+    }
+    m = mn;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) sh_a[wave][E * lane + e] = A[e];
+  if (lane == 0) {
+    sh_m[wave] = m;
+    sh_s[wave] = sum;
+  }
+  __syncthreads();
+  if (tid >= D) return;
+  float M = -INFINITY, total = 0.f, out = 0.f;
+#pragma unroll
+  for (int q = 0; q < kWaves; ++q) M = fmaxf(M, sh_m[q]);
+#pragma unroll
+  for (int q = 0; q < kWaves; ++q) {
+    const float f = part_weight(sh_m[q], M);
+    total = fmaf(sh_s[q], f, total);
+    out = fmaf(sh_a[q][tid], f, out);
+  }
+  store_out<DT>(a.out, row * D + tid, out, total);
 }
 
 namespace {
 
-template <int DT, int D> hipError_t attend(const PagedAttnArgs& a, int nt, hipStream_t stream) {
-  const int64_t cols = (int64_t)a.max_q * a.pc.group();
-  const dim3 grid((unsigned)(a.pc.h_kv * ((cols + 16 * nt - 1) / (16 * nt))), (unsigned)a.n_split, (unsigned)a.pc.n_prob);
+int tiles_of(int64_t cols) { return cols <= 16 ? 1 : 2; }
+
+template <int DT, int D, int NT> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
+  const int64_t cols = (int64_t)a.max_q * a.pc.group(), units = a.pc.h_kv * ((cols + 16 * NT - 1) / (16 * NT));
   const size_t lds = (size_t)kWaves * std::min<int64_t>(cols, 16) * D * sizeof(float);
-  if (nt == 1) paged_attn4_kernel<DT, D, 1><<<grid, kThreads, lds, stream>>>(a);
-  else paged_attn4_kernel<DT, D, 2><<<grid, kThreads, lds, stream>>>(a);
+  if (a.shares == 0) {
+    paged_attn4_kernel<DT, D, NT, false><<<dim3((unsigned)units, 1, (unsigned)a.pc.n_prob), kThreads, lds, stream>>>(a);
+    return hipGetLastError();
+  }
+  paged_attn4_kernel<DT, D, NT, true><<<(unsigned)(units * a.shares), kThreads, lds, stream>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  paged_join4_kernel<DT, D><<<dim3((unsigned)cols, (unsigned)a.pc.h_kv, (unsigned)a.pc.n_prob), kThreads, 0, stream>>>(a, 16 * NT);
   return hipGetLastError();
+}
+template <int DT, int D> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
+  return tiles_of((int64_t)a.max_q * a.pc.group()) == 1 ? attend<DT, D, 1>(a, stream) : attend<DT, D, 2>(a, stream);
 }
 
 }  // namespace
 
-hipError_t launch_paged_attention4(const PagedAttnArgs& a, int nt, hipStream_t stream) {
-  if (a.pc.dtype == kDtBf16) return a.pc.d == 64 ? attend<kDtBf16, 64>(a, nt, stream) : attend<kDtBf16, 128>(a, nt, stream);
-  return a.pc.d == 64 ? attend<kDtF32, 64>(a, nt, stream) : attend<kDtF32, 128>(a, nt, stream);
+// Workgroups that the chip holds at once, over the units of (kv head, group of columns).
+int paged4_shares(const Paged& pc, int max_q) {
+  const int64_t cols = (int64_t)max_q * pc.group();
+  const int nt = tiles_of(cols);
+  const int64_t units = pc.h_kv * ((cols + 16 * nt - 1) / (16 * nt));
+  const int64_t held = 256 * ((nt == 1 ? 3 : 2) - (pc.dtype == kDtF32 && pc.d == 128 ? 1 : 0));
+  return (int)((held + units - 1) / units);
+}
+
+size_t paged4_prefix_bytes(const Paged& pc, int max_q) {
+  const int64_t cols = (int64_t)max_q * pc.group(), nt = tiles_of(cols);
+  return (size_t)(((cols + 16 * nt - 1) / (16 * nt) * (pc.n_prob + 1) * (int64_t)sizeof(int32_t) + 255) / 256 * 256);
+}
+
+size_t paged4_ws_bytes(const Paged& pc, int max_q, int shares) {
+  const int64_t cols = (int64_t)max_q * pc.group(), nt = tiles_of(cols), groups = (cols + 16 * nt - 1) / (16 * nt);
+  const int64_t parts = groups * pc.h_kv * shares * 2 * std::min<int64_t>(cols, 16 * nt);
+  return paged4_prefix_bytes(pc, max_q) + (size_t)(parts * (pc.d + 2)) * sizeof(float);
+}
+
+hipError_t launch_paged_attention4(const PagedAttnArgs& a, hipStream_t stream) {
+  if (a.pc.dtype == kDtBf16) return a.pc.d == 64 ? attend<kDtBf16, 64>(a, stream) : attend<kDtBf16, 128>(a, stream);
+  return a.pc.d == 64 ? attend<kDtF32, 64>(a, stream) : attend<kDtF32, 128>(a, stream);
 }
 
 }  // namespace kv
