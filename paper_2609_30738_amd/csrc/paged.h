@@ -93,6 +93,8 @@ struct PagedAttnArgs {
   // up to 32 columns over 4-bit blocks: workgroups that share a unit's rounds (0: one for each problem), and their prefix sums
   int shares;
   int32_t* prefix;
+  int group;           // h_q / h_kv, and its reciprocal in units of 2^-32, rounded up (0: a group of one)
+  uint32_t group_inv;
 };
 // prompt_waves: 0 for paged_attention.hip's kernel, else the waves of paged_prompt.hip's (32 columns each).
 struct PagedPlan {
@@ -110,7 +112,7 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan,
 int paged4_shares(const Paged& pc, int max_q);
 size_t paged4_prefix_bytes(const Paged& pc, int max_q);
 size_t paged4_ws_bytes(const Paged& pc, int max_q, int shares);
-hipError_t launch_paged_attention4(const PagedAttnArgs& a, hipStream_t stream);
+hipError_t launch_paged_attention4(PagedAttnArgs a, hipStream_t stream);
 // Blocks of a split that the prompt kernel of so many waves holds in LDS beside its tiles
 // (two workgroups of four waves share a CU's 160 KB, one of eight has it alone).
 constexpr int prompt_split_blocks(int waves) { return waves == 4 ? 256 : 4096; }

@@ -34,41 +34,67 @@ constexpr int kRound4 = kWaves * 16 * kTiles4;  // rows of a workgroup's round
 
 typedef const __attribute__((address_space(4))) int32_t* uniform_ints;  // read by scalar loads
 
-// Rounds of problem p's rows for the columns from col0 on (at least one if it has such columns).
-__device__ __forceinline__ int rounds_of(const PagedAttnArgs& a, int p, int col0, int cols, int G) {
-  const Span sp = span_of(a, p);
+// The token of a column, column / group: by the group's reciprocal, exact below 2^28.
+__device__ __forceinline__ int token_of(const PagedAttnArgs& a, int col) {
+  return a.group_inv ? (int)__umulhi((uint32_t)col, a.group_inv) : col;
+}
+
+// Rounds of a problem's rows for the columns from col0 on (at least one if it has such columns).
+__device__ __forceinline__ int rounds_of(const PagedAttnArgs& a, const Span& sp, int col0, int cols, int G) {
   const int n = min(sp.n_tok * G - col0, cols);
-  return n <= 0 ? 0 : max(1, (sp.visible((col0 + n - 1) / G) + kRound4 - 1) / kRound4);
+  return n <= 0 ? 0 : max(1, (int)((uint32_t)(sp.visible(token_of(a, col0 + n - 1)) + kRound4 - 1) / kRound4));
 }
 
 // Rounds to a share, of T in n shares.
-__device__ __forceinline__ int share_of(int T, int n) { return max((int)(((int64_t)T + n - 1) / n), kLeastRounds4); }
+__device__ __forceinline__ int share_of(int T, int n) {
+  return max((int)(((uint32_t)T + (uint32_t)n - 1u) / (uint32_t)n), kLeastRounds4);
+}
 
 // Place of a share's part of a unit's column: slot 0 of a problem that begins before the share, 1 of one that ends behind it.
 __device__ __forceinline__ int64_t part4_at(int unit, int share, int slot, int col, int cols, int shares) {
   return (((int64_t)unit * shares + share) * 2 + slot) * cols + col;
 }
 
-// Inclusive sum over a workgroup; total: of all.  Starts and ends synchronised.
-__device__ __forceinline__ int scan_sum(int v, int& total) {
-  __shared__ int sums[kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// store_out of four elements.
+template <int DT> __device__ __forceinline__ void store_out4(void* out, int64_t at, const f32x4v& A, float S) {
+  float o[4];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  if (lane == 63) sums[wave] = v;
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) v += sums[w];
-    total += sums[w];
-  }
-  __syncthreads();
-  return v;
+  for (int k = 0; k < 4; ++k) o[k] = S == 0.f ? 0.f : A[k] / S;
+  if constexpr (DT == kDtBf16)
+    *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(out) + at) = u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+  else
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(o[0], o[1], o[2], o[3]);
 }
+
+// A wave's view of 256 problems, four consecutive ones to a lane: what they see, their rounds, and the rounds before them.
+struct Shares {
+  Span sp[4];
+  int rounds[4], before[4], total;
+  __device__ __forceinline__ void of(const PagedAttnArgs& a, int q0, int col0, int cols, int G) {
+    const int lane = threadIdx.x & 63;
+    int sum = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int q = q0 + 4 * lane + k;
+      sp[k] = span_of(a, min(q, a.pc.n_prob - 1));
+      rounds[k] = q < a.pc.n_prob ? rounds_of(a, sp[k], col0, cols, G) : 0;
+      sum += rounds[k];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += u;
+    }
+    total = __builtin_amdgcn_readlane(incl, 63);
+    int at = incl - sum;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      before[k] = at;
+      at += rounds[k];
+    }
+  }
+};
 
 }  // namespace
 
@@ -82,65 +108,70 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   constexpr int QN = DT == kDtBf16 ? 1 : 3;        // bf16 terms of a query
   constexpr int PN = DT == kDtF32 ? 3 : (NT == 1 ? 2 : 1);  // bf16 terms of a weight
   constexpr int COLS = 16 * NT;
+  constexpr int kStride = D + 4;                   // of a column in LDS: its lanes' writes fall on all banks
   __shared__ float sh_m[kWaves][16], sh_s[kWaves][16];
-  extern __shared__ __align__(16) float sh_acc[];  // [kWaves][up to 16 columns][D]
+  extern __shared__ __align__(16) float sh_acc[];  // [kWaves][up to 16 columns][kStride]
 
-  const int g = blockIdx.x % a.pc.h_kv, G = a.pc.h_q / a.pc.h_kv;
-  const int groups = (a.max_q * G + COLS - 1) / COLS, cg = blockIdx.x / a.pc.h_kv % groups, col0 = cg * COLS;
+  const int g = blockIdx.x, cg = blockIdx.y, G = a.group, col0 = cg * COLS;
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int shift = a.pc.shift, R = 1 << shift;
 
   // the share: rounds `at` to `end` of all problems' one after the other, from problem p on, whose first one is `base`
-  const int share = SHARES ? (int)(blockIdx.x / a.pc.h_kv / groups) : 0;
+  const int share = SHARES ? (int)blockIdx.z : 0;
   int p = SHARES ? 0 : (int)blockIdx.z, base = 0, at = 0, end = 1;
+  Span sp;
   if constexpr (SHARES) {
-    __shared__ int first[2];
-    int rounds = tid < a.pc.n_prob ? rounds_of(a, tid, col0, COLS, G) : 0, total;
-    int sum = scan_sum(rounds, total), T = total;
-    for (int q = kThreads; q < a.pc.n_prob; q += kThreads) {
-      scan_sum(q + tid < a.pc.n_prob ? rounds_of(a, q + tid, col0, COLS, G) : 0, total);
-      T += total;
+    // every wave by itself
+    Shares s;
+    s.of(a, 0, col0, COLS, G);
+    int T = s.total;
+    for (int q = 256; q < a.pc.n_prob; q += 256) {
+      s.of(a, q, col0, COLS, G);
+      T += s.total;
     }
     const int S = share_of(T, a.shares);
-    at = (int)min((int64_t)share * S, (int64_t)T);
+    at = (int)min((uint32_t)share * (uint32_t)S, (uint32_t)T);
     end = min(at + S, T);
-    const bool writes = share == 0 && g == 0;
+    const bool writes = share == 0 && g == 0 && wave == 0;  // the sums, for the join
     if (at >= end && !writes) return;
-    int32_t* prefix = a.prefix + (int64_t)cg * (a.pc.n_prob + 1);  // for the join
-    for (int q = 0, before = 0; q < a.pc.n_prob; q += kThreads) {
-      if (q > 0) {
-        rounds = q + tid < a.pc.n_prob ? rounds_of(a, q + tid, col0, COLS, G) : 0;
-        sum = scan_sum(rounds, total);
-      } else if (a.pc.n_prob > kThreads) {
-        sum = scan_sum(rounds, total);
+    int32_t* prefix = a.prefix + (int64_t)cg * (a.pc.n_prob + 1);
+    if (a.pc.n_prob > 256) s.of(a, 0, col0, COLS, G);
+    bool found = false;
+    for (int q = 0, before = 0; q < a.pc.n_prob; q += 256) {
+      if (q > 0) s.of(a, q, col0, COLS, G);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int mine = before + s.before[k];
+        const uint64_t has = __ballot(at >= mine && at < mine + s.rounds[k]);
+        if (has) {
+          const int l = __ffsll((unsigned long long)has) - 1;
+          p = q + 4 * l + k;
+          base = __builtin_amdgcn_readlane(mine, l);
+          sp.tok0 = __builtin_amdgcn_readlane(s.sp[k].tok0, l);
+          sp.n_tok = __builtin_amdgcn_readlane(s.sp[k].n_tok, l);
+          sp.len = __builtin_amdgcn_readlane(s.sp[k].len, l);
+          sp.cap = s.sp[k].cap;
+          found = true;
+        }
+        if (writes && q + 4 * lane + k < a.pc.n_prob) prefix[q + 4 * lane + k] = mine;
       }
-      const int mine = before + sum - rounds;
-      if (at >= mine && at < mine + rounds) {
-        first[0] = q + tid;
-        first[1] = mine;
-      }
-      if (writes && q + tid < a.pc.n_prob) prefix[q + tid] = mine;
-      before += total;
-      if (!writes && before > at) break;
+      before += s.total;
+      if (!writes && found) break;
     }
-    if (writes && tid == 0) prefix[a.pc.n_prob] = T;
+    if (writes && lane == 0) prefix[a.pc.n_prob] = T;
     if (at >= end) return;
-    __syncthreads();
-    p = __builtin_amdgcn_readfirstlane(first[0]);
-    base = __builtin_amdgcn_readfirstlane(first[1]);
+  } else {
+    sp = span_of(a, p);
   }
 
-  for (; at < end; ++p) {
-    const Span sp = span_of(a, p);
-    const int n_cols = __builtin_amdgcn_readfirstlane(min(sp.n_tok * G - col0, COLS));
-    if (n_cols <= 0) {
-      if constexpr (SHARES) continue;
-      return;
-    }
-    const int vis_max = __builtin_amdgcn_readfirstlane(sp.visible((col0 + n_cols - 1) / G));
-    const int vis_min = __builtin_amdgcn_readfirstlane(sp.visible(col0 / G));
-    const int all = max(1, (vis_max + kRound4 - 1) / kRound4);  // the problem's rounds, and those of the share
+  while (true) {
+    const int n_cols = min(sp.n_tok * G - col0, COLS);
+    if (!SHARES && n_cols <= 0) return;
+    if (n_cols > 0) {
+    const int vis_max = __builtin_amdgcn_readfirstlane(sp.visible(token_of(a, col0 + n_cols - 1)));
+    const int vis_min = __builtin_amdgcn_readfirstlane(sp.visible(token_of(a, col0)));
+    const int all = max(1, (int)((uint32_t)(vis_max + kRound4 - 1) / kRound4));  // the problem's rounds, and those of the share
     const int from = at - base, to = SHARES ? min(end - base, all) : all;
     const int r0 = from * kRound4, r1 = min(vis_max, to * kRound4);
     const bool whole = !SHARES || (from == 0 && to == all);
@@ -203,13 +234,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   };
 
   const int rb0 = r0 + wave * STEP;
-  if (rb0 < r1) {
-    look(rb0);
-    locate(rb0);
-    load_k();
-    load_v();
-    if (rb0 + kRound4 < r1) look(rb0 + kRound4);
-  }
+  if (rb0 < r1) look(rb0);
   // a negative scale turns the queries' signs; a scale of 0 gives equal weights, as the least number does
   const float c = fmaxf(fabsf(a.c), 0x1p-126f);
   // the queries' operand: column n, elements D / 4 kg + 8 s .. + 7
@@ -219,7 +244,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
   for (int ct = 0; ct < NT; ++ct) {
     const int col = col0 + 16 * ct + n;
     const bool live = 16 * ct + n < n_cols;
-    const int j = live ? col / G : 0, h = live ? col % G : 0;
+    const int j = live ? token_of(a, col) : 0, h = live ? col - j * G : 0;
     vis[ct] = live ? sp.visible(j) : 0;
     const int64_t at = (int64_t)(sp.tok0 + j) * a.q_stride + (int64_t)(g * G + h) * D;
 #pragma unroll
@@ -239,6 +264,13 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
         split_terms<QN>(f, qf[ct][s]);
       }
     }
+  }
+
+  if (rb0 < r1) {
+    locate(rb0);
+    load_k();
+    load_v();
+    if (rb0 + kRound4 < r1) look(rb0 + kRound4);
   }
 
   float m[NT], mu[NT];  // mu: m (0 before the first finite logit) and kSlack octaves
@@ -385,37 +417,41 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < NI; i += 4)
-          *reinterpret_cast<float4*>(&sh_acc[(wave * cols + n) * D + (4 * kg + j) * NI + i]) =
+          *reinterpret_cast<float4*>(&sh_acc[(wave * cols + n) * kStride + (4 * kg + j) * NI + i]) =
               make_float4(acc[ct][i][j], acc[ct][i + 1][j], acc[ct][i + 2][j], acc[ct][i + 3][j]);
     }
     __syncthreads();
-    for (int idx = tid; idx < cols * D; idx += kThreads) {
-      const int cc = idx / D, e = idx % D;
+    for (int idx = tid; idx < cols * (D / 4); idx += kThreads) {
+      const int cc = idx / (D / 4), e = idx % (D / 4) * 4;
       float M = -INFINITY;
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) M = fmaxf(M, sh_m[i][cc]);
-      float S = 0.f, A = 0.f;
+      float S = 0.f;
+      f32x4v A = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) {
         const float f = part_weight(sh_m[i][cc], M);
         S = fmaf(sh_s[i][cc], f, S);
-        A = fmaf(sh_acc[(i * cols + cc) * D + e], f, A);
+        const f32x4v x = *reinterpret_cast<const f32x4v*>(&sh_acc[(i * cols + cc) * kStride + e]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) A[k] = fmaf(x[k], f, A[k]);
       }
       const int col = col0 + 16 * ct + cc;
-      const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
       if (whole) {
-        store_out<DT>(a.out, row * D + e, A, S);
+        const int j = token_of(a, col);
+        store_out4<DT>(a.out, ((int64_t)(sp.tok0 + j) * a.pc.h_q + g * G + (col - j * G)) * D + e, A, S);
       } else {
         float* pt = a.part + part4_at(cg * a.pc.h_kv + g, share, from > 0 ? 0 : 1, 16 * ct + cc, min(a.max_q * G, COLS), a.shares) * (D + 2);
-        if (e == 0) {
-          pt[0] = M;
-          pt[1] = S;
-        }
-        pt[2 + e] = A;
+        if (e == 0) *reinterpret_cast<float2*>(pt) = make_float2(M, S);
+        *reinterpret_cast<float2*>(pt + 2 + e) = make_float2(A[0], A[1]);
+        *reinterpret_cast<float2*>(pt + 4 + e) = make_float2(A[2], A[3]);
       }
     }
     if (ct + 1 < NT || SHARES) __syncthreads();
   }
+    }
+    if (!SHARES || at >= end) return;
+    sp = span_of(a, ++p);
   }
 }
 
@@ -425,14 +461,16 @@ template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void paged_join4_kernel(PagedAttnArgs a, int COLS) {
   constexpr int E = D / 64, kJoin = 4;
   __shared__ float sh_a[kWaves][D], sh_m[kWaves], sh_s[kWaves];
-  const int col = blockIdx.x, g = blockIdx.y, p = blockIdx.z, G = a.pc.h_q / a.pc.h_kv, cg = col / COLS;
+  const int col = blockIdx.x, g = blockIdx.y, p = blockIdx.z, G = a.group, cg = (int)((uint32_t)col / (uint32_t)COLS);
   const int32_t* prefix = a.prefix + (int64_t)cg * (a.pc.n_prob + 1);
   const int lo = prefix[p], hi = prefix[p + 1], T = prefix[a.pc.n_prob];
   const Span sp = span_of(a, p);
   if (col >= sp.n_tok * G) return;
-  const int S = share_of(T, a.shares), s0 = lo / S, n = (hi - 1) / S - s0 + 1;
+  const uint32_t S = share_of(T, a.shares);
+  const int s0 = (int)((uint32_t)lo / S), n = (int)((uint32_t)(hi - 1) / S) - s0 + 1;
   if (n == 1) return;  // one share had them all
-  const int64_t row = (int64_t)(sp.tok0 + col / G) * a.pc.h_q + g * G + col % G;
+  const int j = token_of(a, col);
+  const int64_t row = (int64_t)(sp.tok0 + j) * a.pc.h_q + g * G + (col - j * G);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, cols = min(a.max_q * G, COLS);
   float m = -INFINITY, sum = 0.f, A[E];
 #pragma unroll
@@ -443,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void paged_join4_kernel(PagedAttnArgs a, 
     for (int j = 0; j < kJoin; ++j) {
       const bool in = i + j * kWaves < n;
       const int s = s0 + (in ? i + j * kWaves : i);
-      const float* x = a.part + part4_at(cg * a.pc.h_kv + g, s, (int64_t)s * S > lo ? 0 : 1, col % COLS, cols, a.shares) * (D + 2);
+      const float* x = a.part + part4_at(cg * a.pc.h_kv + g, s, (uint32_t)s * S > (uint32_t)lo ? 0 : 1, col - cg * COLS, cols, a.shares) * (D + 2);
       xm[j] = in ? x[0] : -INFINITY;
       xs[j] = in ? x[1] : 0.f;
 #pragma unroll
@@ -490,16 +528,17 @@ namespace {
 int tiles_of(int64_t cols) { return cols <= 16 ? 1 : 2; }
 
 template <int DT, int D, int NT> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
-  const int64_t cols = (int64_t)a.max_q * a.pc.group(), units = a.pc.h_kv * ((cols + 16 * NT - 1) / (16 * NT));
-  const size_t lds = (size_t)kWaves * std::min<int64_t>(cols, 16) * D * sizeof(float);
+  const int64_t cols = (int64_t)a.max_q * a.group;
+  const unsigned h_kv = (unsigned)a.pc.h_kv, groups = (unsigned)((cols + 16 * NT - 1) / (16 * NT));
+  const size_t lds = (size_t)kWaves * std::min<int64_t>(cols, 16) * (D + 4) * sizeof(float);
   if (a.shares == 0) {
-    paged_attn4_kernel<DT, D, NT, false><<<dim3((unsigned)units, 1, (unsigned)a.pc.n_prob), kThreads, lds, stream>>>(a);
+    paged_attn4_kernel<DT, D, NT, false><<<dim3(h_kv, groups, (unsigned)a.pc.n_prob), kThreads, lds, stream>>>(a);
     return hipGetLastError();
   }
-  paged_attn4_kernel<DT, D, NT, true><<<(unsigned)(units * a.shares), kThreads, lds, stream>>>(a);
+  paged_attn4_kernel<DT, D, NT, true><<<dim3(h_kv, groups, (unsigned)a.shares), kThreads, lds, stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  paged_join4_kernel<DT, D><<<dim3((unsigned)cols, (unsigned)a.pc.h_kv, (unsigned)a.pc.n_prob), kThreads, 0, stream>>>(a, 16 * NT);
+  paged_join4_kernel<DT, D><<<dim3((unsigned)cols, h_kv, (unsigned)a.pc.n_prob), kThreads, 0, stream>>>(a, 16 * NT);
   return hipGetLastError();
 }
 template <int DT, int D> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
@@ -528,7 +567,9 @@ size_t paged4_ws_bytes(const Paged& pc, int max_q, int shares) {
   return paged4_prefix_bytes(pc, max_q) + (size_t)(parts * (pc.d + 2)) * sizeof(float);
 }
 
-hipError_t launch_paged_attention4(const PagedAttnArgs& a, hipStream_t stream) {
+hipError_t launch_paged_attention4(PagedAttnArgs a, hipStream_t stream) {
+  a.group = a.pc.group();
+  a.group_inv = a.group > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group) : 0u;
   if (a.pc.dtype == kDtBf16) return a.pc.d == 64 ? attend<kDtBf16, 64>(a, stream) : attend<kDtBf16, 128>(a, stream);
   return a.pc.d == 64 ? attend<kDtF32, 64>(a, stream) : attend<kDtF32, 128>(a, stream);
 }
