@@ -1,10 +1,12 @@
 // New rows into the blocks of a paged cache with the keys rotated on the way, and the rotated queries
 // (kv_paged_append_rotated).
 //
-// paged_rotated_kernel: some workgroups rotate queries as kv_rotate does.  The others take runs of tokens in consecutive slots
-//   of one block (as paged_append_kernel): the turns of the run's tokens go to LDS once, then a wave takes one head of K or
-//   of V after the other.  A key's chunk is turned in registers, with the chunk of the other halves of its pairs from its
-//   lane, and coded from the 32-bit values: it never reaches memory in another form.
+// Some workgroups rotate queries as kv_rotate does.  The others form the turns of their tokens' pairs once, in LDS, and go
+// over the heads with them; a key's chunk is turned in registers, with the chunk of the other halves of its pairs from its
+// lane, and coded from the 32-bit values: it never reaches memory in another form.
+//   paged_rotated_kernel (8 bits): runs of tokens in consecutive slots of one block (as paged_append_kernel), whose rows of a
+//     head share a scale; a tile of rows of a few heads at a time, the scale through LDS.
+//   paged_rotated4_kernel (4 bits): a few tokens, wherever their slots are, four rows at a time to a wave.
 #include <math.h>
 
 #include <algorithm>
@@ -23,100 +25,172 @@ struct AppendRotatedArgs {
   uint32_t tok_bytes;  // between two tokens' rows: at most 2^28
   const int32_t* slots;
   int64_t q_wgs;       // workgroups of the queries
-  int n_share, parts;  // workgroups that share the runs of 64 tokens, and a run's heads
+  int n_share, parts;  // workgroups that share the runs of 64 tokens, and the heads
 };
 
 namespace {
 
-// Rows row0 .. row0 + n - 1 of one block and head, turned; load as in store_rows, turns [n][half].
-template <int DT, int QT, int D, int SHIFT, typename Load>
-__device__ __forceinline__ void store_turned(uint8_t* codes, ScaleOf<QT>* scale, int row0, int n, const float2* turns, int half,
-                                             const TurnChunk<DT, D>& turned, Load load) {
-  constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH, NC = kChunks<DT, D, SHIFT>;
-  const int lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
-  // the row's turns (the last row's past the end)
-  auto of = [&](int i) { return turns + min(i * RPP + rr, n - 1) * half; };
-  if constexpr (QT == kQtE2m1) {
-    constexpr int NB = NC < kBatch4 ? NC : kBatch4;
-    for (int i0 = 0; i0 * RPP < n; i0 += NB) {
-      u32x4_t x[NB];
+// The rows of a block in tiles.  Long runs: a tile's rows fall to the four waves, and a lane's chunks of a few heads are in
+// registers together.  Short ones: a wave takes a head by itself.
+constexpr int kHeld = 8;
+template <int DT, int D, int SHIFT, bool LONG> struct Tiling {
+  static constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH, W = LONG ? kStoreThreads / 64 : 1;
+  static constexpr int ROWS = RPP * W;  // of a tile
+  static constexpr int TILES = (1 << SHIFT) > ROWS ? (1 << SHIFT) / ROWS : 1;
+  static constexpr bool TWICE = !LONG || TILES > kHeld;  // runs of more than TB tiles are read twice
+  static constexpr int TB = !LONG ? 1 : TWICE ? kHeld : TILES, HEADS = LONG ? kHeld / TB : 1;
+};
+
+// A workgroup's run: rows row0 .. row0 + n - 1 of a block, and the heads from g to end - 1 of K (KV 0, turned) or V.
+struct Run {
+  int row0, n;
+  int64_t unit0;        // of the block's first head
+  const uint8_t* rows;  // of the first token
+  uint32_t tok_bytes;
+};
+
+template <int DT, int QT, int D, int SHIFT, bool INTERLEAVED, bool LONG, int KV>
+__device__ __forceinline__ void store_heads(const Paged& pc, const Run& run, int g, int end, const Turns& turns,
+                                            const TurnChunk<DT, D, INTERLEAVED>& turned, int& turn_of_sh) {
+  using T = Tiling<DT, D, SHIFT, LONG>;
+  using C = TurnChunk<DT, D, INTERLEAVED>;
+  constexpr int EPT = T::EPT, CH = T::CH, HB = T::HEADS, TB = T::TB, W = T::W;
+  __shared__ float sh_amax[2][W][kHeld];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % CH;
+  const int r_lane = (LONG ? wave * T::RPP : 0) + lane / CH;
+  uint8_t* const codes = unit_codes<QT, D, SHIFT>(KV ? pc.v : pc.k, run.unit0);
+  float* const scales = unit_scale<QT, D, SHIFT>(KV ? pc.v_scale : pc.k_scale, run.unit0);
+  for (; g < end; g += HB) {
+    // past the last head and row: theirs again
+    auto head = [&](int h) { return min(g + h, end - 1); };
+    auto row = [&](int t) { return min(t * T::ROWS + r_lane, run.n - 1); };
+    float v[HB][TB][EPT];
+    auto take = [&](int t0) __attribute__((always_inline)) {
+      u32x4_t x[HB][TB];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        x[i] = u32x4_t{0u, 0u, 0u, 0u};
-        if ((i0 + i) * RPP < n) x[i] = load(i0 + i);
+      for (int t = 0; t < TB; ++t) {
+        const uint8_t* src = run.rows + (int64_t)row(t0 + t) * run.tok_bytes + c * 16;
+#pragma unroll
+        for (int h = 0; h < HB; ++h) x[h][t] = *reinterpret_cast<const u32x4_t*>(src + head(h) * (CH * 16));
       }
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        if ((i0 + i) * RPP >= n) break;
-        float f[EPT];
-        turned(x[i], of(i0 + i), f);
-        const int r = (i0 + i) * RPP + rr;
-        store_chunk4<D, EPT>(codes, scale, row0 + r, 1 << SHIFT, c, r < n, f);
-      }
-    }
-  } else {
-    // chunks that do not fit the registers are loaded again
-    constexpr int NH = NC > kHeldChunks ? 1 : NC;
-    const float old = row0 > 0 ? *scale : 0.f;
-    u32x4_t x[NH];
-    if constexpr (NH == NC) {
+      for (int t = 0; t < TB; ++t) {
+        float2 cs[C::PAIRS];
+        if constexpr (KV == 0) turns.get(row(t0 + t), turned.mine, cs);
 #pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        x[i] = u32x4_t{0u, 0u, 0u, 0u};
-        if (i * RPP < n) x[i] = load(i);
-      }
-    }
-    uint32_t amax = 0;
-    bool odd = false;  // an infinity or a NaN among the lane's values
-    auto largest = [&](int i, const u32x4_t& y) __attribute__((always_inline)) {
-      float f[EPT];
-      turned(y, of(i), f);
-#pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        const uint32_t u = __float_as_uint(f[e]) & 0x7FFFFFFFu;
-        amax = max(amax, u < 0x7F800000u ? u : 0u);
-        odd = odd || u >= 0x7F800000u;
-      }
-    };
-    auto store = [&](int i, const u32x4_t& y, float inv, auto finite) __attribute__((always_inline)) {
-      float f[EPT];
-      turned(y, of(i), f);
-      if (i * RPP + rr < n)
-        store_chunk<QT, decltype(finite)::value>(codes + (row0 + i * RPP + rr) * D + c * EPT, f, inv);
-    };
-    auto each = [&](auto f) __attribute__((always_inline)) {
-      if constexpr (NH == NC) {
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          // (a value is formed anew in each pass over the chunks: registers)
-          asm volatile("" : "+v"(x[i][0]), "+v"(x[i][1]), "+v"(x[i][2]), "+v"(x[i][3]));
-          if (i * RPP < n) f(i, x[i]);
+        for (int h = 0; h < HB; ++h) {
+          if constexpr (KV == 0) turned(x[h][t], cs, v[h][t]);
+          else chunk_values<DT>(x[h][t], v[h][t]);
         }
-      } else {
-        for (int i = 0; i * RPP < n; ++i) f(i, load(i));
       }
     };
-    each(largest);
-    const float s = grown_scale<QT, D>(codes, row0, old, block_scale<QT>(wave_max_u32(amax))), inv = inv_scale(s);
-    if (__ballot(odd)) each([&](int i, const u32x4_t& y) { store(i, y, inv, std::false_type{}); });
-    else each([&](int i, const u32x4_t& y) { store(i, y, inv, std::true_type{}); });
-    if (lane == 0) *scale = s;
+    float amax[HB], odd = 0.f;  // odd: NaN where an infinity or a NaN is among the lane's values
+#pragma unroll
+    for (int h = 0; h < HB; ++h) amax[h] = 0.f;
+    auto largest = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < HB; ++h)
+#pragma unroll
+        for (int t = 0; t < TB; ++t)
+#pragma unroll
+          for (int e = 0; e < EPT; ++e) {
+            amax[h] = fmaxf(amax[h], fabsf(v[h][t][e]));
+            odd = fmaf(v[h][t][e], 0.f, odd);
+          }
+    };
+    // the finite values' largest, of values that are not all finite
+    auto largest_finite = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < HB; ++h)
+#pragma unroll
+        for (int t = 0; t < TB; ++t)
+#pragma unroll
+          for (int e = 0; e < EPT; ++e) amax[h] = fmaxf(amax[h], fabsf(v[h][t][e]) < INFINITY ? fabsf(v[h][t][e]) : 0.f);
+    };
+    bool any = T::TWICE;
+    const bool once = run.n <= TB * T::ROWS;
+    if constexpr (T::TWICE) {
+      for (int t0 = 0; t0 * T::ROWS < run.n; t0 += TB) {
+        take(t0);
+        largest_finite();
+      }
+    } else {
+      take(0);
+      largest();
+      any = __ballot(!(odd == 0.f)) != 0;
+      if (any) {
+#pragma unroll
+        for (int h = 0; h < HB; ++h) amax[h] = 0.f;
+        largest_finite();
+      }
+    }
+    float old[HB];
+#pragma unroll
+    for (int h = 0; h < HB; ++h) old[h] = run.row0 > 0 ? scales[head(h)] : 0.f;
+    const int turn = turn_of_sh;
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      amax[h] = wave_max_uniform(amax[h]);
+      if (LONG && lane == h) sh_amax[turn][wave][h] = amax[h];
+    }
+    if constexpr (LONG) {
+      __syncthreads();
+      turn_of_sh ^= 1;
+    }
+    float inv[HB];
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      float m = amax[h];
+      if constexpr (LONG) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) m = fmaxf(m, sh_amax[turn][w][h]);
+      }
+      float s = block_scale<QT>(__float_as_uint(m));
+      if (run.row0 > 0) {
+        // the block's rows in use move to a larger scale by one wave
+        if (g + h < end && (!LONG || h % W == wave)) grown_scale<QT, D>(codes + ((int64_t)(g + h) << SHIFT) * D, run.row0, old[h], s);
+        if (old[h] >= s && old[h] < INFINITY) s = old[h];
+      }
+      if ((LONG ? threadIdx.x : lane) == 0 && g + h < end) scales[g + h] = s;
+      inv[h] = s > 0.f ? __uint_as_float((254u << 23) - __float_as_uint(s)) : 1.f;  // of a power of two
+    }
+    auto put = [&](int t0, auto finite) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < TB; ++t) {
+        const int r = (t0 + t) * T::ROWS + r_lane;
+#pragma unroll
+        for (int h = 0; h < HB; ++h)
+          if (r < run.n && g + h < end)
+            store_chunk<QT, decltype(finite)::value>(codes + (((int64_t)(g + h) << SHIFT) + run.row0 + r) * D + c * EPT, v[h][t], inv[h]);
+      }
+    };
+    if constexpr (T::TWICE) {
+      for (int t0 = 0; t0 * T::ROWS < run.n; t0 += TB) {
+        if (!once) take(t0);
+        put(t0, std::false_type{});
+      }
+    } else if (any) {
+      put(0, std::false_type{});
+    } else {
+      put(0, std::true_type{});
+    }
   }
 }
 
 }  // namespace
 
-template <int DT, int QT, int D, int SHIFT>
+template <int DT, int QT, int D, int SHIFT, bool INTERLEAVED, bool LONG>
 __global__ __launch_bounds__(kStoreThreads) void paged_rotated_kernel(AppendRotatedArgs a) {
-  constexpr int CH = D * (int)sizeof(typename Elem<DT>::T) / 16, RPP = 64 / CH, R = 1 << SHIFT, kWaves = kStoreThreads / 64;
-  extern __shared__ __align__(16) float2 tab[];
+  using C = TurnChunk<DT, D, INTERLEAVED>;
+  constexpr int R = 1 << SHIFT;
+  extern __shared__ __align__(16) float4 lds[];
   int64_t id = blockIdx.x;
   if (id < a.q_wgs) {
-    rotate_group<DT, D>(a.rq, id / a.rq.parts, (int)(id % a.rq.parts), tab);
+    rotate_group<DT, D>(a.rq, id / a.rq.parts, (int)(id % a.rq.parts), lds);
     return;
   }
   id -= a.q_wgs;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_tok = a.rq.n_tok;
+  const int lane = threadIdx.x & 63, n_tok = a.rq.n_tok;
   const int part = (int)(id % a.parts);
   id /= a.parts;
   const int share = (int)(id % a.n_share);
@@ -127,7 +201,10 @@ __global__ __launch_bounds__(kStoreThreads) void paged_rotated_kernel(AppendRota
   const int slot = t < n_tok ? a.slots[t] : -1;
   const int before = t > 0 && t < n_tok ? a.slots[t - 1] : -1;
   const bool begins = slot >= 0 && slot < n_slots && (before < 0 || slot != before + 1 || (slot & (R - 1)) == 0);
-  const TurnChunk<DT, D> turned(a.rq.rot);
+  const C turned(a.rq.rot);
+  const Turns turns(lds, a.rq.rot, C::PAIRS);
+  const int per = (a.pc.h_kv + a.parts - 1) / a.parts, g0 = part * per, g1 = min(g0 + per, a.pc.h_kv);
+  int turn = 0;
   uint64_t runs = __ballot(begins);  // the same in every wave
   for (int rank = 0; runs; ++rank, runs &= runs - 1) {
     if (rank % a.n_share != share) continue;
@@ -145,38 +222,140 @@ __global__ __launch_bounds__(kStoreThreads) void paged_rotated_kernel(AppendRota
       }
       n += 64;
     }
-    fill_turns(tab, a.rq.rot, a.rq.pos + t0, n);
+    turns.fill(a.rq.rot, a.rq.pos + t0, n);
     __syncthreads();
-    const uint32_t mine = lane / CH * a.tok_bytes + lane % CH * 16;
-    for (int u = part * kWaves + wave; u < 2 * a.pc.h_kv; u += a.parts * kWaves) {
-      const int kv = u & 1, g = u >> 1;
-      const int64_t unit = (int64_t)(s0 >> SHIFT) * a.pc.h_kv + g;
-      // a wave-uniform address and a lane's 32-bit offset
-      const uint8_t* src = static_cast<const uint8_t*>(kv ? a.v_new : a.k_new) + (int64_t)t0 * a.tok_bytes + g * (CH * 16);
-      auto load = [&](int i) {
-        u32x4_t x = {0u, 0u, 0u, 0u};
-        if (i * RPP + lane / CH < n) x = *reinterpret_cast<const u32x4_t*>(src + (int64_t)i * RPP * a.tok_bytes + mine);
-        return x;
-      };
-      uint8_t* codes = unit_codes<QT, D, SHIFT>(kv ? a.pc.v : a.pc.k, unit);
-      auto* scale = unit_scale<QT, D, SHIFT>(kv ? a.pc.v_scale : a.pc.k_scale, unit);
-      if (kv) store_rows<DT, QT, D, SHIFT>(codes, scale, row0, n, load);
-      else store_turned<DT, QT, D, SHIFT>(codes, scale, row0, n, tab, a.rq.rot.rot >> 1, turned, load);
+    Run run{row0, n, (int64_t)(s0 >> SHIFT) * a.pc.h_kv, static_cast<const uint8_t*>(a.k_new) + (int64_t)t0 * a.tok_bytes, a.tok_bytes};
+    const uint8_t* v_rows = static_cast<const uint8_t*>(a.v_new) + (int64_t)t0 * a.tok_bytes;
+    if constexpr (LONG) {
+      store_heads<DT, QT, D, SHIFT, INTERLEAVED, true, 0>(a.pc, run, g0, g1, turns, turned, turn);
+      run.rows = v_rows;
+      store_heads<DT, QT, D, SHIFT, INTERLEAVED, true, 1>(a.pc, run, g0, g1, turns, turned, turn);
+    } else {
+      for (int u = 2 * g0 + (threadIdx.x >> 6); u < 2 * g1; u += kStoreThreads / 64) {
+        const int g = __builtin_amdgcn_readfirstlane(u >> 1);
+        if (u & 1) {
+          Run v = run;
+          v.rows = v_rows;
+          store_heads<DT, QT, D, SHIFT, INTERLEAVED, false, 1>(a.pc, v, g, g + 1, turns, turned, turn);
+        } else {
+          store_heads<DT, QT, D, SHIFT, INTERLEAVED, false, 0>(a.pc, run, g, g + 1, turns, turned, turn);
+        }
+      }
     }
     __syncthreads();
   }
 }
 
+// Tokens of a workgroup of paged_rotated4_kernel: a wave's 64 chunks of 16 bytes are whole rows of a head.
+template <int DT, int D> constexpr int kRotatedRows4 = kStoreThreads * 16 / (D * (int)sizeof(typename Elem<DT>::T));
+
+template <int DT, int D, bool INTERLEAVED>
+__global__ __launch_bounds__(kStoreThreads) void paged_rotated4_kernel(AppendRotatedArgs a) {
+  using C = TurnChunk<DT, D, INTERLEAVED>;
+  constexpr int EPT = C::EPT, CH = C::CH, RPP = 64 / CH, ROWS = kRotatedRows4<DT, D>, kBatch = 8;
+  extern __shared__ __align__(16) float4 lds[];
+  int64_t id = blockIdx.x;
+  if (id < a.q_wgs) {
+    rotate_group<DT, D>(a.rq, id / a.rq.parts, (int)(id % a.rq.parts), lds);
+    return;
+  }
+  id -= a.q_wgs;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane % CH, part = (int)(id % a.parts);
+  const int64_t t0 = id / a.parts * ROWS;
+  const int n = (int)min((int64_t)ROWS, a.rq.n_tok - t0), r = wave * RPP + lane / CH;
+  const int slot = r < n ? a.slots[t0 + r] : -1, R = 1 << a.pc.shift;
+  const bool live = slot >= 0 && (slot >> a.pc.shift) < a.pc.n_blocks;
+  const int64_t unit0 = (int64_t)(live ? slot >> a.pc.shift : 0) * a.pc.h_kv;  // of the block's first head
+  const int row = live ? slot & (R - 1) : 0;
+  // consecutive heads fall to a part: rows of a token lie beside each other
+  const int per = (a.pc.h_kv + a.parts - 1) / a.parts, g0 = part * per, g1 = min(g0 + per, a.pc.h_kv);
+  const int64_t mine = (t0 + (r < n ? r : 0)) * (int64_t)a.tok_bytes + c * 16;
+  u32x4_t x[kBatch];
+  auto load = [&](const void* rows, int g) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (g + i < g1) x[i] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(rows) + mine + (g + i) * (CH * 16));
+  };
+  load(a.k_new, g0);
+  const Turns turns(lds, a.rq.rot, C::PAIRS);
+  turns.fill(a.rq.rot, a.rq.pos + t0, n);
+  __syncthreads();
+  const C turned(a.rq.rot);
+  float2 cs[C::PAIRS];
+  turns.get(min(r, n - 1), turned.mine, cs);
+  auto put = [&](int kv, int g, const float (&f)[EPT]) __attribute__((always_inline)) {
+    const int64_t unit = (unit0 + g) << a.pc.shift;
+    store_chunk4<D, EPT>((kv ? a.pc.v : a.pc.k) + unit * (D / 2), static_cast<uint8_t*>(kv ? a.pc.v_scale : a.pc.k_scale) + unit * (D / kGroup4),
+                         row, R, c, live, f);
+  };
+  for (int g = g0; g < g1; g += kBatch) {
+    if (g > g0) load(a.k_new, g);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (g + i >= g1) break;
+      float f[EPT];
+      turned(x[i], cs, f);
+      put(0, g + i, f);
+    }
+    load(a.v_new, g);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (g + i >= g1) break;
+      if constexpr (DT == kDtBf16) {
+        const int64_t unit = (unit0 + g + i) << a.pc.shift;
+        store_chunk4_bf16<D>(a.pc.v + unit * (D / 2), static_cast<uint8_t*>(a.pc.v_scale) + unit * (D / kGroup4), row, R, c, live, x[i]);
+      } else {
+        float f[EPT];
+        chunk_values<DT>(x[i], f);
+        put(1, g + i, f);
+      }
+    }
+  }
+}
+
+namespace {
+
+// Whether 8-bit appending takes the runs as long ones: by the tokens to a request.  256 single rows 14.0 us as short ones, 31.6
+// as long ones, 2000 28.6 and 57; 1000 tokens of four prompts in blocks of 64 rows 69 and 21.
+bool is_long(const Paged& pc, int n_tok) { return n_tok > 4 * (int64_t)pc.n_prob; }
+
+template <int DT, int D, bool INTERLEAVED> hipError_t append4(AppendRotatedArgs a, hipStream_t stream) {
+  constexpr int ROWS = kRotatedRows4<DT, D>;
+  const int64_t groups = ((int64_t)a.rq.n_tok + ROWS - 1) / ROWS;
+  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(a.pc.h_kv, 1024 / groups));
+  const size_t lds = turn_bytes(a.rq.rot.rot, std::max(ROWS, kRotateRows<DT, D>));
+  paged_rotated4_kernel<DT, D, INTERLEAVED><<<(unsigned)(a.q_wgs + groups * a.parts), kStoreThreads, lds, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <int DT, int QT, int D, int SHIFT, bool INTERLEAVED, bool LONG> hipError_t append(AppendRotatedArgs a, hipStream_t stream) {
+  const int64_t windows = ((int64_t)a.rq.n_tok + 63) / 64;
+  // a run to a workgroup: those of a prompt, or single rows of many requests; then parts of its heads (two to four waves
+  // with short runs), as many as fill the chip
+  constexpr int64_t kFill = LONG ? 2048 : 1024;
+  a.n_share = LONG ? std::max(1, 64 >> SHIFT) : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(a.rq.n_tok, 64), kFill / windows));
+  constexpr int HEADS = LONG ? Tiling<DT, D, SHIFT, true>::HEADS : 2;
+  const int most = (a.pc.h_kv + HEADS - 1) / HEADS;
+  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, kFill / (windows * a.n_share)));
+  const size_t lds = turn_bytes(a.rq.rot.rot, std::max(kRotateRows<DT, D>, 1 << SHIFT));
+  auto kernel = paged_rotated_kernel<DT, QT, D, SHIFT, INTERLEAVED, LONG>;
+  if (lds > (64 << 10)) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<(unsigned)(a.q_wgs + windows * a.n_share * a.parts), kStoreThreads, lds, stream>>>(a);
+  return hipGetLastError();
+}
+template <int DT, int QT, int D, int SHIFT, bool INTERLEAVED> hipError_t append(const AppendRotatedArgs& a, hipStream_t stream) {
+  return is_long(a.pc, a.rq.n_tok) ? append<DT, QT, D, SHIFT, INTERLEAVED, true>(a, stream)
+                                   : append<DT, QT, D, SHIFT, INTERLEAVED, false>(a, stream);
+}
+
+}  // namespace
+
 hipError_t launch_paged_append_rotated(const Paged& pc, const RotateArgs& rq, const void* k_new, const void* v_new,
                                        int64_t tok_stride, const int32_t* slots, hipStream_t stream) {
   AppendRotatedArgs a{pc, rq, k_new, v_new, (uint32_t)(tok_stride * (pc.dtype == kDtBf16 ? 2 : 4)), slots, 0, 1, 1};
-  const int64_t windows = ((int64_t)rq.n_tok + 63) / 64;
-  // single rows of many requests are runs of their own: as many workgroups to 64 tokens, and then to a run's heads, as
-  // fill the chip
-  constexpr int64_t kFill = 1024;
-  a.n_share = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(rq.n_tok, 64), kFill / windows));
-  const int most = (2 * pc.h_kv + 3) / 4;
-  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, kFill / (windows * a.n_share)));
   return dispatch(pc, [&](auto dt, auto qt, auto d, auto shift) {
     constexpr int RW = kRotateRows<dt.value, d.value>;
     if (rq.x) {
@@ -184,10 +363,12 @@ hipError_t launch_paged_append_rotated(const Paged& pc, const RotateArgs& rq, co
       a.rq.parts = rotate_parts(groups, rq.heads);
       a.q_wgs = groups * a.rq.parts;
     }
-    const size_t lds = (size_t)std::max(RW, 1 << shift.value) * (rq.rot.rot / 2) * sizeof(float2);
-    const unsigned wgs = (unsigned)(a.q_wgs + windows * a.n_share * a.parts);
-    paged_rotated_kernel<dt.value, qt.value, d.value, shift.value><<<wgs, kStoreThreads, lds, stream>>>(a);
-    return hipGetLastError();
+    if constexpr (qt.value == kQtE2m1) {
+      return rq.rot.interleaved ? append4<dt.value, d.value, true>(a, stream) : append4<dt.value, d.value, false>(a, stream);
+    } else {
+      return rq.rot.interleaved ? append<dt.value, qt.value, d.value, shift.value, true>(a, stream)
+                                : append<dt.value, qt.value, d.value, shift.value, false>(a, stream);
+    }
   });
 }
 

@@ -52,16 +52,51 @@ __device__ __forceinline__ float2 turn(double angle, float factor) {
   return make_float2((float)((q == 1 || q == 2 ? -x : x) * factor), (float)((q >= 2 ? -y : y) * factor));
 }
 
-// The turns of n tokens' pairs, tab[token][rot / 2], by the threads of a workgroup.
-__device__ __forceinline__ void fill_turns(float2* tab, const Rotary& rot, const int32_t* pos, int n) {
-  const int half = rot.rot >> 1;
-  for (int i = threadIdx.x; i < n * half; i += kRotateThreads) {
-    const int t = i / half, f = i - t * half;
-    float2 cs = turn((double)pos[t] * rot.freq[f], rot.factor);
-    cs.y *= rot.sign;
-    tab[i] = cs;
+// Turns in LDS: those of a token's pairs two by two, 16 bytes, in the order that a wave's lanes read them without conflicts:
+// with K of them to a lane, all lanes' first ones come first.  Tokens are kTurnPad apart beyond that.
+constexpr int kTurnPad = 4;
+struct Turns {
+  float4* tab;
+  int quads;   // of a token
+  int lanes;   // that share them
+  int stride;  // between two tokens
+  int per, log_per;  // of a lane
+  // EPT: elements of a chunk; a lane's chunk holds both elements of a pair (interleaved), or one of each of EPT pairs
+  __device__ __forceinline__ Turns(float4* lds, const Rotary& rot, int pairs_of_lane) {
+    tab = lds;
+    quads = rot.rot >> 2;
+    per = pairs_of_lane >> 1;
+    log_per = per == 4 ? 2 : per == 2 ? 1 : 0;
+    lanes = quads >> log_per;
+    stride = quads + kTurnPad;
   }
-}
+  // n tokens' turns, by the threads of a workgroup: a thread keeps to two pairs, and takes every eighth token
+  __device__ __forceinline__ void fill(const Rotary& rot, const int32_t* pos, int n) const {
+    const int q = threadIdx.x & 31;
+    if (q >= quads) return;
+    const double f0 = rot.freq[2 * q], f1 = rot.freq[2 * q + 1];
+    float4* to = tab + (q & (per - 1)) * lanes + (q >> log_per);
+    int t = threadIdx.x >> 5;
+    int next = t < n ? pos[t] : 0;
+    for (; t < n; t += kRotateThreads / 32) {
+      const double p = (double)next;
+      if (t + kRotateThreads / 32 < n) next = pos[t + kRotateThreads / 32];
+      const float2 x = turn(p * f0, rot.factor), y = turn(p * f1, rot.factor);
+      to[t * stride] = make_float4(x.x, x.y * rot.sign, y.x, y.y * rot.sign);
+    }
+  }
+  // those of lane l's pairs of token t
+  template <int N> __device__ __forceinline__ void get(int t, int l, float2 (&cs)[N]) const {
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+      const float4 x = tab[t * stride + k * lanes + l];
+      cs[2 * k] = make_float2(x.x, x.y);
+      cs[2 * k + 1] = make_float2(x.z, x.w);
+    }
+  }
+};
+// LDS bytes of n tokens' turns.
+inline size_t turn_bytes(int rot, int n) { return (size_t)n * (rot / 4 + kTurnPad) * sizeof(float4); }
 
 // The pairs (a[e], b[e]) turned by cs[e].
 template <int N> __device__ __forceinline__ void turn_pairs(float (&a)[N], float (&b)[N], const float2 (&cs)[N]) {
@@ -74,49 +109,46 @@ template <int N> __device__ __forceinline__ void turn_pairs(float (&a)[N], float
   }
 }
 
-// A row's chunk (16 bytes) number c, turned: every lane of the wave calls it, the lanes of a row beside each other.  turns:
-// those of the row's pairs.
-template <int DT, int D> struct TurnChunk {
-  static constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT;
-  bool interleaved, in, low;
-  int partner, first;  // the lane of the other halves of the pairs, and the first pair
+// A row's chunk (16 bytes) number c turned, in the layout that LAYOUT says: every lane of the wave calls it, the lanes of a
+// row beside each other.
+template <int DT, int D, bool INTERLEAVED> struct TurnChunk {
+  static constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, PAIRS = INTERLEAVED ? EPT / 2 : EPT;
+  bool in, all;       // whether the chunk is rotated, and every chunk is
+  uint32_t flip;      // the sign bits of the other halves of the pairs
+  int partner, mine;  // the lane that has these, and the lane's place among those that share a row's turns
   __device__ __forceinline__ explicit TurnChunk(const Rotary& rot) {
     const int lane = threadIdx.x & 63, c = lane % CH, half = rot.rot / EPT / 2;
-    interleaved = rot.interleaved;
     in = c < 2 * half;
-    low = c < half;
-    partner = !in ? lane : low ? lane + half : lane - half;
-    first = !in ? 0 : interleaved ? c * EPT / 2 : (low ? c : c - half) * EPT;
+    all = rot.rot == D;
+    partner = !in ? lane : c < half ? lane + half : lane - half;
+    flip = c < half ? (DT == kDtBf16 ? 0x80008000u : 0x80000000u) : 0u;
+    mine = !in ? 0 : INTERLEAVED || c < half ? c : c - half;
   }
-  __device__ __forceinline__ void operator()(const u32x4_t& x, const float2* turns, float (&f)[EPT]) const {
+  __device__ __forceinline__ void operator()(const u32x4_t& x, const float2 (&cs)[PAIRS], float (&f)[EPT]) const {
 #pragma clang fp contract(off)
     chunk_values<DT>(x, f);
-    if (interleaved) {
-      float a[EPT / 2], b[EPT / 2];
-      float2 cs[EPT / 2];
+    float t[EPT];
+    if constexpr (INTERLEAVED) {
 #pragma unroll
       for (int e = 0; e < EPT / 2; ++e) {
-        a[e] = f[2 * e];
-        b[e] = f[2 * e + 1];
-        cs[e] = turns[first + e];
+        const float a = f[2 * e] * cs[e].x, b = f[2 * e + 1] * cs[e].y, u = f[2 * e + 1] * cs[e].x, v = f[2 * e] * cs[e].y;
+        t[2 * e] = a - b;
+        t[2 * e + 1] = u + v;
       }
-      turn_pairs(a, b, cs);
-#pragma unroll
-      for (int e = 0; e < EPT; ++e) f[e] = !in ? f[e] : e & 1 ? b[e / 2] : a[e / 2];
     } else {
       u32x4_t y;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) y[w] = (uint32_t)__shfl((int)x[w], partner, 64);
+      for (int w = 0; w < 4; ++w) y[w] = (uint32_t)__shfl((int)x[w], partner, 64) ^ flip;
       float g[EPT];
       chunk_values<DT>(y, g);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) {
-        const float2 cs = turns[first + e];
-        const float u = f[e] * cs.x, v = g[e] * cs.y;
-        const float t = low ? u - v : u + v;
-        f[e] = in ? t : f[e];
+        const float a = f[e] * cs[e].x, b = g[e] * cs[e].y;
+        t[e] = a + b;
       }
     }
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) f[e] = all || in ? t[e] : f[e];
   }
 };
 
@@ -124,9 +156,9 @@ template <int DT, int D> struct TurnChunk {
 template <int DT, int D> constexpr int kRotateRows = 64 / (D * (int)sizeof(typename Elem<DT>::T) / 32);
 
 // The heads of a group of kRotateRows tokens that fall to one part: waves and parts take heads in turn, kRotateBatch of them in
-// flight.  tab: LDS of the group's turns.  Every thread of the workgroup calls it.
+// flight.  lds: of the group's turns.  Every thread of the workgroup calls it.
 constexpr int kRotateBatch = 4;
-template <int DT, int D> __device__ __forceinline__ void rotate_group(const RotateArgs& a, int64_t group, int part, float2* tab) {
+template <int DT, int D> __device__ __forceinline__ void rotate_group(const RotateArgs& a, int64_t group, int part, float4* lds) {
   using E = typename Elem<DT>::T;
   constexpr int EPT = 16 / (int)sizeof(E), LPR = D / EPT / 2, RW = kRotateRows<DT, D>, kStep = kRotateThreads / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane / LPR, j = lane % LPR;
@@ -153,11 +185,11 @@ template <int DT, int D> __device__ __forceinline__ void rotate_group(const Rota
     }
   };
   load();
-  fill_turns(tab, a.rot, a.pos + t0, n);
+  const Turns turns(lds, a.rot, EPT);
+  turns.fill(a.rot, a.pos + t0, n);
   __syncthreads();
   float2 cs[EPT];
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) cs[e] = in && live ? tab[row * half + EPT * j + e] : make_float2(1.f, 0.f);
+  turns.get(live ? row : 0, in ? j : 0, cs);
   for (; h0 < a.heads; h0 += kRotateBatch * step, load()) {
 #pragma unroll
     for (int i = 0; i < kRotateBatch; ++i) {

@@ -8,8 +8,8 @@
 namespace kv {
 
 template <int DT, int D> __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a) {
-  extern __shared__ __align__(16) float2 tab[];
-  rotate_group<DT, D>(a, blockIdx.x / a.parts, (int)(blockIdx.x % a.parts), tab);
+  extern __shared__ __align__(16) float4 lds[];
+  rotate_group<DT, D>(a, blockIdx.x / a.parts, (int)(blockIdx.x % a.parts), lds);
 }
 
 namespace {
@@ -17,7 +17,7 @@ namespace {
 template <int DT, int D> hipError_t rotate(RotateArgs a, hipStream_t stream) {
   const int64_t groups = ((int64_t)a.n_tok + kRotateRows<DT, D> - 1) / kRotateRows<DT, D>;
   a.parts = rotate_parts(groups, a.heads);
-  const size_t lds = (size_t)kRotateRows<DT, D> * (a.rot.rot / 2) * sizeof(float2);
+  const size_t lds = turn_bytes(a.rot.rot, kRotateRows<DT, D>);
   rotate_kernel<DT, D><<<(unsigned)(groups * a.parts), kRotateThreads, lds, stream>>>(a);
   return hipGetLastError();
 }
