@@ -517,17 +517,27 @@ def decode_attention(cb: CacheBatch, q, k_cache, v_cache, k_new, v_new, scale: f
                                      _stream(stream)), "kv_decode_attention")
 
 
-def _token_rows(t, dtype, device, heads: int, d: int, name: str):
-    """Address and token stride of [tokens, heads, d] rows; tokens may lie apart (slices of a projection)."""
-    shape = t.shape
-    if t.dtype is not dtype or t.device != device or len(shape) != 3 or shape[1] != heads or shape[2] != d:
-        raise ValueError(f"{name} must be a {dtype} tensor [tokens, {heads}, {d}] on {device}")
-    st = t.stride()
-    if st[2] != 1 or (st[1] != d and heads > 1):
+def _token_rows(t, dtype, index: int, heads: int, d: int, name: str):
+    """Address and token stride of [tokens, heads, d] rows on device `index`; tokens may lie apart (slices of a
+    projection)."""
+    n, h, e = t.shape if t.dim() == 3 else (0, -1, -1)
+    if h != heads or e != d or t.dtype is not dtype or t.get_device() != index:
+        raise ValueError(f"{name} must be a {dtype} tensor [tokens, {heads}, {d}] on device {index}")
+    apart, between, one = t.stride()
+    if one != 1 or (between != d and heads > 1):
         raise ValueError(f"the heads of a token must be contiguous in {name}")
-    if shape[0] > 1 and st[0] < heads * d:
+    if n <= 1:
+        return t.data_ptr(), heads * d
+    if apart < heads * d:
         raise ValueError(f"the tokens overlap in {name}")
-    return t.data_ptr(), (st[0] if shape[0] > 1 else heads * d)
+    return t.data_ptr(), apart
+
+
+def _flat(t, dtype, index: int, n: int, name: str):
+    """Address of a contiguous tensor of at least n elements on device `index`."""
+    if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of at least {n} elements on device {index}")
+    return t.data_ptr()
 
 
 class _OnDevice:
@@ -536,6 +546,8 @@ class _OnDevice:
     def _on(self, device):
         import torch
         self.device = device
+        self._index = device.index if device.type == "cuda" else -2  # (no tensor is on it)
+        self._int32, self._int64 = torch.int32, torch.int64
         # the queries under torch.cuda's where this torch has them (torch.cuda.current_stream() makes an object of
         # the stream: 3 us of a call of 9)
         self._current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
@@ -544,7 +556,7 @@ class _OnDevice:
 
     def _stream(self, stream):
         """The stream to launch on: kernels go to the current device, which has to be the tensors'."""
-        index = self.device.index
+        index = self._index
         if index != self._current_device():
             raise ValueError(f"the {self._what} is on {self.device}, which is not the current device")
         return self._raw_stream(index) if stream is None else stream.cuda_stream
@@ -591,7 +603,6 @@ class PagedCache(_OnDevice):
         if table.dim() != 2 or lens.numel() != table.shape[0]:
             raise ValueError("table must be [n_prob, table_stride] and lens [n_prob]")
         self.table, self.lens = table, lens
-        self._int32 = torch.int32
         self._on(table.device)
         self.n_prob = table.shape[0]
         self.struct = KvPagedCache(n_prob=self.n_prob, block_rows=int(block_rows), n_blocks=int(n_blocks),
@@ -628,14 +639,10 @@ class PagedCache(_OnDevice):
 
     def _arg(self, t, dtype, n: int, name: str):
         """Address of a contiguous tensor of at least n elements on the cache's device (None: NULL)."""
-        if t is None:
-            return None
-        if t.dtype is not dtype or not t.is_cuda or t.device != self.device or not t.is_contiguous() or t.numel() < n:
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of at least {n} elements on {self.device}")
-        return t.data_ptr()
+        return None if t is None else _flat(t, dtype, self._index, n, name)
 
     def _rows(self, t, heads: int, name: str):
-        return _token_rows(t, self.rows_dtype, self.device, heads, self.d, name)
+        return _token_rows(t, self.rows_dtype, self._index, heads, self.d, name)
 
 
 def paged_tables(pc: PagedCache, len_in, add, free_blocks, taken_in, taken_out, tok_off, blk_off, slots,
@@ -683,6 +690,7 @@ class Rotary(_OnDevice):
             raise ValueError("freq must be a contiguous float64 device tensor [rot_dim / 2]")
         self.freq = freq
         self._on(freq.device)
+        self._codes = {torch.bfloat16: KV_BF16, torch.float32: KV_F32}
         self.struct = KvRotary(ROTARY_LAYOUTS[layout], 2 * freq.numel(), int(bool(inverse)), float(factor), freq.data_ptr())
         self._ref = ctypes.byref(self.struct)
 
@@ -701,29 +709,21 @@ def rotary_frequencies(family: str, rot_dim: int, base: float = 10000.0, params:
     return np.frombuffer(out, dtype=np.float64).copy(), float(factor.value)
 
 
-def _positions(pos, device, n: int):
-    import torch
-    if pos.dtype is not torch.int32 or pos.device != device or not pos.is_contiguous() or pos.numel() < n:
-        raise ValueError(f"pos must be a contiguous int32 tensor of at least {n} positions on {device}")
-    return pos.data_ptr()
-
-
 def rotate(rot: Rotary, x, pos, out, stream=None) -> None:
     """kv_rotate: x [tokens, heads, d] bf16 or fp32 (tokens of one stride) at positions pos [tokens] int32, to out of the
     same shape and type, which may be x.  No tokens: nothing to do."""
-    import torch
-    if x.dtype not in (torch.bfloat16, torch.float32) or x.dim() != 3:
+    dtype, index = x.dtype, rot._index
+    code = rot._codes.get(dtype)
+    if code is None or x.dim() != 3:
         raise ValueError("x must be a bfloat16 or float32 tensor [tokens, heads, d]")
     n, heads, d = x.shape
-    if out.shape != x.shape:
+    xp, xs = _token_rows(x, dtype, index, heads, d, "x")
+    op, os_ = _token_rows(out, dtype, index, heads, d, "out")
+    if out.shape[0] != n:
         raise ValueError("out must have the shape of x")
-    xp, xs = _token_rows(x, x.dtype, rot.device, heads, d, "x")
-    op, os_ = _token_rows(out, x.dtype, rot.device, heads, d, "out")
-    pp = _positions(pos, rot.device, n)
-    st = rot._stream(stream)
+    pp, st = _flat(pos, rot._int32, index, n, "pos"), rot._stream(stream)
     if n:
-        _check(lib().kv_rotate(rot._ref, KV_BF16 if x.dtype is torch.bfloat16 else KV_F32, heads, d, xp, xs, pp, n, op, os_, st),
-               "kv_rotate")
+        _check(lib().kv_rotate(rot._ref, code, heads, d, xp, xs, pp, n, op, os_, st), "kv_rotate")
 
 
 def paged_append_rotated(pc: PagedCache, rot: Rotary, pos, k_new, v_new, slots, q=None, q_out=None, stream=None) -> None:
@@ -742,7 +742,7 @@ def paged_append_rotated(pc: PagedCache, rot: Rotary, pos, k_new, v_new, slots, 
         op, os_ = pc._rows(q_out, pc.h_q, "q_out")
         if q.shape[0] != n or q_out.shape[0] != n:
             raise ValueError("q and q_out must have as many tokens as k_new")
-    if rot.device != pc.device:
+    if rot._index != pc._index:
         raise ValueError(f"the rotation is on {rot.device}, the cache on {pc.device}")
     pp, sp, st = pc._arg(pos, pc._int32, n, "pos"), pc._arg(slots, pc._int32, n, "slots"), pc._stream(stream)
     if n:
@@ -754,7 +754,6 @@ def paged_rows(pc: PagedCache, row_off, k_out, v_out, n_rows: Optional[int] = No
     """kv_paged_rows: the rows of every problem p into k_out and v_out (either may be None) at row_off[p] h_kv d elements,
     [h_kv][row_off[p + 1] - row_off[p]][d]; row_off [n_prob + 1] int64.  n_rows: the rows that the outputs hold (default:
     all)."""
-    import torch
     unit = pc.h_kv * pc.d
     held = [t.numel() // unit for t in (k_out, v_out) if t is not None]
     if not held:
@@ -762,7 +761,7 @@ def paged_rows(pc: PagedCache, row_off, k_out, v_out, n_rows: Optional[int] = No
     n_rows = min(held) if n_rows is None else int(n_rows)
     kp = pc._arg(k_out, pc.rows_dtype, n_rows * unit, "k_out")
     vp = pc._arg(v_out, pc.rows_dtype, n_rows * unit, "v_out")
-    op, st = pc._arg(row_off, torch.int64, pc.n_prob + 1, "row_off"), pc._stream(stream)
+    op, st = pc._arg(row_off, pc._int64, pc.n_prob + 1, "row_off"), pc._stream(stream)
     if n_rows:
         _check(lib().kv_paged_rows(pc._ref, op, n_rows, kp, vp, st), "kv_paged_rows")
 
