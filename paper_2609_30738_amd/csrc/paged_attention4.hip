@@ -1,13 +1,23 @@
 // Attention of the last tokens of every problem over its 4-bit paged cache (kv_paged_attention on a cache of e2m1
 // codes, up to 32 columns at a time; a column is a (token, query head) pair of the kv head).
 //
-// paged_attn4_kernel: workgroups, columns, splits, references and weights as in paged_attention.hip's kernel; what
-//   differs is how the codes come in.
+// paged_attn4_kernel: columns, references and weights as in paged_attention.hip's kernel.
 //     S^T = K Q^T,  O^T = V^T P^T  by v_mfma_f32_16x16x32_bf16.
-//   The scales belong to a row and 32 of its elements, so they go into the operands, where the conversion from four bits
-//   applies them at no cost (a code times its scale is exact in bf16).  A lane's operand of K is a quarter of a row: at
+//   Codes.  The scales belong to a row and 32 of its elements, so they go into the operands, where the conversion from four
+//   bits applies them at no cost (a code times its scale is exact in bf16).  A lane's operand of K is a quarter of a row: at
 //   d = 128 one 16-byte load and one scale.  For V a lane takes D / 16 elements of each of its rows, a word at d = 128, and
-//   the scales of 16 rows in one load; pairs of rows are put together by byte permutations once converted.
+//   the scales of 16 rows in one load, a byte of which one turn brings to a float's exponent; pairs of rows are put together
+//   by byte permutations once converted.  The weights' sum comes from a row of ones in the same products.
+//   Shares.  Caches of more than a split's rows are one long axis of rounds of 128 rows, problem after problem, that every
+//   unit's workgroups share equally, as many as the chip holds at once: unequal caches cost no idle CUs, and a workgroup
+//   begins once.  The parts of problems that fall to several shares are joined by paged_join4_kernel.
+//   Bound by the cache's reads: one token over 32 caches of 32768 rows (1.07 GB) 182 us, 5.9 TB/s; its loads alone take 175.
+//   24 ragged ones of up to 24001 rows in blocks of 16 (0.41 GB, eight query heads to a kv head) 79 us, 5.1 TB/s (in splits of
+//   2048 rows 86): the scales of 16 rows are half a line; in blocks of 64 76.  Up to five tokens of 16 requests of up to 6001
+//   rows 25.6, in splits 34: latency of the rounds, and 5 for the join; over 32 caches of 100 rows 6.2, latency.
+//   Measured and left: K's codes as they are against e4m3 terms of the queries by v_mfma_scale_f32_16x16x128 (the same for
+//   long caches, 10 us more for five tokens: the queries have to be taken apart first), four tiles a step (the same), two
+//   steps of loads ahead (179 and 25.8, and 1 us more for short calls), four waves a SIMD (the same).
 #include <math.h>
 
 #include <algorithm>
@@ -165,10 +175,12 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
     sp = span_of(a, p);
   }
 
-  while (true) {
+  for (;; sp = span_of(a, p)) {
     const int n_cols = min(sp.n_tok * G - col0, COLS);
-    if (!SHARES && n_cols <= 0) return;
-    if (n_cols > 0) {
+    if (n_cols <= 0) {
+      if (!SHARES || ++p >= a.pc.n_prob) return;
+      continue;
+    }
     const int vis_max = __builtin_amdgcn_readfirstlane(sp.visible(token_of(a, col0 + n_cols - 1)));
     const int vis_min = __builtin_amdgcn_readfirstlane(sp.visible(token_of(a, col0)));
     const int all = max(1, (int)((uint32_t)(vis_max + kRound4 - 1) / kRound4));  // the problem's rounds, and those of the share
@@ -177,281 +189,280 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
     const bool whole = !SHARES || (from == 0 && to == all);
     at = base + to;
     base += all;
-  // The codes and scales of a step's rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n;
-  // their blocks, and where these lie.
-  uint32_t xk[TS][KW], xv[TS][4], ksb[TS];
-  u32x4_t vsb[TS];  // of 16 rows
-  int blk[TS], next_blk[TS];
-  int64_t codes_at[TS], scales_at[TS];
-  const int k_row = 4 * (n & 3) + (n >> 2);
-  // a wave-uniform address and a lane's 32-bit offset
-  const uint32_t k_lane = k_row * RB + kg * (4 * KW), v_lane = kg * RB + n * (NI / 2);
-  const uint32_t ks_lane = (kg * (8 * KW) / kGroup4) * R + k_row, vs_lane = (n * NI / kGroup4) * R;
-  // the table entries of a step's rows are read a step before their codes
-  int ahead[TS];
-  const uniform_ints table = (uniform_ints)(uintptr_t)(a.pc.table + (int64_t)p * a.pc.table_stride);
-  auto look = [&](int rb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < TS; ++t) ahead[t] = table[min(rb + 16 * t, (r1 - 1) & ~15) >> shift];
-  };
-  auto locate = [&](int rb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < TS; ++t) {
-      const int r = min(rb + 16 * t, (r1 - 1) & ~15);
-      next_blk[t] = (uint32_t)ahead[t] < (uint32_t)a.pc.n_blocks ? ahead[t] : -1;
-      const int64_t unit = (int64_t)max(next_blk[t], 0) * a.pc.h_kv + g;
-      codes_at[t] = (unit << shift) * RB + (r & (R - 1)) * RB;
-      scales_at[t] = (unit << shift) * NG + (r & (R - 1));
-    }
-  };
-  auto load_k = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < TS; ++t) {
-      const uint8_t* ks = a.pc.k + codes_at[t];
-      if constexpr (KW == 4) {
-        const u32x4_t u = load_code<NT == 1>(reinterpret_cast<const u32x4_t*>(ks + k_lane));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) xk[t][i] = u[i];
-      } else {
-        const u32x2_t u = load_code<NT == 1>(reinterpret_cast<const u32x2_t*>(ks + k_lane));
-        xk[t][0] = u[0];
-        xk[t][1] = u[1];
-      }
-      ksb[t] = (static_cast<const uint8_t*>(a.pc.k_scale) + scales_at[t])[ks_lane];
-    }
-  };
-  auto load_v = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < TS; ++t) {
-      const uint8_t* vs = a.pc.v + codes_at[t];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (NI == 8) xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint32_t*>(vs + (v_lane + 4 * j * RB)));
-        else xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint16_t*>(vs + (v_lane + 4 * j * RB)));
-      }
-      vsb[t] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.pc.v_scale) + scales_at[t] + vs_lane);
-    }
-  };
 
-  const int rb0 = r0 + wave * STEP;
-  if (rb0 < r1) look(rb0);
-  // a negative scale turns the queries' signs; a scale of 0 gives equal weights, as the least number does
-  const float c = fmaxf(fabsf(a.c), 0x1p-126f);
-  // the queries' operand: column n, elements D / 4 kg + 8 s .. + 7
-  u32x4_t qf[NT][NS][QN];
-  int vis[NT];
+    // The codes and scales of a step's rows: row 16 t + 4 j + kg for V, and for K the row that holds the accumulator's row n;
+    // their blocks, and where these lie.
+    uint32_t xk[TS][KW], xv[TS][4], ksb[TS];
+    u32x4_t vsb[TS];  // of 16 rows
+    int blk[TS], next_blk[TS];
+    int64_t codes_at[TS], scales_at[TS];
+    const int k_row = 4 * (n & 3) + (n >> 2);
+    // a wave-uniform address and a lane's 32-bit offset
+    const uint32_t k_lane = k_row * RB + kg * (4 * KW), v_lane = kg * RB + n * (NI / 2);
+    const uint32_t ks_lane = (kg * (8 * KW) / kGroup4) * R + k_row, vs_lane = (n * NI / kGroup4) * R;
+    // the table entries of a step's rows are read a step before their codes
+    int ahead[TS];
+    const uniform_ints table = (uniform_ints)(uintptr_t)(a.pc.table + (int64_t)p * a.pc.table_stride);
+    auto look = [&](int rb) __attribute__((always_inline)) {
 #pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    const int col = col0 + 16 * ct + n;
-    const bool live = 16 * ct + n < n_cols;
-    const int j = live ? token_of(a, col) : 0, h = live ? col - j * G : 0;
-    vis[ct] = live ? sp.visible(j) : 0;
-    const int64_t at = (int64_t)(sp.tok0 + j) * a.q_stride + (int64_t)(g * G + h) * D;
+      for (int t = 0; t < TS; ++t) ahead[t] = table[min(rb + 16 * t, (r1 - 1) & ~15) >> shift];
+    };
+    auto locate = [&](int rb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const int e = D / 4 * kg + 8 * s;
-      if constexpr (DT == kDtBf16) {
-        qf[ct][s][0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at + e);
-        if (a.c < 0.f) qf[ct][s][0] ^= 0x80008000u;
-      } else {
-        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + e);
-        const float4 x = src[0], y = src[1];
-        float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-        if (a.c < 0.f) {
+      for (int t = 0; t < TS; ++t) {
+        const int r = min(rb + 16 * t, (r1 - 1) & ~15);
+        next_blk[t] = (uint32_t)ahead[t] < (uint32_t)a.pc.n_blocks ? ahead[t] : -1;
+        const int64_t unit = (int64_t)max(next_blk[t], 0) * a.pc.h_kv + g;
+        codes_at[t] = (unit << shift) * RB + (r & (R - 1)) * RB;
+        scales_at[t] = (unit << shift) * NG + (r & (R - 1));
+      }
+    };
+    auto load_k = [&]() __attribute__((always_inline)) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] = -f[i];
+      for (int t = 0; t < TS; ++t) {
+        const uint8_t* ks = a.pc.k + codes_at[t];
+        if constexpr (KW == 4) {
+          const u32x4_t u = load_code<NT == 1>(reinterpret_cast<const u32x4_t*>(ks + k_lane));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xk[t][i] = u[i];
+        } else {
+          const u32x2_t u = load_code<NT == 1>(reinterpret_cast<const u32x2_t*>(ks + k_lane));
+          xk[t][0] = u[0];
+          xk[t][1] = u[1];
         }
-        split_terms<QN>(f, qf[ct][s]);
+        ksb[t] = (static_cast<const uint8_t*>(a.pc.k_scale) + scales_at[t])[ks_lane];
       }
-    }
-  }
-
-  if (rb0 < r1) {
-    locate(rb0);
-    load_k();
-    load_v();
-    if (rb0 + kRound4 < r1) look(rb0 + kRound4);
-  }
-
-  float m[NT], mu[NT];  // mu: m (0 before the first finite logit) and kSlack octaves
-  f32x4v acc[NT][NI], sum[NT];
+    };
+    auto load_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    m[ct] = -INFINITY;
-    mu[ct] = kSlack;
-    sum[ct] = f32x4v{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < TS; ++t) {
+        const uint8_t* vs = a.pc.v + codes_at[t];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) acc[ct][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
-  }
-  const uint32_t v_turn = (8 * kg + 9) & 31;  // turns byte kg of a word to a float's exponent
-
-  // A step's rows; the codes of the step at `next` (if any) load as this one's are used up.
-  auto step = [&](int rb, int next) __attribute__((always_inline)) {
-    int any = 0;
-#pragma unroll
-    for (int t = 0; t < TS; ++t) {
-      blk[t] = next_blk[t];
-      any |= blk[t];
-    }
-    // its rows are not all visible to every column, or a block is missing
-    const bool masked = rb + STEP > vis_min || any < 0;
-    f32x4v lg[NT][TS];
-    // (codes are converted here, not where they were loaded a step before: registers)
-#pragma unroll
-    for (int t = 0; t < TS; ++t)
-#pragma unroll
-      for (int i = 0; i < KW; ++i) asm volatile("" : "+v"(xk[t][i]));
-#pragma unroll
-    for (int t = 0; t < TS; ++t) {
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) lg[ct][t] = f32x4v{0.f, 0.f, 0.f, 0.f};
-      const float ksc = __uint_as_float(ksb[t] << 23);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const u32x4_t kf = decode8_e2m1(xk[t][s], ksc);
-#pragma unroll
-        for (int q = QN - 1; q >= 0; --q)
-#pragma unroll
-          for (int ct = 0; ct < NT; ++ct) lg[ct][t] = mfma16(kf, qf[ct][s][q], lg[ct][t]);
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (NI == 8) xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint32_t*>(vs + (v_lane + 4 * j * RB)));
+          else xv[t][j] = load_code<NT == 1>(reinterpret_cast<const uint16_t*>(vs + (v_lane + 4 * j * RB)));
+        }
+        vsb[t] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.pc.v_scale) + scales_at[t] + vs_lane);
       }
-      if (masked) {
-#pragma unroll
-        for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (blk[t] < 0 || rb + 16 * t + 4 * j + kg >= vis[ct]) lg[ct][t][j] = -INFINITY;
-      }
-    }
-    if (next < r1) {
-      locate(next);
-      load_k();
-      if (next + kRound4 < r1) look(next + kRound4);
-    }
-    float top[NT];
-    bool over = false;
+    };
+
+    const int rb0 = r0 + wave * STEP;
+    if (rb0 < r1) look(rb0);
+    // a negative scale turns the queries' signs; a scale of 0 gives equal weights, as the least number does
+    const float c = fmaxf(fabsf(a.c), 0x1p-126f);
+    // the queries' operand: column n, elements D / 4 kg + 8 s .. + 7
+    u32x4_t qf[NT][NS][QN];
+    int vis[NT];
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) {
-      top[ct] = lg[ct][0][0];
+      const int col = col0 + 16 * ct + n;
+      const bool live = 16 * ct + n < n_cols;
+      const int j = live ? token_of(a, col) : 0, h = live ? col - j * G : 0;
+      vis[ct] = live ? sp.visible(j) : 0;
+      const int64_t at = (int64_t)(sp.tok0 + j) * a.q_stride + (int64_t)(g * G + h) * D;
 #pragma unroll
-      for (int e = 1; e < 4 * TS; ++e) top[ct] = fmaxf(top[ct], lg[ct][e >> 2][e & 3]);
-      over = over || fmaf(top[ct], c, -m[ct]) > kSlack;
-    }
-    if (__ballot(over)) {
+      for (int s = 0; s < NS; ++s) {
+        const int e = D / 4 * kg + 8 * s;
+        if constexpr (DT == kDtBf16) {
+          qf[ct][s][0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at + e);
+          if (a.c < 0.f) qf[ct][s][0] ^= 0x80008000u;
+        } else {
+          const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at + e);
+          const float4 x = src[0], y = src[1];
+          float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+          if (a.c < 0.f) {
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        const float mn = fmaxf(m[ct], column_max(top[ct]) * c);
-        const float f = m[ct] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[ct] - mn);
-        m[ct] = mn;
-        mu[ct] = mn == -INFINITY ? kSlack : mn + kSlack;
-        sum[ct] *= f;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) acc[ct][i] *= f;
+            for (int i = 0; i < 8; ++i) f[i] = -f[i];
+          }
+          split_terms<QN>(f, qf[ct][s]);
+        }
       }
     }
+
+    if (rb0 < r1) {
+      locate(rb0);
+      load_k();
+      load_v();
+      if (rb0 + kRound4 < r1) look(rb0 + kRound4);
+    }
+
+    float m[NT], mu[NT];  // mu: m (0 before the first finite logit) and kSlack octaves
+    f32x4v acc[NT][NI], sum[NT];
 #pragma unroll
-    for (int u = 0; u < TS / 2; ++u) {  // two tiles at a time
-      u32x4_t pf[NT][PN];
+    for (int ct = 0; ct < NT; ++ct) {
+      m[ct] = -INFINITY;
+      mu[ct] = kSlack;
+      sum[ct] = f32x4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        float w[8];
+      for (int i = 0; i < NI; ++i) acc[ct][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
+    }
+    const uint32_t v_turn = (8 * kg + 9) & 31;  // turns byte kg of a word to a float's exponent
+
+    // A step's rows; the codes of the step at `next` (if any) load as this one's are used up.
+    auto step = [&](int rb, int next) __attribute__((always_inline)) {
+      int any = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(lg[ct][2 * u + (e >> 2)][e & 3], c, -mu[ct]));
-        split_terms<PN>(w, pf[ct]);
-        // their sum: as the products take them, with a row of ones
-        const u32x4_t one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-#pragma unroll
-        for (int q = PN - 1; q >= 0; --q) sum[ct] = mfma16(one, pf[ct][q], sum[ct]);
+      for (int t = 0; t < TS; ++t) {
+        blk[t] = next_blk[t];
+        any |= blk[t];
       }
-      float vsc[8];
+      // its rows are not all visible to every column, or a block is missing
+      const bool masked = rb + STEP > vis_min || any < 0;
+      f32x4v lg[NT][TS];
+      // (codes are converted here, not where they were loaded a step before: registers)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        asm volatile("" : "+v"(xv[2 * u + (e >> 2)][e & 3]));
-        const uint32_t s = vsb[2 * u + (e >> 2)][e & 3];
-        vsc[e] = __uint_as_float(__builtin_amdgcn_alignbit(s, s, v_turn));
-      }
-      if (masked) {
-        // a row that a column does not see adds 0 times its values: these have to be finite
+      for (int t = 0; t < TS; ++t)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vsc[e] = fminf(fabsf(vsc[e]), 0x1p125f);
-      }
-      // V^T: pairs of elements of eight rows, put together as pairs of rows
-      auto pair = [&](auto b) __attribute__((always_inline)) {
-        constexpr int B = decltype(b)::value;
-        uint32_t x[8];
+        for (int i = 0; i < KW; ++i) asm volatile("" : "+v"(xk[t][i]));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = decode2_e2m1<B>(xv[2 * u + (e >> 2)][e & 3], vsc[e]);
+      for (int t = 0; t < TS; ++t) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          u32x4_t vf;
+        for (int ct = 0; ct < NT; ++ct) lg[ct][t] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        const float ksc = __uint_as_float(ksb[t] << 23);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vf[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], i ? 0x07060302u : 0x05040100u);
+        for (int s = 0; s < NS; ++s) {
+          const u32x4_t kf = decode8_e2m1(xk[t][s], ksc);
+#pragma unroll
+          for (int q = QN - 1; q >= 0; --q)
+#pragma unroll
+            for (int ct = 0; ct < NT; ++ct) lg[ct][t] = mfma16(kf, qf[ct][s][q], lg[ct][t]);
+        }
+        if (masked) {
 #pragma unroll
           for (int ct = 0; ct < NT; ++ct)
 #pragma unroll
-            for (int q = PN - 1; q >= 0; --q) acc[ct][2 * B + i] = mfma16(vf, pf[ct][q], acc[ct][2 * B + i]);
+            for (int j = 0; j < 4; ++j)
+              if (blk[t] < 0 || rb + 16 * t + 4 * j + kg >= vis[ct]) lg[ct][t][j] = -INFINITY;
         }
-      };
-      pair(std::integral_constant<int, 0>{});
-      pair(std::integral_constant<int, 1>{});
-      if constexpr (NI == 8) {
-        pair(std::integral_constant<int, 2>{});
-        pair(std::integral_constant<int, 3>{});
       }
-    }
-    if (next < r1) load_v();
-  };
+      if (next < r1) {
+        locate(next);
+        load_k();
+        if (next + kRound4 < r1) look(next + kRound4);
+      }
+      float top[NT];
+      bool over = false;
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        top[ct] = lg[ct][0][0];
+#pragma unroll
+        for (int e = 1; e < 4 * TS; ++e) top[ct] = fmaxf(top[ct], lg[ct][e >> 2][e & 3]);
+        over = over || fmaf(top[ct], c, -m[ct]) > kSlack;
+      }
+      if (__ballot(over)) {
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct) {
+          const float mn = fmaxf(m[ct], column_max(top[ct]) * c);
+          const float f = m[ct] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+          m[ct] = mn;
+          mu[ct] = mn == -INFINITY ? kSlack : mn + kSlack;
+          sum[ct] *= f;
+#pragma unroll
+          for (int i = 0; i < NI; ++i) acc[ct][i] *= f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < TS / 2; ++u) {  // two tiles at a time
+        u32x4_t pf[NT][PN];
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct) {
+          float w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(lg[ct][2 * u + (e >> 2)][e & 3], c, -mu[ct]));
+          split_terms<PN>(w, pf[ct]);
+          // their sum: as the products take them, with a row of ones
+          const u32x4_t one = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+          for (int q = PN - 1; q >= 0; --q) sum[ct] = mfma16(one, pf[ct][q], sum[ct]);
+        }
+        float vsc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          asm volatile("" : "+v"(xv[2 * u + (e >> 2)][e & 3]));
+          const uint32_t s = vsb[2 * u + (e >> 2)][e & 3];
+          vsc[e] = __uint_as_float(__builtin_amdgcn_alignbit(s, s, v_turn));
+        }
+        if (masked) {
+          // a row that a column does not see adds 0 times its values: these have to be finite
+#pragma unroll
+          for (int e = 0; e < 8; ++e) vsc[e] = fminf(fabsf(vsc[e]), 0x1p125f);
+        }
+        // V^T: pairs of elements of eight rows, put together as pairs of rows
+        auto pair = [&](auto b) __attribute__((always_inline)) {
+          constexpr int B = decltype(b)::value;
+          uint32_t x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = decode2_e2m1<B>(xv[2 * u + (e >> 2)][e & 3], vsc[e]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            u32x4_t vf;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vf[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], i ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+              for (int q = PN - 1; q >= 0; --q) acc[ct][2 * B + i] = mfma16(vf, pf[ct][q], acc[ct][2 * B + i]);
+          }
+        };
+        pair(std::integral_constant<int, 0>{});
+        pair(std::integral_constant<int, 1>{});
+        if constexpr (NI == 8) {
+          pair(std::integral_constant<int, 2>{});
+          pair(std::integral_constant<int, 3>{});
+        }
+      }
+      if (next < r1) load_v();
+    };
 
-  for (int rb = rb0; rb < r1; rb += kRound4) step(rb, rb + kRound4);  // the waves' steps in turn
+    for (int rb = rb0; rb < r1; rb += kRound4) step(rb, rb + kRound4);  // the waves' steps in turn
 
-  // merge of the waves, 16 columns at a time: element NI (4 kg + j) + i of column n
+    // merge of the waves, 16 columns at a time: element NI (4 kg + j) + i of column n
 #pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    const int cols = min(n_cols - 16 * ct, 16);
-    if (cols <= 0) break;
-    if (kg == 0) {
-      sh_m[wave][n] = m[ct];
-      sh_s[wave][n] = sum[ct][0];
-    }
-    if (n < cols) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < NI; i += 4)
-          *reinterpret_cast<float4*>(&sh_acc[(wave * cols + n) * kStride + (4 * kg + j) * NI + i]) =
-              make_float4(acc[ct][i][j], acc[ct][i + 1][j], acc[ct][i + 2][j], acc[ct][i + 3][j]);
-    }
-    __syncthreads();
-    for (int idx = tid; idx < cols * (D / 4); idx += kThreads) {
-      const int cc = idx / (D / 4), e = idx % (D / 4) * 4;
-      float M = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) M = fmaxf(M, sh_m[i][cc]);
-      float S = 0.f;
-      f32x4v A = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        const float f = part_weight(sh_m[i][cc], M);
-        S = fmaf(sh_s[i][cc], f, S);
-        const f32x4v x = *reinterpret_cast<const f32x4v*>(&sh_acc[(i * cols + cc) * kStride + e]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) A[k] = fmaf(x[k], f, A[k]);
+    for (int ct = 0; ct < NT; ++ct) {
+      const int cols = min(n_cols - 16 * ct, 16);
+      if (cols <= 0) break;
+      if (kg == 0) {
+        sh_m[wave][n] = m[ct];
+        sh_s[wave][n] = sum[ct][0];
       }
-      const int col = col0 + 16 * ct + cc;
-      if (whole) {
-        const int j = token_of(a, col);
-        store_out4<DT>(a.out, ((int64_t)(sp.tok0 + j) * a.pc.h_q + g * G + (col - j * G)) * D + e, A, S);
-      } else {
-        float* pt = a.part + part4_at(cg * a.pc.h_kv + g, share, from > 0 ? 0 : 1, 16 * ct + cc, min(a.max_q * G, COLS), a.shares) * (D + 2);
-        if (e == 0) *reinterpret_cast<float2*>(pt) = make_float2(M, S);
-        *reinterpret_cast<float2*>(pt + 2 + e) = make_float2(A[0], A[1]);
-        *reinterpret_cast<float2*>(pt + 4 + e) = make_float2(A[2], A[3]);
+      if (n < cols) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < NI; i += 4)
+            *reinterpret_cast<float4*>(&sh_acc[(wave * cols + n) * kStride + (4 * kg + j) * NI + i]) =
+                make_float4(acc[ct][i][j], acc[ct][i + 1][j], acc[ct][i + 2][j], acc[ct][i + 3][j]);
       }
+      __syncthreads();
+      for (int idx = tid; idx < cols * (D / 4); idx += kThreads) {
+        const int cc = idx / (D / 4), e = idx % (D / 4) * 4;
+        float M = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) M = fmaxf(M, sh_m[i][cc]);
+        float S = 0.f;
+        f32x4v A = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+          const float f = part_weight(sh_m[i][cc], M);
+          S = fmaf(sh_s[i][cc], f, S);
+          const f32x4v x = *reinterpret_cast<const f32x4v*>(&sh_acc[(i * cols + cc) * kStride + e]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) A[k] = fmaf(x[k], f, A[k]);
+        }
+        const int col = col0 + 16 * ct + cc;
+        if (whole) {
+          const int j = token_of(a, col);
+          store_out4<DT>(a.out, ((int64_t)(sp.tok0 + j) * a.pc.h_q + g * G + (col - j * G)) * D + e, A, S);
+        } else {
+          float* pt = a.part + part4_at(cg * a.pc.h_kv + g, share, from > 0 ? 0 : 1, 16 * ct + cc, min(a.max_q * G, COLS), a.shares) * (D + 2);
+          if (e == 0) *reinterpret_cast<float2*>(pt) = make_float2(M, S);
+          *reinterpret_cast<float2*>(pt + 2 + e) = make_float2(A[0], A[1]);
+          *reinterpret_cast<float2*>(pt + 4 + e) = make_float2(A[2], A[3]);
+        }
+      }
+      if (ct + 1 < NT || SHARES) __syncthreads();
     }
-    if (ct + 1 < NT || SHARES) __syncthreads();
-  }
-    }
-    if (!SHARES || at >= end) return;
-    sp = span_of(a, ++p);
+    if (!SHARES || at >= end || ++p >= a.pc.n_prob) return;
   }
 }
 
@@ -547,13 +558,19 @@ template <int DT, int D> hipError_t attend(const PagedAttnArgs& a, hipStream_t s
 
 }  // namespace
 
-// Workgroups that the chip holds at once, over the units of (kv head, group of columns).
+// Shares of a unit, a (kv head, group of columns): the fewest that take the least time in rounds of the workgroups that the
+// chip holds at once.
 int paged4_shares(const Paged& pc, int max_q) {
   const int64_t cols = (int64_t)max_q * pc.group();
   const int nt = tiles_of(cols);
   const int64_t units = pc.h_kv * ((cols + 16 * nt - 1) / (16 * nt));
   const int64_t held = 256 * ((nt == 1 ? 3 : 2) - (pc.dtype == kDtF32 && pc.d == 128 ? 1 : 0));
-  return (int)((held + units - 1) / units);
+  const int64_t most = std::max<int64_t>(1, held / units) + 8;
+  int64_t best = 1;
+  auto rounds = [&](int64_t n) { return (units * n + held - 1) / held; };
+  for (int64_t n = 2; n <= most; ++n)
+    if (rounds(n) * best < rounds(best) * n) best = n;
+  return (int)best;
 }
 
 size_t paged4_prefix_bytes(const Paged& pc, int max_q) {

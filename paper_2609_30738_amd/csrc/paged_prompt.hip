@@ -1,5 +1,5 @@
-// Attention of many tokens of a problem over its 8-bit paged cache (kv_paged_attention with bf16 queries and
-// more columns, (token, query head) pairs of a kv head, than paged_attention.hip's kernel takes at once).
+// Attention of many tokens of a problem over its paged cache (kv_paged_attention with bf16 queries and more columns,
+// (token, query head) pairs of a kv head, than the kernels of paged_attention.hip and paged_attention4.hip take at once).
 //
 // paged_prompt_kernel: one workgroup of W waves per (32 W columns, split of the rows, kv head, problem), each
 //   wave 32 columns.  Tiles of 64 rows go through LDS in bf16, which holds code * scale exactly (a scale is a
@@ -18,7 +18,7 @@
 //   Bound by the matrix units, 43 % busy, by the weights that they do not hide, and by the LDS beside them, whose
 //   operands a wave reads for itself.  Three prompts of up to 4096 tokens over caches of up to 16384 rows (32 heads
 //   over 8, d = 128): 1838 us, 1.06 PFLOP/s of the 1.58 that a large product reaches; 1135 us at d = 64, 1926 from
-//   int8.  At an earlier step (1900 us) the same without staging took 1612, without the operands' reads 1685, without
+//   int8, 1620 from 4 bits: half the codes to load, and one conversion takes code and scale to bf16.  At an earlier step (1900 us) the same without staging took 1612, without the operands' reads 1685, without
 //   both 1303, the products alone 785.
 //   Measured and left: V transposed as it is staged 2020 (then 1900), both halves' logits before the weights 1890
 //   (then 1842), masked and unmasked tiles as two copies of the code 2905 (then 2372), raised wave priority around the
@@ -193,26 +193,24 @@ __global__ __launch_bounds__(64 * W, 2) void paged_prompt_kernel(PagedAttnArgs a
         vc[i] = *reinterpret_cast<const u32x2_t*>(a.pc.v + at + 8 * (uint32_t)lane);
         ksb[i] = (static_cast<const uint8_t*>(a.pc.k_scale) + sat)[mine];
         vsb[i] = (static_cast<const uint8_t*>(a.pc.v_scale) + sat)[mine];
-        continue;
       } else {
-      const int64_t at = ((unit << shift) + in) * D;
-      kc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.k + at + 16 * (uint32_t)lane);
-      vc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.v + at + 16 * (uint32_t)lane);
-      ksc[i] = next_ks[i];
-      vsc[i] = next_vs[i];
+        const int64_t at = ((unit << shift) + in) * D;
+        kc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.k + at + 16 * (uint32_t)lane);
+        vc[i] = *reinterpret_cast<const u32x4_t*>(a.pc.v + at + 16 * (uint32_t)lane);
+        ksc[i] = next_ks[i];
+        vsc[i] = next_vs[i];
       }
     }
   };
   auto put = [&](uint16_t* to, const Codes& c, float scale) __attribute__((always_inline)) {
-    if constexpr (kFour) {
-#pragma unroll
-      for (int w = 0; w < 2; ++w) *reinterpret_cast<u32x4_t*>(to + 8 * w) = decode8_e2m1(c[w], scale);
-      return;
-    } else
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const u32x2_t y = decode4_bf16<QT>(c[2 * w], scale), z = decode4_bf16<QT>(c[2 * w + 1], scale);
-      *reinterpret_cast<u32x4_t*>(to + 8 * w) = u32x4_t{y[0], y[1], z[0], z[1]};
+      if constexpr (kFour) {
+        *reinterpret_cast<u32x4_t*>(to + 8 * w) = decode8_e2m1(c[w], scale);
+      } else {
+        const u32x2_t y = decode4_bf16<QT>(c[2 * w], scale), z = decode4_bf16<QT>(c[2 * w + 1], scale);
+        *reinterpret_cast<u32x4_t*>(to + 8 * w) = u32x4_t{y[0], y[1], z[0], z[1]};
+      }
     }
   };
   auto stage = [&](int t) __attribute__((always_inline)) {

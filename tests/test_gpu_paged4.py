@@ -395,6 +395,48 @@ def test_attention_of_moving_logits(dtype, d, split, profile):
         assert torch.equal(out, _attend(pc, q, scale, n_q))
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("n", [257, 600, 1025])
+@pytest.mark.parametrize("tokens", [1, 5])
+def test_attention_of_many_unequal_problems(dtype, d, n, tokens):
+    """More requests than a wave looks at at once, most of a few rows or none and some long ones, the first and the last
+    among them, requests without tokens between: shares begin and end in any of them."""
+    rng = _rng(n, d, tokens)
+    lens = np.where(rng.random(n) < 0.2, 0, rng.integers(1, 40, n))
+    lens[[0, 255, 256, n - 1]] = 700, 1, 2500, 641
+    pc = _cache4(rng, dtype, 4, 1, d, 16, lens)
+    n_q = None if tokens == 1 else rng.integers(0, tokens + 1, n)
+    if tokens > 1:
+        n_q[[0, n - 1]] = tokens
+    T = n if n_q is None else int(n_q.sum())
+    q = _q(rng, T, 4, d, dtype)
+    assert _lib.paged_attention_workspace_bytes(pc, T, tokens) > 0
+    _say("attention4 many unequal", dtype, d, n, tokens)
+    _check4(pc, q, 0.1, n_q, _attend(pc, q, 0.1, n_q), "many unequal", tokens)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("max_q", [2, 9])
+@pytest.mark.parametrize("max_len", [300, 2000])
+def test_attention_of_offsets_that_are_none(dtype, max_q, max_len):
+    """Offsets that fall, by so much that the number of columns leaves 32 bits, or lie anywhere: the problems between them
+    are left out, and the ones beside them are not."""
+    import torch
+    rng = _rng(41, max_q)
+    pc = _cache4(rng, dtype, 32, 2, 64, 16, [40, 50, 60, 33, 70, 80, 90], max_len=max_len, stride=125)
+    q = _q(rng, 12, 32, 64, dtype)
+    off = torch.tensor([0, 2, (1 << 27) + 1, 0, (1 << 31) - 1, -(1 << 31), 10, 12], dtype=torch.int32, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    nb = _lib.paged_attention_workspace_bytes(pc, 12, max_q)
+    ws = torch.full((nb,), 0xFF, dtype=torch.uint8, device="cuda") if nb else None
+    _say("attention4 offsets", dtype, max_q, max_len)
+    _lib.paged_attention(pc, q, 0.1, out, off, max_q, ws)
+    assert (out[2:10] == 7).all()
+    for at, p in ((slice(0, 2), slice(0, 1)), (slice(10, 12), slice(6, 7))):
+        one = _lib.PagedCache(dtype, 32, pc.k, pc.v, pc.k_scale, pc.v_scale, pc.table[p], pc.lens[p], max_len)
+        _check4(one, q[at], 0.1, [2], out[at], "beside", max_q)
+
+
 def test_attention_turn_over_more_blocks_than_a_split_holds():
     """5000 rows in blocks of 16: two splits although the batch fills the chip."""
     rng = _rng(31)
