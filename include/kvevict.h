@@ -511,14 +511,15 @@ int kv_rotary_frequencies(int32_t family, double base, const double* params_host
 
 /* Rows rotated by their positions: token t's heads x + t * x_stride + h * d elements, h < heads, to
  * out + t * out_stride + h * d, at position pos[t] (pos [n_tok] on the device).  dtype of x and out; the products in fp32, rounded
- * once.  Strides as in kv_paged_append (0: heads * d).  out may be x with x's stride; any other overlap of their rows is
- * KV_ERR_ARG.  d in {64, 128}, heads >= 1, 1 <= n_tok <= 2^25. */
+ * once.  Strides as in kv_paged_append (0: heads * d).  out may be x with x's stride, or other
+ * columns of the same wide rows; any other overlap of the memory that the two span is KV_ERR_ARG.  d in {64, 128}, heads >= 1, 1 <= n_tok <= 2^25. */
 int kv_rotate(const kv_rotary* rot, int32_t dtype, int32_t heads, int32_t d, const void* x, int64_t x_stride,
               const int32_t* pos, int32_t n_tok, void* out, int64_t out_stride, void* stream);
 
 /* kv_paged_append of rotated keys, at positions pos [n_tok] (a row's place in a cache that was evicted is not its position):
  * k_new is rotated in fp32 and coded from there, as kv_rotate of fp32 rows and kv_paged_append would, v_new as it is.  q
- * (nullable): every token's queries are rotated too, as kv_rotate does from q to q_out, whatever the token's slot.  n_tok <= 2^25. */
+ * (nullable): every token's queries are rotated too, as kv_rotate does from q to q_out, whatever the token's slot; q_out's
+ * rows meet neither k_new's nor v_new's (KV_ERR_ARG).  n_tok <= 2^25. */
 int kv_paged_append_rotated(const kv_paged_cache* pc, const kv_rotary* rot, const int32_t* pos, const void* q, int64_t q_stride,
                             void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new, int64_t tok_stride,
                             const int32_t* slots, int32_t n_tok, void* stream);
@@ -526,7 +527,8 @@ int kv_paged_append_rotated(const kv_paged_cache* pc, const kv_rotary* rot, cons
 /* The caches' rows as contiguous keys and values, in kv_problem's layout, so that an eviction can run over them again:
  * problem p's L_p = row_off[p + 1] - row_off[p] rows to k_out, v_out + row_off[p] * h_kv * d elements, [h_kv][L_p][d] of the cache's
  * dtype (row_off [n_prob + 1] on the device).  Rows from len[p] on, and rows of missing blocks, are zeros.  A problem whose row_off reaches
- * outside [0, n_rows], falls or spans more than max_len is left out.  k_out or v_out may be NULL, not both. */
+ * outside [0, n_rows], falls or spans more than max_len is left out.  k_out or v_out may be NULL, not both; they do not
+ * overlap (KV_ERR_ARG). */
 int kv_paged_rows(const kv_paged_cache* pc, const int64_t* row_off, int64_t n_rows, void* k_out, void* v_out, void* stream);
 
 /* kv_compact_cache_ex into the blocks (sections 1 and 3.1): rows 0 .. B_p - 1 of problem p and head g are
@@ -555,7 +557,8 @@ size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_to
  * tokens outside every problem (a padded batch) stay as they were, and so do a problem's whose tok_off reaches outside
  * [0, n_tok], falls or spans more than max_q.  Turns that a launch does not take are refused (KV_ERR_SHAPE): with fp32
  * queries h_kv ceil(max_q (h_q / h_kv) / 32) > 65535 (8 kv heads of 4: 65,528 tokens go), with bf16 ones
- * ceil(max_q (h_q / h_kv) / 256) ceil(max_len / (4096 block_rows)) > 65535, and max_q > 2^24.  Calls that overlap on one workspace race. */
+ * ceil(max_q (h_q / h_kv) / 256) ceil(max_len / (4096 block_rows)) > 65535, and max_q > 2^24; over KV_E2M1
+ * n_prob (max_len / 128 + 1) >= 2^31 too (up to 32 bf16 columns, any float ones).  Calls that overlap on one workspace race. */
 int kv_paged_attention(const kv_paged_cache* pc, const void* q, int64_t q_stride, const int32_t* tok_off,
                        int32_t n_tok, int32_t max_q, float scale, void* out, void* ws, size_t ws_bytes,
                        void* stream);

@@ -850,15 +850,14 @@ int check_rotary(const kv_rotary* r, int d, kv::Rotary* rot) {
   return KV_OK;
 }
 
-// Whether rows of `bytes` bytes, n of them x_step (out_step) bytes apart, meet in any other way than row for row.
-bool rows_overlap(const void* x, int64_t x_step, const void* out, int64_t out_step, int64_t bytes, int64_t n) {
+// Whether n rows of x_bytes bytes, x_step apart, meet n of out_bytes, out_step apart.
+bool rows_overlap(const void* x, int64_t x_step, int64_t x_bytes, const void* out, int64_t out_step, int64_t out_bytes, int64_t n) {
   const intptr_t p = reinterpret_cast<intptr_t>(x), q = reinterpret_cast<intptr_t>(out);
-  if (x_step == out_step && (p == q || n == 1)) return p != q && p < q + bytes && q < p + bytes;
-  if (p >= q + (n - 1) * out_step + bytes || q >= p + (n - 1) * x_step + bytes) return false;
-  if (x_step != out_step) return n > 1 || (p != q && p < q + bytes && q < p + bytes);
+  if (p >= q + (n - 1) * out_step + out_bytes || q >= p + (n - 1) * x_step + x_bytes) return false;
+  if (x_step != out_step || n == 1) return true;
   // slices of the same wide rows
   const int64_t apart = ((q - p) % x_step + x_step) % x_step;
-  return apart < bytes || x_step - apart < bytes;
+  return apart < x_bytes || x_step - apart < out_bytes;
 }
 
 // The rows of a rotation from x to out.
@@ -874,7 +873,9 @@ int check_rotate(const kv::Rotary& rot, int dtype, int heads, int d, const void*
   if (st == KV_OK) st = check_stride(pc, heads, &out_stride);
   if (st != KV_OK) return st;
   const int64_t e = dtype == kv::kDtBf16 ? 2 : 4;
-  if (rows_overlap(x, x_stride * e, out, out_stride * e, heads * d * e, n_tok)) return KV_ERR_ARG;
+  const int64_t bytes = (int64_t)heads * d * e;
+  const bool in_place = x == out && (x_stride == out_stride || n_tok == 1);
+  if (!in_place && rows_overlap(x, x_stride * e, bytes, out, out_stride * e, bytes, n_tok)) return KV_ERR_ARG;
   *a = {rot, x, out, x_stride, out_stride, pos, n_tok, heads, 1};
   return KV_OK;
 }
@@ -982,8 +983,13 @@ int kv_paged_append_rotated(const kv_paged_cache* c, const kv_rotary* r, const i
   st = check_stride(pc, pc.h_kv, &tok_stride);
   if (st != KV_OK) return st;
   kv::RotateArgs rq{rot, nullptr, nullptr, 0, 0, pos, n_tok, 0, 1};
-  if (q) st = check_rotate(rot, pc.dtype, pc.h_q, pc.d, q, q_stride, pos, n_tok, q_out, q_out_stride, &rq);
-  if (st != KV_OK) return st;
+  if (q) {
+    st = check_rotate(rot, pc.dtype, pc.h_q, pc.d, q, q_stride, pos, n_tok, q_out, q_out_stride, &rq);
+    if (st != KV_OK) return st;
+    const int64_t e = pc.dtype == kv::kDtBf16 ? 2 : 4, q_bytes = (int64_t)pc.h_q * pc.d * e, bytes = (int64_t)pc.h_kv * pc.d * e;
+    for (const void* rows : {k_new, v_new})
+      if (rows_overlap(rows, tok_stride * e, bytes, q_out, rq.out_stride * e, q_bytes, n_tok)) return KV_ERR_ARG;
+  }
   return launch_status(kv::launch_paged_append_rotated(pc, rq, k_new, v_new, tok_stride, slots, static_cast<hipStream_t>(stream)));
 }
 
@@ -993,6 +999,9 @@ int kv_paged_rows(const kv_paged_cache* c, const int64_t* row_off, int64_t n_row
   if (st != KV_OK) return st;
   if (!row_off || (!k_out && !v_out)) return KV_ERR_NULL;
   if (!aligned16(k_out) || !aligned16(v_out) || n_rows < 1) return KV_ERR_ARG;
+  const uintptr_t kp = reinterpret_cast<uintptr_t>(k_out), vp = reinterpret_cast<uintptr_t>(v_out);
+  const uintptr_t row_bytes = (uintptr_t)pc.h_kv * pc.d * (pc.dtype == kv::kDtBf16 ? 2 : 4), apart = kp > vp ? kp - vp : vp - kp;
+  if (k_out && v_out && apart / row_bytes < (uintptr_t)n_rows) return KV_ERR_ARG;
   return launch_status(kv::launch_paged_rows(pc, row_off, n_rows, k_out, v_out, static_cast<hipStream_t>(stream)));
 }
 

@@ -24,15 +24,17 @@ template <int DT, int QT, int D> __global__ __launch_bounds__(256) void paged_ro
   constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH, NC = 16 / RPP;
   constexpr int CB = QT == kQtE2m1 ? EPT / 2 : EPT;  // bytes of a chunk's codes
   const int g = blockIdx.y, p = blockIdx.z, lane = threadIdx.x & 63, c = lane % CH, rr = lane / CH;
+  const int r0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 16, shift = a.pc.shift, j = r0 >> shift, in = r0 & ((1 << shift) - 1);
+  // (loads beside each other)
   const int64_t off = a.row_off[p], end = a.row_off[p + 1];
+  const int id = j < a.pc.table_stride ? a.pc.table[(int64_t)p * a.pc.table_stride + j] : -1;
+  const int rows = a.pc.len[p];
   // none where the offsets fall or leave the output
   if (off < 0 || end < off || end > a.n_rows || end - off > a.pc.max_len) return;
-  const int L = (int)(end - off), r0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 16;
+  const int L = (int)(end - off);
   if (r0 >= L) return;
-  const int shift = a.pc.shift, j = r0 >> shift, in = r0 & ((1 << shift) - 1);
-  const int id = j < a.pc.table_stride ? a.pc.table[(int64_t)p * a.pc.table_stride + j] : -1;
   const bool has = id >= 0 && id < a.pc.n_blocks;
-  const int len = has ? min(max(a.pc.len[p], 0), L) : 0;  // rows from here on are zeros
+  const int len = has ? min(max(rows, 0), L) : 0;  // rows from here on are zeros
   const int64_t unit = (int64_t)(has ? id : 0) * a.pc.h_kv + g;
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {

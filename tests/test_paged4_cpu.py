@@ -201,6 +201,20 @@ def test_rotate_overlaps():
         assert _rotate(r, **kw) == _lib.KV_ERR_ARG, kw
     c = ctypes.byref(_cache(**E2M1))
     assert _append_rotated(c, r, qo=at(8)) == _append_rotated(c, r, qo=at(4096)) == _lib.KV_ERR_ARG
+    # the rotated queries over the keys or values: the same rows, a slice that reaches into theirs
+    far = ctypes.c_void_p(P.value + (1 << 20))
+    for kw in (dict(k=far), dict(v=far), dict(k=ctypes.c_void_p(far.value + 2 * 3 * 1024)),
+               dict(v=ctypes.c_void_p(far.value + 2 * (6144 + 4088)), stride=6144, qos=6144)):
+        assert _append_rotated(c, r, qo=far, **kw) == _lib.KV_ERR_ARG, kw
+
+
+def test_attention_counts_rounds_in_32_bits():
+    """All problems' rounds of 128 rows, n_prob (max_len / 128 + 1), stay below 2^31."""
+    far = dict(E2M1, max_len=1 << 24, table_stride=1 << 18, block_rows=64)
+    assert (1 << 24) // 128 + 1 == 131073 and 16383 * 131073 < 1 << 31 < 16384 * 131073
+    for n, code in ((16384, _lib.KV_ERR_SHAPE), (65535, _lib.KV_ERR_SHAPE), (16383, _lib.KV_ERR_WORKSPACE)):
+        c = ctypes.byref(_cache(n_prob=n, **far))
+        assert _attend(c, n_tok=n, max_q=1) == code, n
 
 
 def test_append_rotated_checks():
@@ -217,6 +231,9 @@ def test_append_rotated_checks():
 def test_rows_checks():
     c = ctypes.byref(_cache(**E2M1))
     assert _rows(None) == _rows(c, off=NULL) == _rows(c, k=NULL, v=NULL) == _lib.KV_ERR_NULL
+    row = 8 * 128 * 2
+    for kw in (dict(), dict(v=ctypes.c_void_p(P.value + 9 * row - 16)), dict(k=ctypes.c_void_p(P.value + 8 * row))):
+        assert _rows(c, n=9, **kw) == _lib.KV_ERR_ARG, kw  # keys and values overlap
     assert _rows(c, k=ODD) == _rows(c, v=ODD, k=NULL) == _rows(c, n=0) == _rows(c, n=-1) == _lib.KV_ERR_ARG
 
 
