@@ -1,6 +1,10 @@
 // New rows into the blocks of a paged cache with the keys rotated on the way, and the rotated queries
 // (kv_paged_append_rotated).
 //
+// Bound by HBM: 36,000 tokens of 32 query heads and 8 of K and V into 8 bits (1.0 GB) 197 us, 5.1 TB/s, a copy's 5.5; K and V
+// alone (219 MB) 72, 3.1 TB/s.  The same into 4 bits 235.  64 single tokens 8.4, 24 into 4 bits 6: a chain of loads (slots, then
+// the block's scale), the turns and the launch.
+//
 // Some workgroups rotate queries as kv_rotate does.  The others form the turns of their tokens' pairs once, in LDS, and go
 // over the heads with them; a key's chunk is turned in registers, with the chunk of the other halves of its pairs from its
 // lane, and coded from the 32-bit values: it never reaches memory in another form.
@@ -31,14 +35,16 @@ struct AppendRotatedArgs {
 namespace {
 
 // The rows of a block in tiles.  Long runs: a tile's rows fall to the four waves, and a lane's chunks of a few heads are in
-// registers together.  Short ones: a wave takes a head by itself.
+// registers together, kHeld of them, of at most four heads.  Short ones: a wave takes a head by itself.
+// K and V of 36,000 tokens in blocks of 64 rows 72 us, with 4 chunks 74, with 16 77; of 128 rows 89, 122, 108; of 16 rows,
+// four heads 67, eight 79.
 constexpr int kHeld = 8;
 template <int DT, int D, int SHIFT, bool LONG> struct Tiling {
   static constexpr int EPT = 16 / (int)sizeof(typename Elem<DT>::T), CH = D / EPT, RPP = 64 / CH, W = LONG ? kStoreThreads / 64 : 1;
   static constexpr int ROWS = RPP * W;  // of a tile
   static constexpr int TILES = (1 << SHIFT) > ROWS ? (1 << SHIFT) / ROWS : 1;
   static constexpr bool TWICE = !LONG || TILES > kHeld;  // runs of more than TB tiles are read twice
-  static constexpr int TB = !LONG ? 1 : TWICE ? kHeld : TILES, HEADS = LONG ? kHeld / TB : 1;
+  static constexpr int TB = !LONG ? 1 : TWICE ? kHeld : TILES, HEADS = LONG ? std::min(kHeld / TB, 4) : 1;
 };
 
 // A workgroup's run: rows row0 .. row0 + n - 1 of a block, and the heads from g to end - 1 of K (KV 0, turned) or V.
@@ -315,13 +321,14 @@ __global__ __launch_bounds__(kStoreThreads) void paged_rotated4_kernel(AppendRot
 
 namespace {
 
-// Whether 8-bit appending takes the runs as long ones: by the tokens to a request.  256 single rows 14.0 us as short ones, 31.6
-// as long ones, 2000 28.6 and 57; 1000 tokens of four prompts in blocks of 64 rows 69 and 21.
+// Whether 8-bit appending takes the runs as long ones: by the tokens to a request.  2000 single rows 28.6 us as short ones,
+// 57 as long ones; 1000 tokens of four prompts in blocks of 64 rows 69 and 21.
 bool is_long(const Paged& pc, int n_tok) { return n_tok > 4 * (int64_t)pc.n_prob; }
 
 template <int DT, int D, bool INTERLEAVED> hipError_t append4(AppendRotatedArgs a, hipStream_t stream) {
   constexpr int ROWS = kRotatedRows4<DT, D>;
   const int64_t groups = ((int64_t)a.rq.n_tok + ROWS - 1) / ROWS;
+  // parts of the heads, up to 1024 workgroups (10,500 tokens into 4 bits 22 us, with 2048 23; single ones the same)
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(a.pc.h_kv, 1024 / groups));
   const size_t lds = turn_bytes(a.rq.rot.rot, std::max(ROWS, kRotateRows<DT, D>));
   paged_rotated4_kernel<DT, D, INTERLEAVED><<<(unsigned)(a.q_wgs + groups * a.parts), kStoreThreads, lds, stream>>>(a);
@@ -330,10 +337,11 @@ template <int DT, int D, bool INTERLEAVED> hipError_t append4(AppendRotatedArgs 
 
 template <int DT, int QT, int D, int SHIFT, bool INTERLEAVED, bool LONG> hipError_t append(AppendRotatedArgs a, hipStream_t stream) {
   const int64_t windows = ((int64_t)a.rq.n_tok + 63) / 64;
-  // a run to a workgroup: those of a prompt, or single rows of many requests; then parts of its heads (two to four waves
-  // with short runs), as many as fill the chip
-  constexpr int64_t kFill = LONG ? 2048 : 1024;
-  a.n_share = LONG ? std::max(1, 64 >> SHIFT) : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(a.rq.n_tok, 64), kFill / windows));
+  // a run to a workgroup: those of a prompt, or single rows of many requests (up to 1024 workgroups: 2000 single rows 28.6 us,
+  // with 512 37.8, with 2048 35.4); then parts of its heads, each of which forms the run's turns: 2048 workgroups of long runs
+  // (72.1, with 1024 77.7, with 4096 73.5), 256 of short ones (256 single rows 10.5, with 1024 13.9; 128 8.7 and 9.4)
+  constexpr int64_t kFill = LONG ? 2048 : 256;
+  a.n_share = LONG ? std::max(1, 64 >> SHIFT) : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(a.rq.n_tok, 64), 1024 / windows));
   constexpr int HEADS = LONG ? Tiling<DT, D, SHIFT, true>::HEADS : 2;
   const int most = (a.pc.h_kv + HEADS - 1) / HEADS;
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, kFill / (windows * a.n_share)));

@@ -3,6 +3,8 @@
 // rotate_kernel: one workgroup of four waves per (a few tokens, part of the heads).  The turns of the tokens' pairs are the
 //   same for every head: the workgroup forms them once, in 64 bits, beside the first rows' loads, and keeps them in LDS; a
 //   lane holds those of its chunks in registers while it goes over the heads.
+//   Bound by HBM: 31744 tokens of 32 heads of 128 (520 MB read and written) 91 us, 5.7 TB/s; in fp32 186; 64 tokens 6.2, of
+//   which the kernel takes 3.4.
 #include "rotary.h"
 
 namespace kv {
