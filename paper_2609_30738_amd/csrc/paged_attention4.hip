@@ -11,10 +11,10 @@
 //   Shares.  Caches of more than a split's rows are one long axis of rounds of 128 rows, problem after problem, that every
 //   unit's workgroups share equally, as many as the chip holds at once: unequal caches cost no idle CUs, and a workgroup
 //   begins once.  The parts of problems that fall to several shares are joined by paged_join4_kernel.
-//   Bound by the cache's reads: one token over 32 caches of 32768 rows (1.07 GB) 182 us, 5.9 TB/s; its loads alone take 175.
-//   24 ragged ones of up to 24001 rows in blocks of 16 (0.41 GB, eight query heads to a kv head) 79 us, 5.1 TB/s (in splits of
-//   2048 rows 86): the scales of 16 rows are half a line; in blocks of 64 76.  Up to five tokens of 16 requests of up to 6001
-//   rows 25.6, in splits 34: latency of the rounds, and 5 for the join; over 32 caches of 100 rows 6.2, latency.
+//   Bound by the cache's reads: one token over 32 caches of 32768 rows (1.07 GB) 180 us, 6.0 TB/s; its loads alone take 175.
+//   24 ragged ones of up to 24001 rows in blocks of 16 (0.41 GB, eight query heads to a kv head) 78 us, 5.2 TB/s (in splits of
+//   2048 rows 86): the scales of 16 rows are half a line; in blocks of 64 74.  Up to five tokens of 16 requests of up to 6001
+//   rows 26, in splits 34: latency of the rounds, and 5 for the join; over 32 caches of 100 rows 6.2, latency.
 //   Measured and left: K's codes as they are against e4m3 terms of the queries by v_mfma_scale_f32_16x16x128 (the same for
 //   long caches, 10 us more for five tokens: the queries have to be taken apart first), four tiles a step (the same), two
 //   steps of loads ahead (179 and 25.8, and 1 us more for short calls), four waves a SIMD (the same).
@@ -39,7 +39,9 @@ constexpr int kWaves = kAttnWaves;
 constexpr int kTiles4 = 2;
 template <int DT, int D, int NT> constexpr int kMinWaves4 = (NT == 1 ? 3 : 2) - (DT == kDtF32 && D == 128 ? 1 : 0);
 
-constexpr int kLeastRounds4 = 2;  // of a share
+// Of a share: with one, its first loads are most of it, and there are more to join (one cache of up to 6000 rows 10.6 us, with
+// one round 11.5, with four 12.0; 8 of up to 2000 13.2, 13.2 and 14.3).
+constexpr int kLeastRounds4 = 2;
 constexpr int kRound4 = kWaves * 16 * kTiles4;  // rows of a workgroup's round
 
 typedef const __attribute__((address_space(4))) int32_t* uniform_ints;  // read by scalar loads

@@ -2,6 +2,8 @@
 //
 // paged_rows_kernel: one workgroup of four waves per (64 rows, kv head, problem), a wave 16 rows of K and of V, whose block
 //   is the wave's.  A lane writes 16 bytes; the codes of all 16 rows are in flight together.
+//   Bound by HBM: 44,400 rows of 8 heads of 128 from 4 bits (48 MB read, 182 MB written) 37 us, 6.2 TB/s, 15,400 rows 16.7;
+//   24 caches of up to 131 rows 4.7: offsets, tables and lengths in one step of loads, codes and scales in another.
 #include <math.h>
 
 #include <algorithm>

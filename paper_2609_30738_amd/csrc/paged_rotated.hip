@@ -1,8 +1,8 @@
 // New rows into the blocks of a paged cache with the keys rotated on the way, and the rotated queries
 // (kv_paged_append_rotated).
 //
-// Bound by HBM: 36,000 tokens of 32 query heads and 8 of K and V into 8 bits (1.0 GB) 197 us, 5.1 TB/s, a copy's 5.5; K and V
-// alone (219 MB) 72, 3.1 TB/s.  The same into 4 bits 235.  64 single tokens 8.4, 24 into 4 bits 6: a chain of loads (slots, then
+// Bound by HBM: 44,400 tokens of 32 query heads and 8 of K and V into 8 bits (1.0 GB) 197 us, 5.1 TB/s, a copy's 5.5; K and V
+// alone (273 MB) 72, 3.8 TB/s.  The same into 4 bits 198 and 66.  64 single tokens 8.4, 24 into 4 bits 6: a chain of loads (slots, then
 // the block's scale), the turns and the launch.
 //
 // Some workgroups rotate queries as kv_rotate does.  The others form the turns of their tokens' pairs once, in LDS, and go
@@ -36,7 +36,7 @@ namespace {
 
 // The rows of a block in tiles.  Long runs: a tile's rows fall to the four waves, and a lane's chunks of a few heads are in
 // registers together, kHeld of them, of at most four heads.  Short ones: a wave takes a head by itself.
-// K and V of 36,000 tokens in blocks of 64 rows 72 us, with 4 chunks 74, with 16 77; of 128 rows 89, 122, 108; of 16 rows,
+// K and V of 44,400 tokens in blocks of 64 rows 72 us, with 4 chunks 74, with 16 77; of 128 rows 89, 122, 108; of 16 rows,
 // four heads 67, eight 79.
 constexpr int kHeld = 8;
 template <int DT, int D, int SHIFT, bool LONG> struct Tiling {
@@ -322,13 +322,13 @@ __global__ __launch_bounds__(kStoreThreads) void paged_rotated4_kernel(AppendRot
 namespace {
 
 // Whether 8-bit appending takes the runs as long ones: by the tokens to a request.  2000 single rows 28.6 us as short ones,
-// 57 as long ones; 1000 tokens of four prompts in blocks of 64 rows 69 and 21.
+// 57 as long ones; 1200 tokens of four prompts in blocks of 64 rows 69 and 21.
 bool is_long(const Paged& pc, int n_tok) { return n_tok > 4 * (int64_t)pc.n_prob; }
 
 template <int DT, int D, bool INTERLEAVED> hipError_t append4(AppendRotatedArgs a, hipStream_t stream) {
   constexpr int ROWS = kRotatedRows4<DT, D>;
   const int64_t groups = ((int64_t)a.rq.n_tok + ROWS - 1) / ROWS;
-  // parts of the heads, up to 1024 workgroups (10,500 tokens into 4 bits 22 us, with 2048 23; single ones the same)
+  // parts of the heads, up to 1024 workgroups (15,400 tokens into 4 bits 22 us, with 2048 23; single ones the same)
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(a.pc.h_kv, 1024 / groups));
   const size_t lds = turn_bytes(a.rq.rot.rot, std::max(ROWS, kRotateRows<DT, D>));
   paged_rotated4_kernel<DT, D, INTERLEAVED><<<(unsigned)(a.q_wgs + groups * a.parts), kStoreThreads, lds, stream>>>(a);

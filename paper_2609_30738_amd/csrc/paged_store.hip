@@ -9,6 +9,7 @@
 //   paged_compact_kernel: 96 rows of 32 layers and 8 heads 7.4 us (lengths, positions, their ranks and rows are a
 //     chain of loads); 1792 to 256 rows of 32 layers of 32768, in int8, 63 us for 207 MB, read in rows of 256
 //     bytes.
+//   Into 4 bits no row waits for another's largest: 15,400 rows 17 us, the 96 kept ones 7.6.
 #include <limits.h>
 #include <math.h>
 
