@@ -540,8 +540,8 @@ int kv_paged_compact(const kv_problem* pr, const void* k, const void* v, const i
                      int32_t budget, int32_t keep_tail, const int32_t* budget_host,
                      const int32_t* budget_dev, const kv_paged_cache* pc, void* stream);
 
-/* Bytes of device workspace kv_paged_attention needs (0 if none; 256-byte alignment).  Returns 0 for
- * invalid arguments as well. */
+/* Bytes of device workspace kv_paged_attention needs (0 if none; 256-byte alignment), which may be more for a smaller max_q: a
+ * workspace for several takes the largest of theirs.  Returns 0 for invalid arguments as well. */
 size_t kv_paged_attention_workspace_bytes(const kv_paged_cache* pc, int32_t n_tok, int32_t max_q);
 
 /* Attention of the last tokens of every problem over its cache (one generated token, a few drafted ones, or

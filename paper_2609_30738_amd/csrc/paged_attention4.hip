@@ -550,7 +550,7 @@ template <int DT, int D, int NT> hipError_t attend(const PagedAttnArgs& a, hipSt
   }
   paged_attn4_kernel<DT, D, NT, true><<<dim3(h_kv, groups, (unsigned)a.shares), kThreads, lds, stream>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.shares == 1) return e;
   paged_join4_kernel<DT, D><<<dim3((unsigned)cols, h_kv, (unsigned)a.pc.n_prob), kThreads, 0, stream>>>(a, 16 * NT);
   return hipGetLastError();
 }

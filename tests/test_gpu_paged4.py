@@ -395,6 +395,19 @@ def test_attention_of_moving_logits(dtype, d, split, profile):
         assert torch.equal(out, _attend(pc, q, scale, n_q))
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("n", [1, 6, 40])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, -1e-40, 3.0])
+def test_attention_of_any_scale(dtype, d, n, scale):
+    """Negative, zero, denormal and large scales; short caches and ones of several rounds."""
+    rng = _rng(d, n, 31)
+    for lens in ([70, 300, 9], [1500, 0, 640]):
+        pc = _cache4(rng, dtype, 8, 2, d, 32, lens)
+        q = _q(rng, 3 * n, 8, d, dtype)
+        _say("attention4 scale", dtype, d, n, scale, lens)
+        _check4(pc, q, scale, [n] * 3, _attend(pc, q, scale, [n] * 3), f"scale {scale} {lens}")
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
 @pytest.mark.parametrize("n", [257, 600, 1025])
 @pytest.mark.parametrize("tokens", [1, 5])
@@ -413,6 +426,17 @@ def test_attention_of_many_unequal_problems(dtype, d, n, tokens):
     assert _lib.paged_attention_workspace_bytes(pc, T, tokens) > 0
     _say("attention4 many unequal", dtype, d, n, tokens)
     _check4(pc, q, 0.1, n_q, _attend(pc, q, 0.1, n_q), "many unequal", tokens)
+
+
+def test_attention_of_as_many_columns_as_the_chip_holds():
+    """256 fp32 tokens of 32 heads: a workgroup to a kv head's 32 columns goes over all problems, and nothing is joined."""
+    rng = _rng(33)
+    pc = _cache4(rng, "f32", 32, 8, 128, 64, [1300, 0, 290], max_len=1400)
+    n_q = [256, 0, 40]
+    q = _q(rng, 300, 32, 128, "f32")
+    assert _lib.paged_attention_workspace_bytes(pc, 300, 256) > 0
+    _say("attention4 many columns")
+    _check4(pc, q, 0.09, n_q, _attend(pc, q, 0.09, n_q), "many columns")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
