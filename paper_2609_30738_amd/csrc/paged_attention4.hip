@@ -17,7 +17,8 @@
 //   rows 26, in splits 34: latency of the rounds, and 5 for the join; over 32 caches of 100 rows 6.2, latency.
 //   Measured and left: K's codes as they are against e4m3 terms of the queries by v_mfma_scale_f32_16x16x128 (the same for
 //   long caches, 10 us more for five tokens: the queries have to be taken apart first), four tiles a step (the same), two
-//   steps of loads ahead (179 and 25.8, and 1 us more for short calls), four waves a SIMD (the same).
+//   steps of loads ahead (179 and 25.8, and 1 us more for short calls), four waves a SIMD for up to 16 columns (200), three for
+//   32 (their registers spill: 49 for five tokens), the next problem's lengths beside the merge (the same).
 #include <math.h>
 
 #include <algorithm>
