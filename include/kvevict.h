@@ -487,7 +487,7 @@ int kv_paged_append(const kv_paged_cache* pc, const void* k_new, const void* v_n
  *   (a c - b s, b c + a s),  c = factor cos(p freq[i]),  s = factor sin(p freq[i]);
  * elements from rot_dim on stay as they are.  inverse other than 0: by the angle -p freq[i], which is also the
  * gradient of the rotation: of out's gradient it makes x's.  freq: rot_dim / 2 values in radians a position, doubles on the
- * device; angles are formed in 64 bits, so that far positions (and negative ones) lose nothing; |p freq[i]| < 2^31.
+ * device; angles are products in 64 bits (off by at most 2^-30 at 2^24 radians), p of either sign; |p freq[i]| < 2^31.
  * layout other than KV_ROTARY_HALF and KV_ROTARY_INTERLEAVED, or a factor that is not finite: KV_ERR_ARG. */
 typedef struct kv_rotary {
   int32_t layout;
@@ -512,7 +512,8 @@ int kv_rotary_frequencies(int32_t family, double base, const double* params_host
 /* Rows rotated by their positions: token t's heads x + t * x_stride + h * d elements, h < heads, to
  * out + t * out_stride + h * d, at position pos[t] (pos [n_tok] on the device).  dtype of x and out; the products in fp32, rounded
  * once.  Strides as in kv_paged_append (0: heads * d).  out may be x with x's stride, or other
- * columns of the same wide rows; any other overlap of the memory that the two span is KV_ERR_ARG.  d in {64, 128}, heads >= 1, 1 <= n_tok <= 2^25. */
+ * columns of the same wide rows; any other overlap of the memory that the two span is KV_ERR_ARG.  d in {64, 128}, heads >= 1,
+ * 1 <= n_tok <= 2^25. */
 int kv_rotate(const kv_rotary* rot, int32_t dtype, int32_t heads, int32_t d, const void* x, int64_t x_stride,
               const int32_t* pos, int32_t n_tok, void* out, int64_t out_stride, void* stream);
 
