@@ -325,3 +325,46 @@ def test_append_rotated_binding_refuses():
     before = _bits(pc.k).copy()
     _lib.paged_append_rotated(pc, r, pos[:0], k[:0], k[:0], slots[:0], q=q[:0], q_out=torch.empty_like(q)[:0])
     assert np.array_equal(_bits(pc.k), before)
+
+
+def test_captured_prompts_and_single_rows():
+    """Prompts into 8-bit blocks of 128 rows (their turns take most of a workgroup's LDS) and single rows behind them, captured
+    once and replayed with other rows and positions, other work between the replays: every replay equals the eager calls."""
+    import torch
+    rng = _rng(51)
+    h_q, h_kv, d, R, lens = 4, 2, 128, 128, [200, 128, 3]
+    r, _, _ = _rotary("plain", 128, "half")
+    caches = [_pool(_lib.PagedCache.allocate("f32", "e4m3", h_q, h_kv, d, R, 9, 3, 3)) for _ in range(2)]
+    blocks = rng.permutation(9).reshape(3, 3)
+    first = [blocks[p, i // R] * R + i % R for p in range(3) for i in range(lens[p])]
+    then = [blocks[p, lens[p] // R] * R + lens[p] % R for p in range(3)]
+    slots = [_dev(np.asarray(x, np.int32)) for x in (first, then)]
+    qkv = [torch.zeros(len(x), h_q + 2 * h_kv, d, device="cuda") for x in (first, then)]
+    pos = [torch.zeros(len(x), dtype=torch.int32, device="cuda") for x in (first, then)]
+    outs = [[torch.zeros(len(x), h_q, d, device="cuda") for x in (first, then)] for _ in range(2)]
+
+    def step(pc, out):
+        for i in range(2):
+            _lib.paged_append_rotated(pc, r, pos[i], qkv[i][:, h_q:h_q + h_kv], qkv[i][:, h_q + h_kv:], slots[i], q=qkv[i][:, :h_q], q_out=out[i])
+
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step(caches[0], outs[0])
+    torch.cuda.synchronize()
+    for i in range(4):
+        for x, p in zip(qkv, pos):
+            x.copy_(_dev(rng.standard_normal(x.shape).astype(np.float32) * 3.0 ** i))
+            p.copy_(_dev(rng.integers(0, 1 << 20, len(p)).astype(np.int32)))
+        _say("captured prompts", i)
+        graph.replay()
+        other = torch.randn(200, 200, device="cuda") @ torch.randn(200, 200, device="cuda")
+        step(caches[1], outs[1])
+        torch.cuda.synchronize()
+        del other
+        for a, b in zip(outs[0], outs[1]):
+            assert torch.equal(a, b), i
+        for n in ("k", "v", "k_scale", "v_scale"):
+            x, y = (getattr(c, n).view(torch.uint8) for c in caches)
+            assert torch.equal(x, y), (i, n)
