@@ -1103,7 +1103,7 @@ int kv_paged_attention(const kv_paged_cache* c, const void* q, int64_t q_stride,
   a.shares = plan.shares;
   if (plan.shares) {
     a.prefix = static_cast<int32_t*>(ws);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kv::paged4_prefix_bytes(a.pc, max_q));
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kv::paged4_prefix_bytes(a.pc, max_q, plan.shares));
   }
   return launch_status(kv::launch_paged_attention(a, plan, static_cast<hipStream_t>(stream)));
 }

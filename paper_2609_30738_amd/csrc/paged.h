@@ -93,6 +93,7 @@ struct PagedAttnArgs {
   // up to 32 columns over 4-bit blocks: workgroups that share a unit's rounds (0: one for each problem), and their prefix sums
   int shares;
   int32_t* prefix;
+  int32_t* first;  // the problems that the shares begin in (null: not wanted)
   int group;           // h_q / h_kv, and its reciprocal in units of 2^-32, rounded up (0: a group of one)
   uint32_t group_inv;
 };
@@ -110,7 +111,7 @@ size_t paged_ws_bytes(const Paged& pc, int n_tok, int max_q, const PagedPlan& pl
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t stream);
 // Up to 32 columns at a time over 4-bit blocks (paged_attention4.hip).
 int paged4_shares(const Paged& pc, int max_q);
-size_t paged4_prefix_bytes(const Paged& pc, int max_q);
+size_t paged4_prefix_bytes(const Paged& pc, int max_q, int shares);
 size_t paged4_ws_bytes(const Paged& pc, int max_q, int shares);
 hipError_t launch_paged_attention4(PagedAttnArgs a, hipStream_t stream);
 // Blocks of a split that the prompt kernel of so many waves holds in LDS beside its tiles

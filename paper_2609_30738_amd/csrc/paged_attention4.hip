@@ -174,6 +174,7 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
     }
     if (writes && lane == 0) prefix[a.pc.n_prob] = T;
     if (at >= end) return;
+    if (a.first && g == 0 && wave == 0 && lane == 0) a.first[(int64_t)cg * a.shares + share] = p;
   } else {
     sp = span_of(a, p);
   }
@@ -470,17 +471,22 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
 }
 
 // One workgroup per (column, kv head, problem): the parts of the shares that the problem's rounds fall to, the waves' in
-// turn, kJoin at a time in flight.
-template <int DT, int D>
+// turn, kJoin at a time in flight.  BY_SHARE: per (column, kv head, share but the first), for the problem that it begins in
+// the middle of, where no earlier one does.
+template <int DT, int D, bool BY_SHARE>
 __global__ __launch_bounds__(kThreads) void paged_join4_kernel(PagedAttnArgs a, int COLS) {
   constexpr int E = D / 64, kJoin = 4;
   __shared__ float sh_a[kWaves][D], sh_m[kWaves], sh_s[kWaves];
-  const int col = blockIdx.x, g = blockIdx.y, p = blockIdx.z, G = a.group, cg = (int)((uint32_t)col / (uint32_t)COLS);
+  const int col = blockIdx.x, g = blockIdx.y, G = a.group, cg = (int)((uint32_t)col / (uint32_t)COLS);
   const int32_t* prefix = a.prefix + (int64_t)cg * (a.pc.n_prob + 1);
-  const int lo = prefix[p], hi = prefix[p + 1], T = prefix[a.pc.n_prob];
+  const int T = prefix[a.pc.n_prob], share = (int)blockIdx.z + 1;
+  int p = BY_SHARE ? a.first[(int64_t)cg * a.shares + share] : (int)blockIdx.z;
+  const uint32_t S = share_of(T, a.shares);
+  if (BY_SHARE && (uint32_t)share * S >= (uint32_t)T) return;  // no such share: its problem was not written
+  const int lo = prefix[p], hi = prefix[p + 1];
   const Span sp = span_of(a, p);
   if (col >= sp.n_tok * G) return;
-  const uint32_t S = share_of(T, a.shares);
+  if (BY_SHARE && ((uint32_t)share * S <= (uint32_t)lo || (uint32_t)(share - 1) * S > (uint32_t)lo)) return;
   const int s0 = (int)((uint32_t)lo / S), n = (int)((uint32_t)(hi - 1) / S) - s0 + 1;
   if (n == 1) return;  // one share had them all
   const int j = token_of(a, col);
@@ -541,7 +547,7 @@ namespace {
 
 int tiles_of(int64_t cols) { return cols <= 16 ? 1 : 2; }
 
-template <int DT, int D, int NT> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
+template <int DT, int D, int NT> hipError_t attend(PagedAttnArgs a, hipStream_t stream) {
   const int64_t cols = (int64_t)a.max_q * a.group;
   const unsigned h_kv = (unsigned)a.pc.h_kv, groups = (unsigned)((cols + 16 * NT - 1) / (16 * NT));
   const size_t lds = (size_t)kWaves * std::min<int64_t>(cols, 16) * (D + 4) * sizeof(float);
@@ -549,10 +555,18 @@ template <int DT, int D, int NT> hipError_t attend(const PagedAttnArgs& a, hipSt
     paged_attn4_kernel<DT, D, NT, false><<<dim3(h_kv, groups, (unsigned)a.pc.n_prob), kThreads, lds, stream>>>(a);
     return hipGetLastError();
   }
+  // The join by the fewer of problems and shares, since most of its workgroups only end: one token over 2048 caches of 100 rows
+  // (a bound of 4096) 126 us, by problems 169, four tokens 166 and 347; 100 caches of 1000 rows the same, four tokens over 64 39.8
+  // by as many shares, by problems 36.9.
+  const bool by_share = a.pc.n_prob > a.shares;
+  a.first = by_share ? a.prefix + (int64_t)groups * (a.pc.n_prob + 1) : nullptr;
   paged_attn4_kernel<DT, D, NT, true><<<dim3(h_kv, groups, (unsigned)a.shares), kThreads, lds, stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.shares == 1) return e;
-  paged_join4_kernel<DT, D><<<dim3((unsigned)cols, h_kv, (unsigned)a.pc.n_prob), kThreads, 0, stream>>>(a, 16 * NT);
+  if (by_share)
+    paged_join4_kernel<DT, D, true><<<dim3((unsigned)cols, h_kv, (unsigned)(a.shares - 1)), kThreads, 0, stream>>>(a, 16 * NT);
+  else
+    paged_join4_kernel<DT, D, false><<<dim3((unsigned)cols, h_kv, (unsigned)a.pc.n_prob), kThreads, 0, stream>>>(a, 16 * NT);
   return hipGetLastError();
 }
 template <int DT, int D> hipError_t attend(const PagedAttnArgs& a, hipStream_t stream) {
@@ -576,15 +590,15 @@ int paged4_shares(const Paged& pc, int max_q) {
   return (int)best;
 }
 
-size_t paged4_prefix_bytes(const Paged& pc, int max_q) {
+size_t paged4_prefix_bytes(const Paged& pc, int max_q, int shares) {
   const int64_t cols = (int64_t)max_q * pc.group(), nt = tiles_of(cols);
-  return (size_t)(((cols + 16 * nt - 1) / (16 * nt) * (pc.n_prob + 1) * (int64_t)sizeof(int32_t) + 255) / 256 * 256);
+  return (size_t)(((cols + 16 * nt - 1) / (16 * nt) * (pc.n_prob + 1 + shares) * (int64_t)sizeof(int32_t) + 255) / 256 * 256);
 }
 
 size_t paged4_ws_bytes(const Paged& pc, int max_q, int shares) {
   const int64_t cols = (int64_t)max_q * pc.group(), nt = tiles_of(cols), groups = (cols + 16 * nt - 1) / (16 * nt);
   const int64_t parts = groups * pc.h_kv * shares * 2 * std::min<int64_t>(cols, 16 * nt);
-  return paged4_prefix_bytes(pc, max_q) + (size_t)(parts * (pc.d + 2)) * sizeof(float);
+  return paged4_prefix_bytes(pc, max_q, shares) + (size_t)(parts * (pc.d + 2)) * sizeof(float);
 }
 
 hipError_t launch_paged_attention4(PagedAttnArgs a, hipStream_t stream) {

@@ -428,6 +428,27 @@ def test_attention_of_many_unequal_problems(dtype, d, n, tokens):
     _check4(pc, q, 0.1, n_q, _attend(pc, q, 0.1, n_q), "many unequal", tokens)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("n", [230, 600])
+@pytest.mark.parametrize("tokens", [1, 3])
+def test_attention_of_more_problems_than_shares(dtype, d, n, tokens):
+    """Many more requests than the workgroups that share a kv head's rows: short ones, empty ones, ones without tokens, long
+    ones that several workgroups share beside each other, at the start and at the end."""
+    rng = _rng(n, d, tokens, 7)
+    lens = np.where(rng.random(n) < 0.1, 0, rng.integers(1, 200, n))
+    lens[[0, 100, 101, 102, n - 1]] = 1900, 5000, 129, 3001, 1400
+    pc = _cache4(rng, dtype, 16, 8, d, 32, lens)
+    n_q = None if tokens == 1 else rng.integers(0, tokens + 1, n)
+    if tokens > 1:
+        n_q[[0, 100, 101, n - 1]] = tokens
+    T = n if n_q is None else int(n_q.sum())
+    q = _q(rng, T, 16, d, dtype)
+    _say("attention4 many problems", dtype, d, n, tokens)
+    out = _attend(pc, q, 0.1, n_q)
+    _check4(pc, q, 0.1, n_q, out, "many problems", tokens)
+    assert __import__("torch").equal(out, _attend(pc, q, 0.1, n_q))
+
+
 def test_attention_of_as_many_columns_as_the_chip_holds():
     """256 fp32 tokens of 32 heads: a workgroup to a kv head's 32 columns goes over all problems, and nothing is joined."""
     rng = _rng(33)
