@@ -27,6 +27,7 @@
 #include "common.h"
 #include "paged.h"
 #include "paged_codes.h"
+#include "paged_shares.h"
 #include "paged_span.h"
 
 namespace kv {
@@ -40,9 +41,6 @@ constexpr int kWaves = kAttnWaves;
 constexpr int kTiles4 = 2;
 template <int DT, int D, int NT> constexpr int kMinWaves4 = (NT == 1 ? 3 : 2) - (DT == kDtF32 && D == 128 ? 1 : 0);
 
-// Of a share: with one, its first loads are most of it, and there are more to join (one cache of up to 6000 rows 10.6 us, with
-// one round 11.5, with four 12.0; 8 of up to 2000 13.2, 13.2 and 14.3).
-constexpr int kLeastRounds4 = 2;
 constexpr int kRound4 = kWaves * 16 * kTiles4;  // rows of a workgroup's round
 
 typedef const __attribute__((address_space(4))) int32_t* uniform_ints;  // read by scalar loads
@@ -56,11 +54,6 @@ __device__ __forceinline__ int token_of(const PagedAttnArgs& a, int col) {
 __device__ __forceinline__ int rounds_of(const PagedAttnArgs& a, const Span& sp, int col0, int cols, int G) {
   const int n = min(sp.n_tok * G - col0, cols);
   return n <= 0 ? 0 : max(1, (int)((uint32_t)(sp.visible(token_of(a, col0 + n - 1)) + kRound4 - 1) / kRound4));
-}
-
-// Rounds to a share, of T in n shares.
-__device__ __forceinline__ int share_of(int T, int n) {
-  return max((int)(((uint32_t)T + (uint32_t)n - 1u) / (uint32_t)n), kLeastRounds4);
 }
 
 // Place of a share's part of a unit's column: slot 0 of a problem that begins before the share, 1 of one that ends behind it.
@@ -144,8 +137,8 @@ __global__ __launch_bounds__(kThreads, (kMinWaves4<DT, D, NT>)) void paged_attn4
       T += s.total;
     }
     const int S = share_of(T, a.shares);
-    at = (int)min((uint32_t)share * (uint32_t)S, (uint32_t)T);
-    end = min(at + S, T);
+    at = share_begin(T, S, share);
+    end = share_end(T, S, at);
     const bool writes = share == 0 && g == 0 && wave == 0;  // the sums, for the join
     if (at >= end && !writes) return;
     int32_t* prefix = a.prefix + (int64_t)cg * (a.pc.n_prob + 1);
