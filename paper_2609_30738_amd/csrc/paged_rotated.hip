@@ -158,7 +158,7 @@ __device__ __forceinline__ void store_heads(const Paged& pc, const Run& run, int
         if (old[h] >= s && old[h] < INFINITY) s = old[h];
       }
       if ((LONG ? threadIdx.x : lane) == 0 && g + h < end) scales[g + h] = s;
-      inv[h] = s > 0.f ? __uint_as_float((254u << 23) - __float_as_uint(s)) : 1.f;  // of a power of two
+      inv[h] = inv_scale(s);
     }
     auto put = [&](int t0, auto finite) __attribute__((always_inline)) {
 #pragma unroll
