@@ -9,7 +9,7 @@ import pytest
 
 from oracle import paged
 from paper_2609_30738_amd import _lib
-from tests.test_gpu_paged import _dev, _dt, _host, _image, _rng, _same_image, _say
+from tests.test_gpu_paged import _dev, _dt, _host, _image, _pool, _rng, _rows, _same_image, _say
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +60,91 @@ def test_held_scales_at_the_ends(dtype, qtype, d, layout, n_prob, tokens):
     for c, s, x in zip(codes, scales, (k32, v)):
         paged.append(c, s, _host(x), slots, qtype)
     _same_image(pc, codes, scales, "held scales")
+
+
+def _few(rng, n):
+    """Up to four rows a request."""
+    return rng.integers(0, 5, n)
+
+
+def _one_long(rng, n):
+    """One request of many rows among single and empty ones."""
+    adds = rng.integers(0, 2, n)
+    adds[n // 3] = 2 * n
+    return adds
+
+
+def _one_each(rng, n):
+    return np.ones(n, int)
+
+
+def _appended(rng, dtype, qtype, d, R, layout, rot, counts, n_prob, h_kv, odd=False):
+    """Three calls of up to four tokens a request on average, behind what the last ones left: codes and scales as defined,
+    the queries of two of them as kv_rotate's."""
+    import torch
+    steps = [counts(rng, n_prob) for _ in range(3)]
+    rows = np.sum(steps, 0)
+    stride = int(rows.max()) // R + 1
+    n_blocks = int((rows // R + 1).sum()) + 3
+    pc = _pool(_lib.PagedCache.allocate(dtype, qtype, 2 * h_kv, h_kv, d, R, n_blocks, n_prob, stride))
+    ids, table, at = rng.permutation(n_blocks), [], 0
+    for n in rows // R + 1:
+        table.append(ids[at:at + n])
+        at += n
+    f, factor = _lib.rotary_frequencies("bands", rot, 1e4, (8.0, 8192.0, 1.0, 4.0))
+    r = _lib.Rotary(layout, _dev(f), factor)
+    codes, scales = _image(pc)
+    codes, held = [x.copy() for x in codes], np.zeros(n_prob, int)
+    for step, adds in enumerate(steps):
+        slots = [table[p][i // R] * R + i % R for p in range(n_prob) for i in range(held[p], held[p] + adds[p])]
+        slots += [-1, n_blocks * R] if step == 1 and len(slots) + 2 <= 4 * n_prob else []
+        T = len(slots)
+        assert T <= 4 * n_prob
+        qkv = _rows(rng, T, 4 * h_kv, d, dtype) * 2.0 ** (3 * step)  # (scales that grow)
+        if odd:
+            for _ in range(6):
+                qkv[rng.integers(T), rng.integers(2 * h_kv, 4 * h_kv), rng.integers(d)] = float(rng.choice([np.nan, np.inf, -np.inf]))
+        q, k, v = qkv[:, :2 * h_kv], qkv[:, 2 * h_kv:3 * h_kv], qkv[:, 3 * h_kv:]
+        pos = _dev(rng.integers(0, 1 << 20, T).astype(np.int32))
+        want, k32 = torch.empty(q.shape, dtype=q.dtype, device="cuda"), _turned(r, k, pos)
+        _lib.rotate(r, q, pos, want)
+        q_out = torch.empty_like(want) if step != 1 else None
+        _say("rotated runs", dtype, qtype, d, R, layout, rot, counts.__name__, n_prob, step, T)
+        _lib.paged_append_rotated(pc, r, pos, k, v, _dev(np.asarray(slots, np.int32)), q=None if q_out is None else q, q_out=q_out)
+        for c, s, x in zip(codes, scales, (k32, v)):
+            paged.append(c, s, _host(x), np.asarray(slots), qtype)
+        _same_image(pc, codes, scales, f"step {step}")
+        assert q_out is None or torch.equal(q_out, want), step
+        held += adds
+
+
+@pytest.mark.parametrize("dtype,qtype", TYPES)
+@pytest.mark.parametrize("d,layout,rot", [(128, "half", 128), (64, "interleaved", 64), (128, "interleaved", 48), (64, "half", 16)])
+@pytest.mark.parametrize("R", [16, 32, 64, 128])
+@pytest.mark.parametrize("counts,n_prob", [(_few, 5), (_few, 90), (_one_long, 40), (_one_long, 130)])
+def test_runs_of_few_rows(dtype, qtype, d, layout, rot, R, counts, n_prob):
+    """Runs of a few rows, and one of up to a block's among single ones: past a wave's tile (4 to 16 rows), over ends of
+    blocks, behind rows whose scale grows, over several windows of 64 tokens."""
+    _appended(_rng(R, d, rot, n_prob, len(dtype), 1), dtype, qtype, d, R, layout, rot, counts, n_prob, 2)
+
+
+@pytest.mark.parametrize("dtype,qtype", TYPES)
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("counts,n_prob", [(_few, 60), (_one_long, 50)])
+def test_runs_of_numbers_that_are_none(dtype, qtype, layout, counts, n_prob):
+    """NaN and infinite elements in runs of all sizes."""
+    _appended(_rng(n_prob, len(dtype), 2), dtype, qtype, 64, 64, layout, 32, counts, n_prob, 2, odd=True)
+
+
+@pytest.mark.parametrize("dtype,qtype", TYPES)
+@pytest.mark.parametrize("R,h_kv", [(16, 1), (128, 3)])
+def test_one_row_of_many_requests(dtype, qtype, R, h_kv):
+    """More requests than a workgroup each: every workgroup takes several, the last window is not full."""
+    _appended(_rng(R, h_kv, len(dtype), 3), dtype, qtype, 64, R, "half", 64, _one_each, 1300, h_kv)
+
+
+def test_single_rows_and_few_of_them_with_many_heads():
+    """More heads than one round of a workgroup's waves takes, beside parts of the heads."""
+    rng = _rng(4)
+    for n_prob in (1, 3, 200):
+        _appended(rng, "bf16", "e4m3", 128, 64, "half", 128, _one_each, n_prob, 13)
