@@ -562,6 +562,18 @@ class _OnDevice:
         return self._raw_stream(index) if stream is None else stream.cuda_stream
 
 
+_FOUR_BITS = "float4_e2m1fn_x2"
+
+
+def _code_types():
+    """The types of a paged cache's codes, those of 4 bits where this torch has them."""
+    import torch
+    types = {torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8}
+    if hasattr(torch, _FOUR_BITS):
+        types[getattr(torch, _FOUR_BITS)] = KV_E2M1
+    return types
+
+
 class PagedCache(_OnDevice):
     """A batch of 8- or 4-bit caches in shared blocks (kv_paged_cache), around the caller's device tensors:
     k, v [n_blocks, h_kv, block_rows, d] (torch.float8_e4m3fn or int8), k_scale, v_scale
@@ -576,7 +588,7 @@ class PagedCache(_OnDevice):
                  max_len: Optional[int] = None):
         import torch
         n_blocks, h_kv, block_rows, d = k.shape
-        qtype = {torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8, torch.float4_e2m1fn_x2: KV_E2M1}.get(k.dtype)
+        qtype = _code_types().get(k.dtype)
         if qtype is None or v.dtype != k.dtype or v.shape != k.shape:
             raise ValueError("k and v must be float8_e4m3fn, int8 or float4_e2m1fn_x2 tensors of one shape")
         n_scales, scales = n_blocks * h_kv, torch.float32
@@ -624,8 +636,10 @@ class PagedCache(_OnDevice):
         lengths of 0."""
         import torch
         dev = torch.device("cuda") if device is None else torch.device(device)
-        qt = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8, "e2m1": torch.float4_e2m1fn_x2}[qtype]
         four = qtype == "e2m1"
+        if four and not hasattr(torch, _FOUR_BITS):
+            raise ValueError(f"4-bit caches need a torch that has {_FOUR_BITS}")
+        qt = getattr(torch, {"e4m3": "float8_e4m3fn", "int8": "int8", "e2m1": _FOUR_BITS}[qtype])
         pool = lambda: torch.empty(n_blocks, h_kv, block_rows, d // 2 if four else d, dtype=torch.uint8, device=dev).view(qt)
         scales = lambda: (torch.empty(n_blocks, h_kv, d // 32, block_rows, dtype=torch.uint8, device=dev)
                           .view(torch.float8_e8m0fnu) if four else
