@@ -517,12 +517,17 @@ def decode_attention(cb: CacheBatch, q, k_cache, v_cache, k_new, v_new, scale: f
                                      _stream(stream)), "kv_decode_attention")
 
 
+def _place(index: int) -> str:
+    """A device by its index, for what is said to the caller (below 0: that of an object on the host)."""
+    return f"cuda:{index}" if index >= 0 else "a GPU"
+
+
 def _token_rows(t, dtype, index: int, heads: int, d: int, name: str):
     """Address and token stride of [tokens, heads, d] rows on device `index`; tokens may lie apart (slices of a
     projection)."""
     n, h, e = t.shape if t.dim() == 3 else (0, -1, -1)
     if h != heads or e != d or t.dtype is not dtype or t.get_device() != index:
-        raise ValueError(f"{name} must be a {dtype} tensor [tokens, {heads}, {d}] on device {index}")
+        raise ValueError(f"{name} must be a {dtype} tensor [tokens, {heads}, {d}] on {_place(index)}")
     apart, between, one = t.stride()
     if one != 1 or (between != d and heads > 1):
         raise ValueError(f"the heads of a token must be contiguous in {name}")
@@ -536,7 +541,7 @@ def _token_rows(t, dtype, index: int, heads: int, d: int, name: str):
 def _flat(t, dtype, index: int, n: int, name: str):
     """Address of a contiguous tensor of at least n elements on device `index`."""
     if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous() or t.numel() < n:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of at least {n} elements on device {index}")
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of at least {n} elements on {_place(index)}")
     return t.data_ptr()
 
 

@@ -28,6 +28,17 @@ def test_8_bit_caches_do_without_4_bit_types(monkeypatch):
         _lib.PagedCache("bf16", 4, pool, pool, pool, pool, table, lens)
 
 
+def test_refusals_name_the_place():
+    """A tensor on the host is refused as one that is not on a GPU, by no index that the caller never gave."""
+    table, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    pool = torch.zeros(8, 2, 16, 64, dtype=torch.int8)
+    with pytest.raises(ValueError, match="^table must be a contiguous torch.int32 tensor of at least 0 elements on a GPU$"):
+        _lib.PagedCache("bf16", 4, pool, pool, torch.zeros(8, 2), torch.zeros(8, 2), table, lens)
+    for index, place in ((1, "cuda:1"), (-2, "a GPU")):
+        with pytest.raises(ValueError, match=rf"^x must be a torch.float32 tensor \[tokens, 2, 64\] on {place}$"):
+            _lib._token_rows(torch.zeros(3, 2, 64), torch.float32, index, 2, 64, "x")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("qtype", ["e4m3", "int8"])
 def test_appending_without_4_bit_types(monkeypatch, qtype):
