@@ -3,6 +3,9 @@
 //
 // paged_attn4_kernel: columns, references and weights as in paged_attention.hip's kernel.
 //     S^T = K Q^T,  O^T = V^T P^T  by v_mfma_f32_16x16x32_bf16.
+//   Weights of bf16 queries: two bf16 terms for up to 16 columns (as close to 64 bits as fp32 weights), one for more, 2^-9 of
+//   each.  Up to five tokens of 16 requests, root mean square over the output's: 0.00165 from 64 bits, of which 0.00159 is
+//   the output's own rounding; with two terms 0.00159, and 28.7 us for 26.3.
 //   Codes.  The scales belong to a row and 32 of its elements, so they go into the operands, where the conversion from four
 //   bits applies them at no cost (a code times its scale is exact in bf16).  A lane's operand of K is a quarter of a row: at
 //   d = 128 one 16-byte load and one scale.  For V a lane takes D / 16 elements of each of its rows, a word at d = 128, and
@@ -11,9 +14,10 @@
 //   Shares.  Caches of more than a split's rows are one long axis of rounds of 128 rows, problem after problem, that every
 //   unit's workgroups share equally, as many as the chip holds at once: unequal caches cost no idle CUs, and a workgroup
 //   begins once.  The parts of problems that fall to several shares are joined by paged_join4_kernel.
-//   Bound by the cache's reads: one token over 32 caches of 32768 rows (1.07 GB) 180 us, 6.0 TB/s; its loads alone take 175.
-//   24 ragged ones of up to 24001 rows in blocks of 16 (0.41 GB, eight query heads to a kv head) 78 us, 5.2 TB/s (in splits of
-//   2048 rows 86): the scales of 16 rows are half a line; in blocks of 64 74.  Up to five tokens of 16 requests of up to 6001
+//   Bound by the cache's reads: one token over 32 caches of up to 32768 rows (1.07 GB) 183 us, 5.8 TB/s, of which this kernel
+//   takes 172 to 177 (at an earlier step, of 188 us, the loads alone took 175).
+//   24 ragged ones of up to 24001 rows in blocks of 16 (0.41 GB, eight query heads to a kv head) 79 us, 5.1 TB/s (in splits of
+//   2048 rows 86), this kernel 73: the scales of 16 rows are half a line; in blocks of 64 74 in all.  Up to five tokens of 16 requests of up to 6001
 //   rows 26, in splits 34: latency of the rounds, and 5 for the join; over 32 caches of 100 rows 6.2, latency.
 //   Measured and left: K's codes as they are against e4m3 terms of the queries by v_mfma_scale_f32_16x16x128 (the same for
 //   long caches, 10 us more for five tokens: the queries have to be taken apart first), four tiles a step (the same), two
@@ -569,7 +573,9 @@ template <int DT, int D> hipError_t attend(const PagedAttnArgs& a, hipStream_t s
 }  // namespace
 
 // Shares of a unit, a (kv head, group of columns): the fewest that take the least time in rounds of the workgroups that the
-// chip holds at once.
+// chip holds at once.  The more columns the bound max_q admits, the fewer each group gets (fp32 turns: with 8 heads one from
+// 32 groups on), though requests of a token all fall to the first: 60 of them over 32768 rows beside a turn of 64 (256) fp32
+// tokens take 7.5 ms (29.7), by themselves 0.47; over 8 bits, where every problem has workgroups, 5.3 (6.3).
 int paged4_shares(const Paged& pc, int max_q) {
   const int64_t cols = (int64_t)max_q * pc.group();
   const int nt = tiles_of(cols);

@@ -1,6 +1,6 @@
 // Device side of the paged cache: codes and scales.
 //
-// 8 bits.  // A scale is a power of two (or 0: a block of zeros), the least one with max|x| <= 448 s for e4m3
+// 8 bits.  A scale is a power of two (or 0: a block of zeros), the least one with max|x| <= 448 s for e4m3
 // and 127 s for int8 over the block's finite values.  A value is code * s: exact in bf16, whatever the
 // code, while it is a normal number (e4m3's smallest code at scales below 2^-117 is not: it may become 0).
 // A power of two costs e4m3 nothing (its precision does not depend on the scale) and int8 up to one bit of

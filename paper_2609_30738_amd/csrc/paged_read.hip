@@ -3,7 +3,9 @@
 // paged_rows_kernel: one workgroup of four waves per (64 rows, kv head, problem), a wave 16 rows of K and of V, whose block
 //   is the wave's.  A lane writes 16 bytes; the codes of all 16 rows are in flight together.
 //   Bound by HBM: 44,400 rows of 8 heads of 128 from 4 bits (48 MB read, 182 MB written) 37 us, 6.2 TB/s, 15,400 rows 16.7;
-//   24 caches of up to 131 rows 4.7: offsets, tables and lengths in one step of loads, codes and scales in another.
+//   24 caches of up to 131 rows 4.7: offsets, tables and lengths in one step of loads, codes and scales in another.  58,584 rows
+//   from 8 bits 70 us, 5.2 TB/s (from 4 56), into fp32 121 (121), of 64 elements 28 (24).  Workgroups are launched for the bound on the
+//   lengths: 2048 caches of 100 rows 233 us under a bound of 128, 2785 under 32768.
 #include <math.h>
 
 #include <algorithm>

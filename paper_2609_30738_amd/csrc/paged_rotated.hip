@@ -321,8 +321,16 @@ __global__ __launch_bounds__(kStoreThreads) void paged_rotated4_kernel(AppendRot
 
 namespace {
 
-// Whether 8-bit appending takes the runs as long ones: by the tokens to a request.  2000 single rows 28.6 us as short ones,
-// 57 as long ones; 1200 tokens of four prompts in blocks of 64 rows 69 and 21.
+// Whether 8-bit appending takes the runs as long ones: by the tokens to a request, a padded batch's among them, for the whole
+// call.  In us as short and as long ones, in blocks of 16 / 64 / 128 rows:
+//   with queries: 2000 single rows 28 / 28 / 42 and 103 / 382 / 367; five rows of 64 requests 12 / 12 / 13 and 23 / 64 / 61;
+//     one prompt of 2048 tokens beside 255 requests without rows 33 / 94 / 152 and 15 / 17 / 22, beside 255 single rows
+//     33 / 80 / 151 and 94 / 331 / 316;
+//   without: 20 rows of 64 requests 19 / 28 / 23 and 14 / 25 / 24, four prompts of 300 tokens 17 / 50 / 95 and 12 / 16 / 18.
+// A workgroup takes the runs that fall to it one after the other, and in blocks of 64 rows all runs of 64 tokens fall to one.
+// So requests of 5 to about 16 rows each would be faster as short runs, where a prompt that brings a call to as many rows to a
+// request is faster as long ones; a prompt beside single rows is slow either way (kv_rotate of both and kv_paged_append:
+// 32 / 41 / 52).
 bool is_long(const Paged& pc, int n_tok) { return n_tok > 4 * (int64_t)pc.n_prob; }
 
 template <int DT, int D, bool INTERLEAVED> hipError_t append4(AppendRotatedArgs a, hipStream_t stream) {
